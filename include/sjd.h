@@ -47,7 +47,11 @@ enum sjd_status {
     SJD_ECAPACITY = -5  /* more sequences / context than created for  */
 };
 
-enum sjd_dtype { SJD_F32 = 0, SJD_BF16 = 1 };
+enum sjd_dtype {
+    SJD_F32 = 0,
+    SJD_BF16 = 1,
+    SJD_FP8 = 2  /* caches of the tree operators only: e4m3 codes, one power of two a token and key/value head as their scale */
+};
 
 /* kernel_flags bits */
 enum {
@@ -311,6 +315,124 @@ int sjd_op_sampling_rows(void *hip_stream, const float *logits_c, const float *l
 
 /* out[4*i .. 4*i+3] = Philox4x32-10(counter = (i, row, seq, 0), key = seed), i < n. */
 int sjd_op_philox(void *hip_stream, uint64_t seed, uint32_t row, uint32_t seq, uint32_t *out, int32_t n);
+
+/* ---- operators of a step of tree speculation: rotary positions, the paged key/value cache (plain or quantised), attention of
+ * a tree of drafts over it, verification of the tree.  A window of drafts is a tree without branches, and a single token a
+ * tree of one node.
+ *
+ * Unlike the single operations above these allocate nothing, enqueue their kernels on `hip_stream` and return at once;
+ * they can be captured into a HIP graph, and a graph that is replayed reads the lengths, tables and positions that are in device
+ * memory then.  Pointers are DEVICE pointers on the stream's device, which is the current one, unless HOST is said; strides are in
+ * elements.  Calls that may run at the same time need workspaces of their own and must not write what the other reads.
+ *
+ * Ragged rows: rows [row_start[b], row_start[b + 1]) of the arrays are sequence b's, b < n_seqs (row_start has n_seqs + 1
+ * entries, ascending; what lies outside [0, n_rows] is cut off), and row row_start[b] + i belongs to position
+ * first_pos[b] + i of its cache.  Outputs of rows of no sequence are left as they were.
+ *
+ * Sizes and pointers are checked on the host (SJD_EINVAL, nothing enqueued).  What is in device memory is checked by the kernels:
+ * a page table entry outside [0, n_pages), or a position outside [0, pages_per_seq * page_tokens), is never
+ * followed: writes to it are dropped, reads of it give zeros, attention does not see it. */
+
+/* A paged cache: plain data; the caller owns both allocations.  Pages of one sequence are listed in its row of the page
+ * table; an unused entry is any value outside [0, n_pages).  Sequences may share pages that nobody writes.  The layout inside a
+ * page is private: it is written by sjd_op_cache_write and sjd_op_cache_compact. */
+typedef struct {
+    void *pages;               /* n_pages * sjd_cache_page_bytes() bytes, 16-byte aligned                       */
+    const int32_t *page_table; /* [n_seqs][pages_per_seq]                                                       */
+    int32_t n_pages, page_tokens; /* page_tokens: a multiple of 32                                              */
+    int32_t n_kv_heads, head_dim; /* head_dim: 32, 64, 96, 128, 192 or 256                                      */
+    int32_t dtype;             /* sjd_dtype of what is stored                                                   */
+    int32_t n_seqs, pages_per_seq;
+} sjd_kv_cache;
+
+/* *bytes (HOST) of one page.  Only page_tokens, n_kv_heads, head_dim and dtype of `cache` are read. */
+int sjd_cache_page_bytes(const sjd_kv_cache *cache, uint64_t *bytes);
+
+/* Writes rows of keys and values, k and v [n_rows][n_kv_heads][head_dim] of src_dtype (SJD_F32 or SJD_BF16; a row's heads are
+ * contiguous, rows k_stride / v_stride apart), to positions first_pos[b] + i.
+ * SJD_FP8: a token's keys of one head share the scale 2^e, and so do its values, with the smallest e in [-100, 119] for which
+ * max |x| <= 448 * 2^e over the finite elements; the code of x is the e4m3 number nearest to x * 2^-e, ties to even, at most
+ * 448 in magnitude.  Infinities and NaN become NaN.  SJD_BF16 rounds to nearest even, SJD_F32 keeps the value.
+ * Nothing else in the pages changes. */
+int sjd_op_cache_write(void *hip_stream, const sjd_kv_cache *cache, int32_t src_dtype, const void *k, int64_t k_stride, const void *v,
+                       int64_t v_stride, const int32_t *row_start, const int32_t *first_pos, int32_t n_rows);
+
+/* The way back: k and v [n_rows][n_kv_heads][head_dim] (contiguous) of dst_dtype receive what is stored at positions first_pos[b] + i:
+ * for SJD_FP8 code * 2^e, exact in either type. */
+int sjd_op_cache_read(void *hip_stream, const sjd_kv_cache *cache, int32_t dst_dtype, void *k, void *v, const int32_t *row_start,
+                      const int32_t *first_pos, int32_t n_rows);
+
+/* Keeps a path of a tree: of the rows at positions first_pos[b] + 0, 1, ..., those of nodes path[b][0 .. path_len[b] - 1] move to
+ * positions first_pos[b] + 0 .. path_len[b] - 1, bit for bit.  path [n_seqs][max_path]; its nodes ascend, and what comes
+ * from the first that does not (or is negative) is ignored. */
+int sjd_op_cache_compact(void *hip_stream, const sjd_kv_cache *cache, const int32_t *first_pos, const int32_t *path,
+                         const int32_t *path_len, int32_t max_path);
+
+/* Frequencies of a rotary embedding for sjd_op_rotary: table [rotary_dim / 2] (HOST; the caller copies it to the device), entry i =
+ * f_i / (2 pi) in units of 2^-64 turns, f_i = theta^(-2i / rotary_dim) radians a position, scaled for contexts `factor` times
+ * as long as the trained_ctx positions that a model was trained on:
+ *   SJD_ROPE_PLAIN   not at all;
+ *   SJD_ROPE_LINEAR  f_i / factor;
+ *   SJD_ROPE_BASE    theta * factor^(rotary_dim / (rotary_dim - 2)) in place of theta (rotary_dim > 2);
+ *   SJD_ROPE_PARTS   by how many turns n_i = trained_ctx * f_i / (2 pi) the pair makes: f_i from high_turns on, f_i / factor
+ *                    up to low_turns, and between them f_i * (g + (1 - g) / factor), g = (n_i - low_turns) / (high_turns - low_turns).
+ * rotary_dim: even, >= 2; theta > 1, factor >= 1 (LINEAR and on), trained_ctx > 0 and 0 <= low_turns < high_turns (PARTS). */
+enum sjd_rope_scaling { SJD_ROPE_PLAIN = 0, SJD_ROPE_LINEAR = 1, SJD_ROPE_BASE = 2, SJD_ROPE_PARTS = 3 };
+int sjd_rope_table(int32_t rotary_dim, double theta, int32_t scaling, double factor, double trained_ctx, double low_turns,
+                   double high_turns, uint64_t *table);
+
+/* Turns pairs of the first rotary_dim dimensions of every head by positions[row] * f_i and multiplies them by `magnitude`; the
+ * other dimensions are copied.  Pairs are (i, i + rotary_dim / 2), or (2i, 2i + 1) with `interleaved`.  x and y [n_rows][heads][head_dim]
+ * of `dtype` (heads contiguous, rows a stride apart), in one call for queries (n_heads) and keys (n_kv_heads; 0: none).  y may
+ * be x with the same stride, and may not overlap it otherwise.  Angles are exact to 2^-33 turns at any position; a negative position
+ * turns back.  head_dim <= 512. */
+int sjd_op_rotary(void *hip_stream, int32_t dtype, int32_t interleaved, const uint64_t *table, int32_t rotary_dim, float magnitude,
+                  const int32_t *positions, int32_t n_rows, int32_t head_dim, const void *q, int64_t q_stride, void *q_out,
+                  int64_t q_out_stride, int32_t n_heads, const void *k, int64_t k_stride, void *k_out, int64_t k_out_stride,
+                  int32_t n_kv_heads);
+
+/* Masks and depths of a tree from its parents (all HOST): node i < n has parent parents[i] < i (negative: a root); bit j of
+ * mask[i][j / 32] is set where node j is i or one of its ancestors, mask [n][mask_words]; depth[i] (may be NULL) = number
+ * of ancestors.  SJD_EINVAL: a parent that does not come first, or mask_words * 32 < n. */
+int sjd_tree_masks(const int32_t *parents, int32_t n, int32_t mask_words, uint32_t *mask, int32_t *depth);
+
+/* Attention of the rows of trees over a cache that holds them already: node i of sequence b (row row_start[b] + i, position
+ * ctx_len[b] + i) attends to positions [0, ctx_len[b]) and to those nodes j of its own tree whose bit j % 32 of
+ * mask[row][j / 32] is set; with mask NULL to nodes 0 .. i (a window).  Row by row out = softmax(scale * q k) v with one kv head to
+ * n_heads / n_kv_heads query heads; a row that sees nothing gets zeros.  Keys and values that a row does not see do not touch it,
+ * infinities and NaN included.
+ * q and out [n_rows][n_heads][head_dim] of `dtype`: SJD_F32 for an SJD_F32 cache, SJD_BF16 for the others.  Probabilities are rounded
+ * to bf16 for the product with values there; sums and the softmax are fp32.  scale > 0, or 0 for 1 / sqrt(head_dim).
+ * max_rows: no tree has more rows (those behind are left as they were).  max_ctx: what ctx_len is expected to reach; it only
+ * chooses how the work is divided, and with it the order of sums.  The workspace (16-byte aligned) has at least the bytes that
+ * sjd_op_tree_attention_workspace writes to *bytes (HOST; may be 0, then it may be NULL) for the same arguments.  SJD_ECAPACITY: it is smaller. */
+int sjd_op_tree_attention_workspace(const sjd_kv_cache *cache, int32_t n_heads, int32_t max_rows, int32_t max_ctx, uint64_t *bytes);
+int sjd_op_tree_attention(void *hip_stream, const sjd_kv_cache *cache, int32_t dtype, const void *q, int64_t q_stride, void *out,
+                          int64_t out_stride, const int32_t *row_start, const int32_t *ctx_len, const uint32_t *mask, int32_t mask_words,
+                          int32_t n_rows, int32_t n_heads, float scale, int32_t max_rows, int32_t max_ctx, void *workspace,
+                          uint64_t workspace_bytes);
+
+/* Verification of trees of drafted tokens: Eq. 2 and 3 of the paper for a node's drafted successors one after the other, from given
+ * random words.  tokens and parents [n_rows]: node i of a sequence (row row_start[b] + i) carries a token and the index of its
+ * parent, which is smaller; node 0 is the root (the last final token, which is not tested).  Row i of p [n_rows][vocab], p_stride apart: the
+ * target's probabilities of what follows node i.  Row i of q: the draft model's, from which i's children were drawn; q NULL: they were
+ * not drawn but chosen (a model's likeliest tokens), each a proposal of probability 1.
+ * From node 0 on, the children x of the node reached, in the order of their indices:  with rho_0 = p and S_0 = 1, child k is
+ * accepted where r q(x) S_k < rho_k(x), r = (accept_words[its row] + 1/2) 2^-32; if not, rho_{k+1} = max(0, rho_k - S_k q) and
+ * S_{k+1} = sum rho_{k+1}.  Where no child is accepted, or max_path nodes are reached, next_token is drawn from the last rho
+ * (from p, where that is all 0): the first id whose cumulated weight exceeds the share draw_words[b] / 2^64 of all.  In distribution the
+ * accepted tokens and the next one are what the target alone would have produced.  All of it is specified bit for bit: double
+ * precision, the products in the order (r q) S and S q, sums of trunc(min(rho, 1) 2^44); p and q that are NaN count as 0 where they
+ * are tested or drawn.  A token outside [0, vocab) is rejected.
+ * Outputs: path [n_seqs][max_path], the nodes reached, node 0 first, -1 behind them; path_len [n_seqs] (accepted drafts + 1; 0 for a
+ * sequence without rows); next_token [n_seqs] (-1 without rows, or where p is all 0).  path and path_len are what
+ * sjd_op_cache_compact takes.  max_rows <= 1024, vocab <= 524288; rows of a tree behind max_rows are ignored.  The workspace
+ * (16-byte aligned) as in sjd_op_tree_attention. */
+int sjd_op_tree_verify_workspace(int32_t n_rows, int32_t n_seqs, int32_t vocab, uint64_t *bytes);
+int sjd_op_tree_verify(void *hip_stream, const int32_t *tokens, const int32_t *parents, const int32_t *row_start, const float *p,
+                       int64_t p_stride, const float *q, int64_t q_stride, const uint32_t *accept_words, const uint64_t *draw_words,
+                       int32_t *path, int32_t *path_len, int32_t *next_token, int32_t n_rows, int32_t n_seqs, int32_t vocab,
+                       int32_t max_rows, int32_t max_path, void *workspace, uint64_t workspace_bytes);
 
 #ifdef __cplusplus
 }

@@ -8,7 +8,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libsjd.so")
 _lib = None
 
-F32, BF16 = 0, 1
+F32, BF16, FP8 = 0, 1, 2
 KERNELS_REFERENCE, NO_GRAPH, KERNELS_ROWGROUPS, ATTENTION_CHUNKED, KERNELS_TILES, NO_L2_WARM, TILES_256_ROWS, NO_ROW_SPLIT, NO_MIXED_WIDTH, NO_K_ROTATION = 1, 2, 4, 8, 16, 32, 64, 128, 256, 512
 KEEP_LOGITS, NO_HEAD_FUSION = 1024, 2048
 OK, EINVAL, ENOMEM, ESTATE, EDEVICE, ECAPACITY = 0, -1, -2, -3, -4, -5
@@ -25,6 +25,11 @@ class ModelDesc(C.Structure):
                                          "sample_lo", "sample_hi")] + \
                [("rms_eps", C.c_float), ("rope_theta", C.c_float)] + \
                [(n, C.c_int32) for n in ("dtype", "max_seqs", "max_ctx", "window", "kv_page_tokens", "kernel_flags")]
+
+
+class KvCacheDesc(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("page_table", C.c_void_p)] + \
+               [(n, C.c_int32) for n in ("n_pages", "page_tokens", "n_kv_heads", "head_dim", "dtype", "n_seqs", "pages_per_seq")]
 
 
 _VPP = C.POINTER(C.c_void_p)
@@ -89,6 +94,18 @@ def lib():
                                            C.c_void_p, C.c_int32, C.POINTER(C.c_float)]
         L.sjd_set_token_ranges.argtypes = [C.c_void_p, C.c_int32, IP, IP, C.c_int32]
         L.sjd_op_philox.argtypes = [C.c_void_p, C.c_uint64, C.c_uint32, C.c_uint32, C.c_void_p, C.c_int32]
+        P, I, I64, CP, U64P = C.c_void_p, C.c_int32, C.c_int64, C.POINTER(KvCacheDesc), C.POINTER(C.c_uint64)
+        L.sjd_cache_page_bytes.argtypes = [CP, U64P]
+        L.sjd_op_cache_write.argtypes = [P, CP, I, P, I64, P, I64, P, P, I]
+        L.sjd_op_cache_read.argtypes = [P, CP, I, P, P, P, P, I]
+        L.sjd_op_cache_compact.argtypes = [P, CP, P, P, P, I]
+        L.sjd_rope_table.argtypes = [I, C.c_double, I, C.c_double, C.c_double, C.c_double, C.c_double, P]
+        L.sjd_op_rotary.argtypes = [P, I, I, P, I, C.c_float, P, I, I, P, I64, P, I64, I, P, I64, P, I64, I]
+        L.sjd_tree_masks.argtypes = [P, I, I, P, P]
+        L.sjd_op_tree_attention_workspace.argtypes = [CP, I, I, I, U64P]
+        L.sjd_op_tree_attention.argtypes = [P, CP, I, P, I64, P, I64, P, P, P, I, I, I, C.c_float, I, I, P, C.c_uint64]
+        L.sjd_op_tree_verify_workspace.argtypes = [I, I, I, U64P]
+        L.sjd_op_tree_verify.argtypes = [P, P, P, P, P, I64, P, I64, P, P, P, P, P, I, I, I, I, I, P, C.c_uint64]
         _lib = L
     return _lib
 
@@ -320,3 +337,223 @@ def op_philox(seed, row, seq, n):
     out = torch.zeros(4 * n, dtype=torch.int32, device="cuda")
     _check(lib().sjd_op_philox(_stream_ptr(), seed, row, seq, out.data_ptr(), n))
     return out.cpu().numpy().view(np.uint32).reshape(n, 4)
+
+
+# ---- operators of a step of tree speculation.  They enqueue their work on the current stream of their tensors' device and return.
+
+_CACHE_DTYPES = {"f32": F32, "bf16": BF16, "fp8": FP8}
+_SCALINGS = {"none": 0, "linear": 1, "base": 2, "parts": 3}
+
+
+def _need(ok, message):
+    if not ok:
+        raise SjdError(EINVAL, message)
+
+
+def _same_device(first, *others):
+    """The device of `first`; the other tensors (None: not given) have to be there too."""
+    _need(first.is_cuda, "tensors must be on a GPU")
+    _need(all(t is None or t.device == first.device for t in others), "tensors are on different devices")
+    return first.device
+
+
+def _index(t, n, name, dtype="int32"):
+    import torch
+    _need(t.dtype == getattr(torch, dtype) and t.dim() == 1 and t.is_contiguous() and (n is None or t.numel() == n),
+          f"{name} must be a contiguous {dtype} vector" + ("" if n is None else f" of {n}"))
+
+
+def _heads_of(x, heads, hd, name):
+    """x [rows, heads, hd] with contiguous heads: its row stride."""
+    import torch
+    _need(x.dtype in (torch.float32, torch.bfloat16), f"{name} must be float32 or bfloat16")
+    _need(x.dim() == 3 and x.shape[1] == heads and x.shape[2] == hd, f"{name} must be [rows, {heads}, {hd}]")
+    _need(x.numel() == 0 or ((hd == 1 or x.stride(2) == 1) and (heads == 1 or x.stride(1) == hd)), f"{name}: the heads of a row must be contiguous")
+    return x.stride(0) if x.shape[0] > 1 else heads * hd
+
+
+def _on(device):
+    import torch
+    return torch.cuda.device(device)
+
+
+class KvCache:
+    """A paged key/value cache ("f32", "bf16" or "fp8") and its page table, int32 CUDA [n_seqs, pages_per_seq]; entries outside
+    [0, n_pages) are unused.  Owns its pages (zeroed); the table is the caller's and may change between calls."""
+
+    def __init__(self, dtype, n_pages, page_tokens, n_kv_heads, head_dim, page_table):
+        import torch
+        _need(dtype in _CACHE_DTYPES, "dtype must be f32, bf16 or fp8")
+        _need(page_table.is_cuda and page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.is_contiguous(),
+              "page_table must be a contiguous int32 CUDA matrix")
+        self.dtype, self.n_kv_heads, self.head_dim, self.page_table = dtype, n_kv_heads, head_dim, page_table
+        self.n_seqs, self.device = page_table.shape[0], page_table.device
+        self.desc = KvCacheDesc(None, page_table.data_ptr(), n_pages, page_tokens, n_kv_heads, head_dim, _CACHE_DTYPES[dtype], *page_table.shape)
+        n = C.c_uint64(0)
+        _check(lib().sjd_cache_page_bytes(C.byref(self.desc), C.byref(n)))
+        _need(n_pages >= 1, "n_pages must be positive")
+        self.pages = torch.zeros(n_pages * n.value, dtype=torch.uint8, device=self.device)
+        self.desc.pages = self.pages.data_ptr()
+
+    def ref(self):
+        return C.byref(self.desc)
+
+
+def op_cache_write(cache, k, v, row_start, first_pos):
+    """Writes k and v [rows, n_kv_heads, head_dim] (float32 or bfloat16; rows may be strided) to positions first_pos[b] + i of sequence b =
+    rows row_start[b] + i.  row_start int32 [n_seqs + 1], first_pos int32 [n_seqs]."""
+    _same_device(cache.page_table, k, v, row_start, first_pos)
+    ks, vs = _heads_of(k, cache.n_kv_heads, cache.head_dim, "k"), _heads_of(v, cache.n_kv_heads, cache.head_dim, "v")
+    _need(k.dtype == v.dtype and k.shape == v.shape, "k and v must have one dtype and shape")
+    _index(row_start, cache.n_seqs + 1, "row_start")
+    _index(first_pos, cache.n_seqs, "first_pos")
+    with _on(cache.device):
+        _check(lib().sjd_op_cache_write(_stream_ptr(), cache.ref(), _dtype_code(k), k.data_ptr(), ks, v.data_ptr(), vs, row_start.data_ptr(),
+                                        first_pos.data_ptr(), k.shape[0]))
+
+
+def op_cache_read(cache, row_start, first_pos, n_rows, dtype=None, out=None):
+    """-> (k, v) [n_rows, n_kv_heads, head_dim] of `dtype` (bfloat16 unless given): what is stored at positions first_pos[b] + i of sequence
+    b, in rows row_start[b] + i.  out: a pair of such tensors to write to.  Rows of no sequence are not written."""
+    import torch
+    _same_device(cache.page_table, row_start, first_pos, *(out or ()))
+    _index(row_start, cache.n_seqs + 1, "row_start")
+    _index(first_pos, cache.n_seqs, "first_pos")
+    dtype = dtype or (out[0].dtype if out else torch.bfloat16)
+    _need(dtype in (torch.float32, torch.bfloat16), "dtype must be float32 or bfloat16")
+    shape = (n_rows, cache.n_kv_heads, cache.head_dim)
+    if out is None:
+        out = tuple(torch.empty(shape, dtype=dtype, device=cache.device) for _ in range(2))
+    _need(all(t.shape == shape and t.dtype == dtype and t.is_contiguous() for t in out), "out must be two contiguous tensors of the result's shape")
+    with _on(cache.device):
+        _check(lib().sjd_op_cache_read(_stream_ptr(), cache.ref(), _dtype_code(out[0]), out[0].data_ptr(), out[1].data_ptr(), row_start.data_ptr(),
+                                       first_pos.data_ptr(), n_rows))
+    return out
+
+
+def op_cache_compact(cache, first_pos, path, path_len):
+    """Moves the entries at positions first_pos[b] + path[b, j] to first_pos[b] + j, j < path_len[b].  path int32 [n_seqs, max_path]."""
+    import torch
+    _same_device(cache.page_table, first_pos, path, path_len)
+    _index(first_pos, cache.n_seqs, "first_pos")
+    _index(path_len, cache.n_seqs, "path_len")
+    _need(path.dtype == torch.int32 and path.dim() == 2 and path.shape[0] == cache.n_seqs and path.is_contiguous(), "path must be a contiguous int32 [n_seqs, max_path]")
+    with _on(cache.device):
+        _check(lib().sjd_op_cache_compact(_stream_ptr(), cache.ref(), first_pos.data_ptr(), path.data_ptr(), path_len.data_ptr(), path.shape[1]))
+
+
+def rope_table(rotary_dim, theta=10000.0, scaling="none", factor=1.0, trained_ctx=0.0, low_turns=1.0, high_turns=32.0, device="cuda"):
+    """Frequencies for op_rotary (sjd_rope_table) on the device, as the bits of an int64 tensor [rotary_dim / 2].  scaling: "none",
+    "linear", "base" or "parts"."""
+    import torch
+    _need(scaling in _SCALINGS, "scaling must be none, linear, base or parts")
+    table = np.zeros(max(rotary_dim // 2, 1), dtype=np.uint64)
+    _check(lib().sjd_rope_table(rotary_dim, theta, _SCALINGS[scaling], factor, trained_ctx, low_turns, high_turns, table.ctypes.data))
+    return torch.from_numpy(table.view(np.int64)).to(device)
+
+
+def op_rotary(q, k, positions, table, interleaved=False, magnitude=1.0, out=None):
+    """Turns q [rows, heads, hd] and k [rows, kv_heads, hd] (or None) by their rows' positions (int32) -> (q', k').  out: tensors to write to, which may
+    be q and k themselves."""
+    import torch
+    device = _same_device(q, k, positions, table, *(out or ()))
+    rows, hd = q.shape[0], q.shape[-1]
+    xs = [q] if k is None else [q, k]
+    if out is None:
+        out = [torch.empty(x.shape, dtype=x.dtype, device=device) for x in xs]
+    ys = [y for y in out if y is not None]
+    _need(len(ys) == len(xs) and all(y.shape == x.shape for x, y in zip(xs, ys)), "out must have the shapes of q and k")
+    _need(all(t.dtype == q.dtype and t.shape[0] == rows for t in xs + ys), "q, k and out must have one dtype and number of rows")
+    _index(positions, rows, "positions")
+    _index(table, None, "table", "int64")
+    args = [a for x, y in zip(xs, ys) for a in (x.data_ptr(), _heads_of(x, x.shape[1], hd, "q and k"), y.data_ptr(), _heads_of(y, y.shape[1], hd, "out"),
+                                                x.shape[1])]
+    args += [None, 0, None, 0, 0] if k is None else []
+    with _on(device):
+        _check(lib().sjd_op_rotary(_stream_ptr(), _dtype_code(q), 1 if interleaved else 0, table.data_ptr(), 2 * table.numel(), magnitude,
+                                   positions.data_ptr(), rows, hd, *args))
+    return ys[0], ys[1] if k is not None else None
+
+
+def tree_masks(parents, mask_words=None):
+    """Host: parents (ints; negative: a root) -> (mask uint32 [n, mask_words], depth int32 [n]): bit j of row i is node i or an ancestor of it."""
+    parents = np.ascontiguousarray(parents, dtype=np.int32)
+    n = len(parents)
+    words = -(-n // 32) if mask_words is None else mask_words
+    mask, depth = np.zeros((n, words), dtype=np.uint32), np.zeros(n, dtype=np.int32)
+    _check(lib().sjd_tree_masks(parents.ctypes.data, n, words, mask.ctypes.data, depth.ctypes.data))
+    return mask, depth
+
+
+def _workspace(given, need, device):
+    import torch
+    if given is None:
+        return torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    _need(given.is_contiguous(), "the workspace must be contiguous")
+    return given
+
+
+def _bytes(t):
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def op_tree_attention(q, cache, row_start, ctx_len, mask=None, max_rows=None, max_ctx=None, scale=0.0, out=None, workspace=None):
+    """Attention of q [rows, heads, head_dim] over the cache: row row_start[b] + i (position ctx_len[b] + i) sees positions [0, ctx_len[b])
+    and the nodes whose bits are set in its row of mask, int32 or uint32 [rows, words]; without a mask nodes 0 .. i.  max_rows: no tree has more
+    (default: all rows); max_ctx: what ctx_len is expected to reach (default: what the page table holds).  -> out like q; rows of no sequence are not written."""
+    import torch
+    device = _same_device(cache.page_table, q, row_start, ctx_len, mask, out, workspace)
+    _need(q.dim() == 3, "q must be [rows, heads, head_dim]")
+    rows, heads = q.shape[0], q.shape[1]
+    stride = _heads_of(q, heads, cache.head_dim, "q")
+    _index(row_start, cache.n_seqs + 1, "row_start")
+    _index(ctx_len, cache.n_seqs, "ctx_len")
+    if mask is not None:
+        _need(mask.dtype in (torch.int32, torch.uint32) and mask.dim() == 2 and mask.shape[0] == rows and mask.is_contiguous(),
+              "mask must be a contiguous int32 or uint32 [rows, words]")
+    if out is None:
+        out = torch.empty((rows, heads, cache.head_dim), dtype=q.dtype, device=device)
+    _need(out.dtype == q.dtype and out.shape == q.shape, "out must be like q")
+    max_rows = max(rows, 1) if max_rows is None else max_rows
+    max_ctx = cache.desc.pages_per_seq * cache.desc.page_tokens if max_ctx is None else max_ctx
+    with _on(device):
+        need = C.c_uint64(0)
+        _check(lib().sjd_op_tree_attention_workspace(cache.ref(), heads, max_rows, max_ctx, C.byref(need)))
+        workspace = _workspace(workspace, need.value, device)
+        _check(lib().sjd_op_tree_attention(_stream_ptr(), cache.ref(), _dtype_code(q), q.data_ptr(), stride, out.data_ptr(),
+                                           _heads_of(out, heads, cache.head_dim, "out"), row_start.data_ptr(), ctx_len.data_ptr(),
+                                           None if mask is None else mask.data_ptr(), 0 if mask is None else mask.shape[1], rows, heads, scale, max_rows,
+                                           max_ctx, None if workspace is None else workspace.data_ptr(), _bytes(workspace)))
+    return out
+
+
+def op_tree_verify(tokens, parents, row_start, p, q, accept_words, draw_words, max_rows=None, max_path=None, workspace=None):
+    """Verifies trees of drafted tokens: tokens, parents int32 [rows]; p (and q, or None) float32 [rows, vocab], rows may be strided; accept_words
+    [rows], the bits of 32-bit words (int32 or uint32); draw_words [n_seqs], of 64-bit words.  -> (path int32 [n_seqs, max_path], path_len int32
+    [n_seqs], next_token int32 [n_seqs])."""
+    import torch
+    device = _same_device(p, tokens, parents, row_start, q, accept_words, draw_words, workspace)
+    rows, seqs = tokens.shape[0], row_start.shape[0] - 1
+    _index(tokens, rows, "tokens")
+    _index(parents, rows, "parents")
+    _index(row_start, seqs + 1, "row_start")
+    for t in (p,) if q is None else (p, q):
+        _need(t.dtype == torch.float32 and t.dim() == 2 and t.shape[0] == rows and t.shape[1] == p.shape[1] and (t.shape[1] == 1 or t.stride(1) == 1),
+              "p and q must be float32 [rows, vocab] with contiguous rows")
+    _index(accept_words, rows, "accept_words", "uint32" if accept_words.dtype == torch.uint32 else "int32")
+    _index(draw_words, seqs, "draw_words", "uint64" if draw_words.dtype == torch.uint64 else "int64")
+    max_rows = min(max(rows, 1), 1024) if max_rows is None else max_rows
+    max_path = max_rows if max_path is None else max_path
+    _need(max_path >= 1, "max_path must be positive")
+    strides = [0 if t is None else t.stride(0) if rows > 1 else t.shape[1] for t in (p, q)]
+    path = torch.empty((seqs, max_path), dtype=torch.int32, device=device)
+    path_len, token = (torch.empty(seqs, dtype=torch.int32, device=device) for _ in range(2))
+    with _on(device):
+        need = C.c_uint64(0)
+        _check(lib().sjd_op_tree_verify_workspace(rows, seqs, p.shape[1], C.byref(need)))
+        workspace = _workspace(workspace, need.value, device)
+        _check(lib().sjd_op_tree_verify(_stream_ptr(), tokens.data_ptr(), parents.data_ptr(), row_start.data_ptr(), p.data_ptr(), strides[0],
+                                        None if q is None else q.data_ptr(), strides[1], accept_words.data_ptr(), draw_words.data_ptr(), path.data_ptr(),
+                                        path_len.data_ptr(), token.data_ptr(), rows, seqs, p.shape[1], max_rows, max_path, workspace.data_ptr(),
+                                        _bytes(workspace)))
+    return path, path_len, token

@@ -13,8 +13,9 @@ COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
           # leading scalar arguments of a kernel arrive in registers instead of through a load
           "-mllvm", "-amdgpu-kernarg-preload-count=14"]
-# (source, extra flags): the decision stage is specified bit for bit and must not contract a*b+c
-UNITS = [("decide.hip", ["-ffp-contract=off"]), ("sjd_api.hip", [])]
+# (source, extra flags): the decision stage and the verification of trees are specified bit for bit and must not contract a*b+c
+UNITS = [("decide.hip", ["-ffp-contract=off"]), ("sjd_api.hip", []), ("tree_ops.hip", []),
+         ("tree_verify.hip", ["-ffp-contract=off"])]
 
 
 def build(verbose: bool = False) -> str:

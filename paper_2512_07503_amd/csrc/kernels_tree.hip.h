@@ -1,0 +1,492 @@
+// Attention of the rows of trees over a paged cache (layout: cache_layout.h).
+//
+// Row r of the launch is (node i, query head h) of a sequence; the rows of one kv head, ordered (i, h), are cut into tiles of 32, so
+// that the query heads of a group share every key and value that is fetched.  Per block of 32 tokens a wavefront computes
+//   S^T (tokens x rows) = K Q^T,   online softmax per row = per accumulator column,   O^T (dimensions x rows) += V^T P^T,
+// and P^T needs no data movement: the accumulator registers of S^T are the B operand of the second product.
+#pragma once
+#include "common.hip.h"
+#include "kernels_cache.hip.h"
+
+struct TreeArgs {
+    CacheView c;
+    const void *q;             // [n_rows][H][hd], rows q_stride apart
+    void *out;                 // [n_rows][H][hd], rows out_stride apart
+    long q_stride, out_stride;
+    const int32_t *row_start, *ctx_len;
+    const uint32_t *mask;      // [n_rows][mask_words], NULL: a window
+    int mask_words, n_rows, max_rows, H, G, tiles, n_splits;
+    float scale_log2e;
+    float *part_o;             // [group][tile][32][hd]   unnormalised, group = (sequence, kv head, split)
+    float *part_ml;            // [group][tile][2][32]    running maximum (base 2), running sum
+    bool q_wide, out_wide;     // rows 16-byte (out: 4 elements) aligned
+};
+
+// What a workgroup of the launch works on
+struct TreeWork { int b, kvh, tile, split; };
+// tiles of one (sequence, kv head, split) read the same keys and values: they run on one XCD (workgroups go round the 8 XCDs), near each other in time
+SJD_D TreeWork tree_work(const TreeArgs &a, unsigned id) {
+    const unsigned xcd = id & 7, rest = id >> 3;
+    const unsigned tile = rest % a.tiles, group = (rest / a.tiles) * 8 + xcd;
+    TreeWork w;
+    w.tile = tile;
+    w.split = group % a.n_splits;
+    w.kvh = (group / a.n_splits) % a.c.n_kv;
+    w.b = group / a.n_splits / a.c.n_kv;
+    return w;
+}
+inline unsigned tree_grid(const TreeArgs &a) { return (unsigned)(ceil_div_sz((size_t)a.c.n_seqs * a.c.n_kv * a.n_splits, 8) * 8 * a.tiles); }
+SJD_D size_t tree_slot(const TreeArgs &a, int b, int kvh, int split, int tile) {
+    return ((((size_t)b * a.c.n_kv + kvh) * a.n_splits + split) * a.tiles + tile);
+}
+
+// Rows and length of sequence b
+struct TreeSeq { int r0, n, ctx, n_tot; };
+SJD_D TreeSeq tree_seq(const TreeArgs &a, int b) {
+    TreeSeq s;
+    s.r0 = rows_first(a.row_start, b, a.n_rows);
+    s.n = min(rows_count(a.row_start, b, a.n_rows), a.max_rows);
+    const int cap = a.c.pages_per_seq * a.c.page_tokens;
+    s.ctx = min(max(a.ctx_len[b], 0), cap);
+    s.n_tot = min(s.ctx + s.n, cap);
+    return s;
+}
+// ------------------------------------------------------------------------------------------------ one block of 32 tokens
+// by value: __builtin_bit_cast of an element of a vector that is named in place takes the vector's first element, whichever is meant
+SJD_D float as_float(uint32_t u) { return __builtin_bit_cast(float, u); }
+
+// Keys and values of a block as they come from memory; q operand; by kind
+template <int KIND, int HD> struct TreeFrag {
+    static constexpr int NK = HD * (KIND == SJD_F32 ? 4 : KIND == SJD_BF16 ? 2 : 1) / 32;   // 16-byte pieces of a lane: keys, and values
+    static constexpr int NQ = HD * (KIND == SJD_F32 ? 4 : 2) / 32;
+    u32x4 k[NK], v[NK];
+    uint32_t k_scale;          // FP8: byte of token lane % 32
+    uint32_t v_scale[4];       // FP8: bytes of tokens 8 m + 4 g + (0 .. 3)
+
+    SJD_D void load_k(const TreeArgs &a, const unsigned char *block, int slot, int lane) {
+        const u32x4 *p = reinterpret_cast<const u32x4 *>(block + (size_t)slot * HD * (KIND == SJD_F32 ? 4 : KIND == SJD_BF16 ? 2 : 1)) + lane;
+#pragma unroll
+        for (int i = 0; i < NK; ++i) k[i] = p[i * 64];
+        if (KIND == SJD_FP8) k_scale = block[2 * (size_t)a.c.page_tokens * HD + slot + (lane & 31)];
+    }
+    SJD_D void load_v(const TreeArgs &a, const unsigned char *block, int slot, int lane) {
+        const size_t size = KIND == SJD_F32 ? 4 : KIND == SJD_BF16 ? 2 : 1;
+        const u32x4 *p = reinterpret_cast<const u32x4 *>(block + ((size_t)a.c.page_tokens + slot) * HD * size) + lane;
+#pragma unroll
+        for (int i = 0; i < NK; ++i) v[i] = p[i * 64];
+        if (KIND == SJD_FP8) {
+            const uint32_t *s = reinterpret_cast<const uint32_t *>(block + 2 * (size_t)a.c.page_tokens * HD + a.c.page_tokens + slot + 4 * (lane >> 5));
+#pragma unroll
+            for (int m = 0; m < 4; ++m) v_scale[m] = s[2 * m];
+        }
+    }
+};
+
+// two dwords of fp8 codes -> 8 bf16, times a power of two
+SJD_D bf16x8 fp8_to_bf16(uint32_t lo, uint32_t hi, float scale) {
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    const b2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)lo, scale, true);
+    const b2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, scale, true);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+// 2^(byte - 127); a byte that no write leaves (255) counts as 254, so that a token nobody sees stays finite
+SJD_D float scale_of(uint32_t byte) { return __builtin_bit_cast(float, min(byte, 254u) << 23); }
+
+// q(n): piece n of the query operand
+template <int KIND, int HD, typename Q>
+SJD_D f32x16 tree_scores(const TreeFrag<KIND, HD> &f, Q q) {
+    f32x16 s;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) s[v] = 0.0f;
+    if constexpr (KIND == SJD_F32) {
+#pragma unroll
+        for (int i = 0; i < HD / 8; ++i) {
+            const u32x4 qi = q(i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                s = __builtin_amdgcn_mfma_f32_32x32x2f32(as_float(f.k[i][e]), as_float(qi[e]), s, 0, 0, 0);
+        }
+    } else if constexpr (KIND == SJD_BF16) {
+#pragma unroll
+        for (int i = 0; i < HD / 16; ++i)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f.k[i]), __builtin_bit_cast(bf16x8, q(i)), s, 0, 0, 0);
+    } else {
+        const float ks = scale_of(f.k_scale);
+#pragma unroll
+        for (int i = 0; i < HD / 32; ++i) {
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp8_to_bf16(f.k[i][0], f.k[i][1], ks), __builtin_bit_cast(bf16x8, q(2 * i)), s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp8_to_bf16(f.k[i][2], f.k[i][3], ks), __builtin_bit_cast(bf16x8, q(2 * i + 1)), s, 0, 0, 0);
+        }
+    }
+    return s;
+}
+
+// A operand of the second product for dimension block db, half i of the tokens (not F32)
+template <int KIND, int HD> SJD_D bf16x8 tree_values(const TreeFrag<KIND, HD> &f, int db, int i) {
+    if constexpr (KIND == SJD_BF16) return __builtin_bit_cast(bf16x8, f.v[i * (HD / 32) + db]);
+    else return fp8_to_bf16(f.v[db][2 * i], f.v[db][2 * i + 1], 1.0f);
+}
+
+enum { VALUE_FINITE = 0, VALUE_POS_INF = 1, VALUE_NEG_INF = 2, VALUE_NAN = 3 };
+SJD_D int value_class(float x) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    if ((u & 0x7F800000u) != 0x7F800000u) return VALUE_FINITE;
+    return u & 0x007FFFFFu ? VALUE_NAN : u >> 31 ? VALUE_NEG_INF : VALUE_POS_INF;
+}
+// is any of a lane's values infinite or NaN
+template <int KIND, int HD> SJD_D bool tree_values_wild(const TreeFrag<KIND, HD> &f) {
+    bool wild = false;
+#pragma unroll
+    for (int i = 0; i < TreeFrag<KIND, HD>::NK; ++i)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+            const uint32_t u = f.v[i][d];
+            if constexpr (KIND == SJD_F32) wild |= (u & 0x7F800000u) == 0x7F800000u;
+            else if constexpr (KIND == SJD_BF16) wild |= (u & 0x7F80u) == 0x7F80u || (u & 0x7F800000u) == 0x7F800000u;
+            else {   // a byte is 0x7F after its sign is cleared: adding 1 carries into its sign
+                wild |= (((u & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0u;
+            }
+        }
+    return wild;
+}
+
+// infinite and NaN values become 0
+template <int KIND, int HD> SJD_D void tree_values_tame(TreeFrag<KIND, HD> &f) {
+#pragma unroll
+    for (int i = 0; i < TreeFrag<KIND, HD>::NK; ++i)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+            uint32_t u = f.v[i][d];
+            if constexpr (KIND == SJD_F32) u = (u & 0x7F800000u) == 0x7F800000u ? 0u : u;
+            else if constexpr (KIND == SJD_BF16) u &= ((u & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu) | ((u & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u);
+            else u &= ~(((((u & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xFFu);
+            f.v[i][d] = u;
+        }
+}
+
+// o + V P for dimension block db
+template <int KIND, int HD>
+SJD_D f32x16 tree_product(const TreeFrag<KIND, HD> &f, int db, const float (&p32)[16], const u32x4 (&pb)[2], f32x16 o) {
+    if constexpr (KIND == SJD_F32) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+            o = __builtin_amdgcn_mfma_f32_32x32x2f32(as_float(f.v[db * 4 + (v >> 2)][v & 3]), p32[v], o, 0, 0, 0);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tree_values<KIND, HD>(f, db, i), __builtin_bit_cast(bf16x8, pb[i]), o, 0, 0, 0);
+    }
+    return o;
+}
+
+// The running state of a wavefront's 32 rows: O^T, maxima (base 2), this lane's half of the sums
+template <int HD> struct TreeState {
+    f32x16 o[HD / 32];
+    float m, l;
+    SJD_D void clear() {
+#pragma unroll
+        for (int db = 0; db < HD / 32; ++db)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) o[db][v] = 0.0f;
+        m = -INFINITY;
+        l = 0.0f;
+    }
+};
+
+// Softmax of a block's scores into p (and, but for F32, its bf16 operand pb), and the rescaling of the state.  `vis`: bit k = this lane's
+// row sees token k of the block.
+template <int KIND, int HD>
+SJD_D void tree_softmax(const TreeFrag<KIND, HD> &f, f32x16 s, bool masked, uint32_t vis, float scale_log2e, TreeState<HD> &st, int lane,
+                        float (&p)[16], u32x4 (&pb)[2]) {
+    if (masked) {
+        const uint32_t mine = vis >> (4 * (lane >> 5));     // bit 8 (v / 4) + v % 4 belongs to register v
+#pragma unroll
+        for (int v = 0; v < 16; ++v) s[v] = mine >> (8 * (v >> 2) + (v & 3)) & 1u ? s[v] : -INFINITY;
+    }
+    float mx = s[0];
+#pragma unroll
+    for (int v = 1; v < 16; ++v) mx = fmaxf(mx, s[v]);
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * scale_log2e;
+    const float m_new = fmaxf(st.m, mx);
+    const float m_use = m_new == -INFINITY ? 0.0f : m_new;  // a row that has seen nothing so far: not (-inf) - (-inf)
+    const float alpha = __builtin_amdgcn_exp2f(st.m - m_use);
+    float sum = 0.0f;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+        p[v] = __builtin_amdgcn_exp2f(fmaf(s[v], scale_log2e, -m_use));
+        sum += p[v];
+    }
+    st.l = st.l * alpha + sum;
+    st.m = m_new;
+#pragma unroll
+    for (int db = 0; db < HD / 32; ++db)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) st.o[db][v] *= alpha;
+    if constexpr (KIND != SJD_F32) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                const int v = 8 * i + 2 * d;
+                float a = p[v], b = p[v + 1];
+                if constexpr (KIND == SJD_FP8) {           // the values' scales, exact: the product takes plain codes
+                    a *= scale_of(f.v_scale[v >> 2] >> (8 * (v & 3)) & 0xFFu);
+                    b *= scale_of(f.v_scale[v >> 2] >> (8 * ((v + 1) & 3)) & 0xFFu);
+                }
+                pb[i][d] = pack_bf16(a, b);
+            }
+    }
+}
+
+// Values some of which are infinite or NaN, of tokens that not every row sees: in O += V P their 0 * inf would reach the rows that do
+// not.  Which rows see an element of which class is noted in LDS, bit r of wild[class - 1][dimension] for row r, and added at the end; the
+// values become 0.  (Rare, so it is kept off the registers of the loop: with a product of ones per class in its place they went from 209 to
+// 256 and 43 in scratch memory for bf16 heads of 128.)
+template <int KIND, int HD> SJD_D float tree_value(const TreeFrag<KIND, HD> &f, int db, int m, int e) {   // token 8 m + 4 g + e, dimension 32 db + lane % 32
+    if constexpr (KIND == SJD_F32) return as_float(f.v[db * 4 + m][e]);
+    else if constexpr (KIND == SJD_BF16) return bf16_to_float((bf16_t)(f.v[(m >> 1) * (HD / 32) + db][(m & 1) * 2 + (e >> 1)] >> (16 * (e & 1))));
+    else return (f.v[db][m] >> (8 * e) & 0x7Fu) == 0x7Fu ? __builtin_nanf("") : 0.0f;
+}
+template <int KIND, int HD>
+SJD_D void tree_take_wild(TreeFrag<KIND, HD> &f, uint32_t vis, uint32_t (&wild)[3][HD], int lane) {
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t lo = (uint32_t)__ballot(vis >> (8 * m + e) & 1u), hi = (uint32_t)__ballot(vis >> (8 * m + 4 + e) & 1u);
+            const uint32_t rows = lane < 32 ? lo : hi;
+#pragma unroll
+            for (int db = 0; db < HD / 32; ++db) {
+                const int cls = value_class(tree_value<KIND, HD>(f, db, m, e));
+                if (cls != VALUE_FINITE && rows) atomicOr(&wild[cls - 1][db * 32 + (lane & 31)], rows);
+            }
+        }
+    tree_values_tame<KIND, HD>(f);
+}
+// what the noted elements make of dimension j of a row
+template <int HD> SJD_D float tree_add_wild(float x, const uint32_t (&wild)[3][HD], int row, int j) {
+    if (wild[VALUE_POS_INF - 1][j] >> row & 1u) x += INFINITY;
+    if (wild[VALUE_NEG_INF - 1][j] >> row & 1u) x -= INFINITY;
+    if (wild[VALUE_NAN - 1][j] >> row & 1u) x += __builtin_nanf("");
+    return x;
+}
+
+// The query operand of tile `tile`: lane's row = 32 tile + lane % 32.  Rows behind the last are zeros.
+template <int KIND, int HD>
+SJD_D void tree_load_q(const TreeArgs &a, const TreeSeq &s, int kvh, int tile, int lane, u32x4 (&q)[TreeFrag<KIND, HD>::NQ]) {
+    const int rho = 32 * tile + (lane & 31), i = rho / a.G, g = rho - i * a.G;
+    const bool live = i < s.n;
+    constexpr int PIECE = KIND == SJD_F32 ? 4 : 8, SIZE = KIND == SJD_F32 ? 4 : 2;   // elements of 16 bytes
+    const char *src = (const char *)a.q + ((size_t)(s.r0 + (live ? i : 0)) * a.q_stride + (size_t)(kvh * a.G + (live ? g : 0)) * HD) * SIZE;
+#pragma unroll
+    for (int n = 0; n < TreeFrag<KIND, HD>::NQ; ++n) {
+        const char *p = src + (size_t)(n * 2 + (lane >> 5)) * PIECE * SIZE;
+        u32x4 x = {0u, 0u, 0u, 0u};
+        if (live) {
+            if (a.q_wide) x = *reinterpret_cast<const u32x4 *>(p);
+            else if (KIND == SJD_F32) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = reinterpret_cast<const uint32_t *>(p)[e];
+            } else {
+                const uint16_t *h = reinterpret_cast<const uint16_t *>(p);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = h[2 * e] | (uint32_t)h[2 * e + 1] << 16;
+            }
+        }
+        q[n] = x;
+    }
+}
+
+// four dimensions of one output row
+template <int KIND> SJD_D void tree_store(const TreeArgs &a, size_t row, int h, int hd, int j, f32x4 t) {
+    if constexpr (KIND == SJD_F32) {
+        float *p = (float *)a.out + row * a.out_stride + (size_t)h * hd + j;
+        if (a.out_wide) *reinterpret_cast<f32x4 *>(p) = t;
+        else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p[e] = t[e];
+        }
+    } else {
+        bf16_t *p = (bf16_t *)a.out + row * a.out_stride + (size_t)h * hd + j;
+        const uint2 w = {pack_bf16(t[0], t[1]), pack_bf16(t[2], t[3])};
+        if (a.out_wide) *reinterpret_cast<uint2 *>(p) = w;
+        else {
+            p[0] = (bf16_t)w.x; p[1] = (bf16_t)(w.x >> 16); p[2] = (bf16_t)w.y; p[3] = (bf16_t)(w.y >> 16);
+        }
+    }
+}
+
+// --------------------------------------------------------------------------------------------------- wavefronts over tokens
+// Workgroup = (sequence, kv head, tile of 32 rows, split of the context); its wavefronts take the split's blocks in turn and merge
+// through LDS.  For few rows: what bounds it is the stream of keys and values.
+constexpr int kTreeWaves = 4;
+
+// A lane's registers hold its queries, keys, values and output: from 40 (fp8 heads of 32) to 512 of 512 (fp32 heads of 256).  Wide heads
+// leave the queries in LDS, and fp32 heads of 256 ask for keys and values only when the other ones are done with.
+template <int KIND, int HD> constexpr bool kTreeQueriesInLds = KIND == SJD_F32 ? HD >= 192 : HD == 256;
+template <int KIND, int HD> constexpr bool kTreeLateLoads = KIND == SJD_F32 && HD == 256;
+constexpr int tree_waves_per_simd(int kind, int hd) {
+    return hd * (kind == SJD_F32 ? 4 : kind == SJD_BF16 ? 2 : 1) / 4 + hd * (kind == SJD_F32 ? 2 : 1) / 4 + hd / 2 <= 191 ? 2 : 1;
+}
+
+template <int KIND, int HD>
+__global__ __launch_bounds__(kTreeWaves * 64, tree_waves_per_simd(KIND, HD)) void tree_attention_kernel(TreeArgs a) {
+    constexpr int DB = HD / 32, NW = kTreeWaves;
+    const TreeWork w = tree_work(a, blockIdx.x);
+    if (w.b >= a.c.n_seqs) return;
+    const TreeSeq s = tree_seq(a, w.b);
+    if (32 * w.tile >= s.n * a.G) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const TreeBlocks range = tree_blocks(a.mask, s.ctx, s.n_tot, min((32 * w.tile + 31) / a.G, s.n - 1), w.split, a.n_splits);
+    const int rho = 32 * w.tile + (lane & 31), node = rho / a.G;
+    const bool live = node < s.n;
+    const uint32_t *mask = a.mask && live ? a.mask + (size_t)(s.r0 + node) * a.mask_words : nullptr;
+    TreeState<HD> st;
+    st.clear();
+    TreeFrag<KIND, HD> f;
+    u32x4 q[TreeFrag<KIND, HD>::NQ];
+    const int32_t *table = a.c.page_table + (size_t)w.b * a.c.pages_per_seq;
+    auto page_of = [&](int blk) {
+        const int page = table[32 * blk / a.c.page_tokens];      // a block lies below n_tot, hence within the table
+        return (unsigned)page < (unsigned)a.c.n_pages ? page : -1;
+    };
+    int blk = range.first + wave, page = blk < range.last ? page_of(blk) : -1;
+    if (page >= 0) {
+        f.load_k(a, cache_block(a.c, page, w.kvh), 32 * blk % a.c.page_tokens, lane);
+        if (!kTreeLateLoads<KIND, HD>) f.load_v(a, cache_block(a.c, page, w.kvh), 32 * blk % a.c.page_tokens, lane);
+    }
+    tree_load_q<KIND, HD>(a, s, w.kvh, w.tile, lane, q);
+    __shared__ uint32_t wild[3][HD], any_wild;
+    for (int i = threadIdx.x; i < 3 * HD; i += NW * 64) (&wild[0][0])[i] = 0u;
+    if (threadIdx.x == 0) any_wild = 0u;
+    constexpr int NL = kTreeQueriesInLds<KIND, HD> ? TreeFrag<KIND, HD>::NQ : 1;
+    __shared__ u32x4 q_lds[NL][64];
+    if constexpr (kTreeQueriesInLds<KIND, HD>) {
+        if (wave == 0)
+#pragma unroll
+            for (int n = 0; n < NL; ++n) q_lds[n][lane] = q[n];
+    }
+    __syncthreads();
+    auto query = [&](int n) {
+        if constexpr (kTreeQueriesInLds<KIND, HD>) return q_lds[n][lane];
+        else return q[n];
+    };
+    while (blk < range.last) {
+        const int next = blk + NW;
+        const int next_page = next < range.last ? page_of(next) : -1;
+        const unsigned char *next_block = next_page >= 0 ? cache_block(a.c, next_page, w.kvh) : nullptr;
+        const int next_slot = 32 * next % a.c.page_tokens, t0 = 32 * blk;
+        if (page >= 0) {
+            const bool masked = t0 + 32 > s.ctx;
+            uint32_t vis = 0xFFFFFFFFu;
+            if (masked) vis = live ? tree_visible(mask, a.mask_words, s.ctx, s.n_tot, node, t0) : 0u;
+            const f32x16 sc = tree_scores<KIND, HD>(f, query);
+            if (kTreeLateLoads<KIND, HD>) {
+                __builtin_amdgcn_sched_barrier(0);
+                f.load_v(a, cache_block(a.c, page, w.kvh), t0 % a.c.page_tokens, lane);
+            } else if (next_page >= 0) f.load_k(a, next_block, next_slot, lane);
+            float p[16];
+            u32x4 pb[2];
+            tree_softmax<KIND, HD>(f, sc, masked, vis, a.scale_log2e, st, lane, p, pb);
+            if (masked && __ballot(tree_values_wild<KIND, HD>(f))) {
+                if (lane == 0) any_wild = 1;
+                tree_take_wild<KIND, HD>(f, vis, wild, lane);
+            }
+#pragma unroll
+            for (int db = 0; db < DB; ++db) st.o[db] = tree_product<KIND, HD>(f, db, p, pb, st.o[db]);
+            if (kTreeLateLoads<KIND, HD>) {
+                __builtin_amdgcn_sched_barrier(0);
+                if (next_page >= 0) f.load_k(a, next_block, next_slot, lane);
+            } else if (next_page >= 0) f.load_v(a, next_block, next_slot, lane);
+        } else if (next_page >= 0) {
+            f.load_k(a, next_block, next_slot, lane);
+            if (!kTreeLateLoads<KIND, HD>) f.load_v(a, next_block, next_slot, lane);
+        }
+        blk = next;
+        page = next_page;
+    }
+    st.l += __shfl_xor(st.l, 32, 64);
+
+    // merge: out = sum_w 2^(m_w - m) O_w / sum_w 2^(m_w - m) l_w, 32 dimensions at a time
+    __shared__ float ml[NW][2][32];
+    __shared__ f32x4 red[NW][4][64];
+    const int row = lane & 31;
+    if (lane < 32) {
+        ml[wave][0][row] = st.m;
+        ml[wave][1][row] = st.l;
+    }
+    __syncthreads();
+    float m_all = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) m_all = fmaxf(m_all, ml[i][0][row]);
+    const float m_use = m_all == -INFINITY ? 0.0f : m_all;
+    float denom = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) denom += __builtin_amdgcn_exp2f(ml[i][0][row] - m_use) * ml[i][1][row];
+    const float mine = __builtin_amdgcn_exp2f(st.m - m_use);
+    const bool split = a.n_splits > 1;
+    const size_t slot = tree_slot(a, w.b, w.kvh, w.split, w.tile);
+    // (denom is NaN, and so is the row, where a score is; it is 0 where the row saw nothing)
+    const float norm = split ? 1.0f : denom == 0.0f ? 0.0f : 1.0f / denom;
+    if (split && wave == 0 && lane < 32) {
+        a.part_ml[slot * 64 + row] = m_all;
+        a.part_ml[slot * 64 + 32 + row] = denom;
+    }
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+        if (db > 0) __syncthreads();
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            red[wave][u][lane] = f32x4{st.o[db][4 * u] * mine, st.o[db][4 * u + 1] * mine, st.o[db][4 * u + 2] * mine, st.o[db][4 * u + 3] * mine};
+        __syncthreads();
+        f32x4 t = red[0][wave][lane];      // NW == 4 quads: wavefront u adds quad u
+#pragma unroll
+        for (int i = 1; i < NW; ++i) t += red[i][wave][lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t[e] = norm == 0.0f ? 0.0f : t[e] * norm;
+        const int j = db * 32 + 8 * wave + 4 * (lane >> 5);
+        if (any_wild)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t[e] = tree_add_wild<HD>(t[e], wild, row, j + e);
+        if (live && split) *reinterpret_cast<f32x4 *>(a.part_o + (slot * 32 + row) * HD + j) = t;
+        if (live && !split) tree_store<KIND>(a, (size_t)s.r0 + node, w.kvh * a.G + rho - node * a.G, HD, j, t);
+    }
+}
+static_assert(kTreeWaves == 4, "a wavefront adds one quad of a lane's 16 accumulators");
+
+// Joins the splits of every row: out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  A thread owns four dimensions of a row.  Rows of
+// splits without a block have m = -inf and l = 0; their (unwritten or zero) O is not read.
+template <int KIND>
+__global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a) {
+    const int quads = a.c.hd >> 2, per = 32 * quads;
+    const unsigned wgs = (per + 255) / 256;
+    const unsigned pair = blockIdx.x / wgs;
+    const int u = (blockIdx.x % wgs) * 256 + threadIdx.x;
+    const int tile = pair % a.tiles, kvh = (pair / a.tiles) % a.c.n_kv, b = pair / a.tiles / a.c.n_kv;
+    if (u >= per) return;
+    const int row = u / quads, j = (u - row * quads) * 4;
+    const TreeSeq s = tree_seq(a, b);
+    const int rho = 32 * tile + row, node = rho / a.G;
+    if (node >= s.n) return;
+    const size_t slot0 = tree_slot(a, b, kvh, 0, tile), step = a.tiles;
+    float m = -INFINITY;
+#pragma unroll 4
+    for (int i = 0; i < a.n_splits; ++i) m = fmaxf(m, a.part_ml[(slot0 + i * step) * 64 + row]);
+    const float m_use = m == -INFINITY ? 0.0f : m;
+    float denom = 0.0f;
+    f32x4 t = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int i = 0; i < a.n_splits; ++i) {
+        const size_t slot = slot0 + i * step;
+        const float l = a.part_ml[slot * 64 + 32 + row];
+        const float w = __builtin_amdgcn_exp2f(a.part_ml[slot * 64 + row] - m_use);
+        const f32x4 o = *reinterpret_cast<const f32x4 *>(a.part_o + (slot * 32 + row) * a.c.hd + j);
+        denom += w * l;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t[e] += l == 0.0f ? 0.0f : finite_f(o[e]) ? w * o[e] : o[e];   // (w may be 0: not 0 * inf)
+    }
+    const float inv = denom == 0.0f ? 0.0f : 1.0f / denom;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) t[e] = denom == 0.0f ? 0.0f : t[e] * inv;
+    tree_store<KIND>(a, (size_t)s.r0 + node, kvh * a.G + rho - node * a.G, a.c.hd, j, t);
+}

@@ -22,6 +22,7 @@
 #include "kernels_few.hip.h"
 #include "kernels_tile.hip.h"
 #include "kernels_lds.hip.h"
+#include "tree_ops.h"
 
 void sjd_set_error(char *buf, const char *fmt, ...) {
     if (!buf) return;
@@ -1052,6 +1053,8 @@ void choose_attention(sjd_ctx *c, int max_kv) {
 }
 
 }  // namespace
+
+char *sjd_call_error() { return g_create_error; }
 
 // =================================================================================================
 extern "C" {

@@ -1,0 +1,436 @@
+// Verification of a tree of drafted tokens against the target's probabilities, from given random words.
+//
+// Every result is specified bit for bit, in double precision and integers, so that it does not depend on how the work is divided:
+//   rho_0(v) = p(v) (0 where p is negative or NaN),  S_0 = 1
+//   child k of a node, token x:  accepted where (r * q(x)) * S_k < rho_k(x),  r = (u32 + 1/2) 2^-32
+//   else  rho_{k+1}(v) = max(0, rho_k(v) - S_k * q(v)),  S_{k+1} = 2^-44 * sum_v w(rho_{k+1}(v)),  w(y) = trunc(min(y, 1) * 2^44)
+//   without q the proposal is certain: q(x) = 1, and rho_{k+1} = rho_k but for rho_{k+1}(x) = 0
+//   the next token: first v with prefix_w(v) > floor(u64 * Z / 2^64), w of the last rho of the last accepted node, Z = sum_v w; of p if Z = 0
+// With rho normalised by S_k this is the acceptance of Eq. 2 of the paper, min(1, rho / q), and the residual of Eq. 3, once per sibling:
+// what a rejected proposal could have been is taken off, and the next sibling is tested against the rest.
+//
+// What a node decides follows from its own rows alone, so all nodes are decided at once, and the path is walked afterwards. A first child
+// takes two values; a sum over the vocabulary is needed only for a second child whose first sibling was rejected, at a node that is
+// not ruled out by the first children above it.  Bound by latency: two rows a sequence are all that has to be read.
+//
+// This translation unit must be compiled with -ffp-contract=off.
+#include "cache_layout.h"
+#include "common.hip.h"
+#include "tree_ops.h"
+
+#pragma clang fp contract(off)
+
+namespace {
+
+constexpr int kMaxNodes = 1024, kMaxVocab = 1 << 19;
+constexpr int kSlice = 2048;          // ids of a row that a workgroup sums for the last draw
+constexpr int kNodeThreads = 1024;    // of a node's workgroup; <= 512 ids a thread, whose sums are exact in a double
+
+struct VerifyArgs {
+    const int32_t *tokens, *parents, *row_start;
+    const float *p, *q;
+    long p_stride, q_stride;
+    const uint32_t *accept_words;
+    const uint64_t *draw_words;
+    int32_t *path, *path_len, *next_token;
+    int n_rows, n_seqs, max_rows, max_path, V, n_slices;
+    bool wide;                 // rows 16-byte aligned
+    // workspace
+    int32_t *choice;           // [n_rows]  accepted child of a node, -1: none
+    double *mass;              // [n_rows]  S after the rejection of that node
+    uint64_t *part;            // [n_seqs][n_slices][2]  sums of a slice: of the last rho, of p
+    int32_t *stop;             // [n_seqs][2]  row of the last accepted node (-1: empty tree), number of its rejected children
+    double *stop_mass;         // [n_rows]  S_0, S_1, ... of these, at the sequence's rows
+    int32_t *stop_token;       // [n_rows]  their tokens
+};
+
+SJD_D void tree_rows(const VerifyArgs &a, int b, int &r0, int &n) {
+    r0 = rows_first(a.row_start, b, a.n_rows);
+    n = min(rows_count(a.row_start, b, a.n_rows), a.max_rows);
+}
+SJD_D double positive(double x) { return x > 0.0 ? x : 0.0; }                  // NaN -> 0
+SJD_D double weight(double y) { return __builtin_trunc((y < 1.0 ? y : 1.0) * 0x1p44); }
+// rho after `m` rejections
+SJD_D double residual(double p, double q, const double *mass, int m) {
+    double r = positive(p);
+    for (int k = 0; k < m; ++k) r = positive(r - mass[k] * q);
+    return r;
+}
+SJD_D bool accepts(uint32_t word, double q, double mass, double rho) {
+    const double r = ((double)word + 0.5) * 0x1p-32;
+    return (r * q) * mass < rho;
+}
+
+SJD_D uint64_t shfl_xor_u64(uint64_t v, int d) {
+    const uint32_t lo = __shfl_xor((uint32_t)v, d, 64), hi = __shfl_xor((uint32_t)(v >> 32), d, 64);
+    return (uint64_t)hi << 32 | lo;
+}
+template <int NW> SJD_D uint64_t block_sum(uint64_t v, uint64_t *scratch /* NW */) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) v += shfl_xor_u64(v, d);
+    __syncthreads();
+    if (lane == 0) scratch[wave] = v;
+    __syncthreads();
+    uint64_t t = 0;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) t += scratch[i];
+    return t;
+}
+
+SJD_D bool known(const VerifyArgs &a, int x) { return (unsigned)x < (unsigned)a.V; }
+
+// Is the first child of the node in row `row` accepted
+SJD_D bool first_accepted(const VerifyArgs &a, int r0, int node, int child) {
+    const int x = a.tokens[r0 + child];
+    if (!known(a, x)) return false;
+    const size_t row = (size_t)(r0 + node);
+    const double q = a.q ? (double)a.q[row * a.q_stride + x] : 1.0;
+    return accepts(a.accept_words[r0 + child], q, 1.0, positive((double)a.p[row * a.p_stride + x]));
+}
+
+// f(id, p, q) for every id of a row, a thread's ids in ascending order; 4 ids at a time
+template <int THREADS, typename F> SJD_D void for_row(const VerifyArgs &a, const float *p, const float *q, int lo, int hi, F f) {
+    if (a.wide) {
+        constexpr int U = 4;
+        for (int v0 = lo + 4 * threadIdx.x; v0 < hi; v0 += 4 * THREADS * U) {
+            float4 pv[U], qv[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int v = v0 + 4 * THREADS * u;
+                if (v + 4 <= hi) {
+                    pv[u] = *reinterpret_cast<const float4 *>(p + v);
+                    qv[u] = q ? *reinterpret_cast<const float4 *>(q + v) : float4{0.0f, 0.0f, 0.0f, 0.0f};
+                } else {
+                    float x[4], y[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        x[e] = v + e < hi ? p[v + e] : 0.0f;
+                        y[e] = v + e < hi && q ? q[v + e] : 0.0f;
+                    }
+                    pv[u] = float4{x[0], x[1], x[2], x[3]};
+                    qv[u] = float4{y[0], y[1], y[2], y[3]};
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int v = v0 + 4 * THREADS * u;
+                f(v, pv[u].x, qv[u].x); f(v + 1, pv[u].y, qv[u].y); f(v + 2, pv[u].z, qv[u].z); f(v + 3, pv[u].w, qv[u].w);
+            }
+        }
+    } else {
+        for (int v = lo + threadIdx.x; v < hi; v += THREADS) f(v, p[v], q ? q[v] : 0.0f);
+    }
+}
+
+// Workgroup = node of a tree: which of its children is accepted
+__global__ __launch_bounds__(kNodeThreads) void verify_nodes_kernel(VerifyArgs a) {
+    const int b = blockIdx.y, node = blockIdx.x, tid = threadIdx.x;
+    int r0, n;
+    tree_rows(a, b, r0, n);
+    if (node >= n) return;
+    __shared__ int parent[kMaxNodes], first[kMaxNodes], child[kMaxNodes], wave_count[kNodeThreads / 64], flag;
+    __shared__ double mass[kMaxNodes];
+    __shared__ uint64_t scratch[kNodeThreads / 64];
+    const int mine = tid < n ? a.parents[r0 + tid] : -1;
+    const bool is_child = tid > node && tid < n && mine == node;
+    // children in ascending order
+    const unsigned long long here = __ballot(is_child);
+    const int lane = tid & 63, wave = tid >> 6;
+    if (lane == 0) wave_count[wave] = __popcll(here);
+    __syncthreads();
+    int before = 0, m = 0;
+    for (int w = 0; w < kNodeThreads / 64; ++w) {
+        if (w < wave) before += wave_count[w];
+        m += wave_count[w];
+    }
+    if (is_child) child[before + __popcll(here & ((1ull << lane) - 1ull))] = tid;
+    __syncthreads();
+    int32_t *out = a.choice + r0 + node;
+    if (m == 0) {
+        if (tid == 0) *out = -1;
+        return;
+    }
+    if (tid == 0) flag = first_accepted(a, r0, node, child[0]);
+    parent[tid] = tid < n && mine >= 0 && mine < tid ? mine : -1;
+    first[tid] = kMaxNodes;
+    __syncthreads();
+    if (flag || m == 1) {
+        if (tid == 0) *out = flag ? child[0] : -1;
+        return;
+    }
+    // Is the node ruled out: on the way up, a first child that is rejected, or another one whose first sibling is accepted
+    if (tid < n && parent[tid] >= 0) atomicMin(&first[parent[tid]], tid);
+    __syncthreads();
+    if (tid == 0) flag = 0;
+    int at = node, up = 0;               // every thread climbs; thread t tests step t of the way
+    while (parent[at] >= 0 && up < tid) { at = parent[at]; ++up; }
+    __syncthreads();
+    if (up == tid && parent[at] >= 0) {
+        const int above = parent[at];
+        if (first_accepted(a, r0, above, first[above]) != (first[above] == at)) flag = 1;
+    } 
+    __syncthreads();
+    if (flag) {
+        if (tid == 0) *out = -1;
+        return;
+    }
+    const float *p = a.p + (size_t)(r0 + node) * a.p_stride, *q = a.q ? a.q + (size_t)(r0 + node) * a.q_stride : nullptr;
+    if (tid == 0) mass[0] = 1.0;
+    int accepted = -1;
+    uint64_t all = 0;                    // without q: sum of the weights of p
+    for (int k = 1; k < m; ++k) {
+        __syncthreads();
+        double sum = 0.0;                // of integers, at most 512 of up to 2^44: exact
+        uint64_t total;
+        if (q || k == 1) {
+            for_row<kNodeThreads>(a, p, q, 0, a.V, [&](int, float pv, float qv) { sum += weight(q ? residual(pv, qv, mass, k) : positive((double)pv)); });
+            total = block_sum<kNodeThreads / 64>((uint64_t)sum, scratch);
+            all = total;
+        }
+        if (!q) {
+            // off comes the weight of every distinct token rejected so far
+            total = all;
+            for (int i = 0; i < k; ++i) {
+                const int x = a.tokens[r0 + child[i]];
+                bool again = !known(a, x);
+                for (int j = 0; j < i && !again; ++j) again = a.tokens[r0 + child[j]] == x;
+                if (!again) total -= (uint64_t)weight(positive((double)p[x]));
+            }
+        }
+        const double s = (double)total * 0x1p-44;
+        if (tid == 0) {
+            mass[k] = s;
+            a.mass[r0 + child[k - 1]] = s;
+        }
+        __syncthreads();
+        const int x = a.tokens[r0 + child[k]];
+        if (known(a, x)) {
+            double rho;
+            if (q) rho = residual(p[x], q[x], mass, k);
+            else {
+                rho = positive((double)p[x]);
+                for (int i = 0; i < k; ++i) if (a.tokens[r0 + child[i]] == x) rho = 0.0;
+            }
+            if (accepts(a.accept_words[r0 + child[k]], q ? (double)q[x] : 1.0, s, rho)) { accepted = child[k]; break; }
+        }
+    }
+    if (tid == 0) *out = accepted;
+}
+
+// Workgroup = slice of the last accepted node's rows: walks the path, sums the slice's weights; slice 0 writes the path
+__global__ __launch_bounds__(256) void verify_walk_kernel(VerifyArgs a) {
+    const int b = blockIdx.y, slice = blockIdx.x, tid = threadIdx.x;
+    int r0, n;
+    tree_rows(a, b, r0, n);
+    __shared__ int choice[kMaxNodes], child[kMaxNodes], way[2], wave_count[4];
+    __shared__ double mass[kMaxNodes];
+    __shared__ uint64_t scratch[4];
+    for (int i = tid; i < n; i += 256) choice[i] = a.choice[r0 + i];
+    if (slice == 0) for (int i = tid; i < a.max_path; i += 256) a.path[(size_t)b * a.max_path + i] = -1;
+    __syncthreads();
+    if (tid == 0) {
+        int at = n > 0 ? 0 : -1, len = n > 0 ? 1 : 0;
+        if (slice == 0 && len) a.path[(size_t)b * a.max_path] = 0;
+        while (at >= 0 && len < a.max_path && choice[at] > at) {
+            at = choice[at];
+            if (slice == 0) a.path[(size_t)b * a.max_path + len] = at;
+            ++len;
+        }
+        way[0] = at;
+        way[1] = len;
+        if (slice == 0) a.path_len[b] = len;
+    }
+    __syncthreads();
+    const int at = way[0];
+    // its rejected children: all of them, unless it is the path's length that ended the walk
+    int m = 0;
+    if (at >= 0 && choice[at] <= at)
+        for (int j0 = at + 1; j0 < n; j0 += 256) {
+            const int j = j0 + tid;
+            const bool is_child = j < n && a.parents[r0 + j] == at;
+            const unsigned long long here = __ballot(is_child);
+            const int lane = tid & 63, wave = tid >> 6;
+            if (lane == 0) wave_count[wave] = __popcll(here);
+            __syncthreads();
+            int before = m;
+            for (int w = 0; w < 4; ++w) {
+                if (w < wave) before += wave_count[w];
+                m += wave_count[w];
+            }
+            if (is_child) child[before + __popcll(here & ((1ull << lane) - 1ull))] = j;
+            __syncthreads();
+        }
+    for (int k = tid; k < m; k += 256) mass[k] = k ? a.mass[r0 + child[k - 1]] : 1.0;
+    __syncthreads();
+    if (slice == 0) {
+        if (tid == 0) { a.stop[2 * b] = at >= 0 ? r0 + at : -1; a.stop[2 * b + 1] = m; }
+        for (int k = tid; k < m; k += 256) {
+            a.stop_mass[r0 + k] = mass[k];
+            a.stop_token[r0 + k] = a.tokens[r0 + child[k]];
+        }
+    }
+    if (at < 0) return;
+    const float *p = a.p + (size_t)(r0 + at) * a.p_stride, *q = a.q ? a.q + (size_t)(r0 + at) * a.q_stride : nullptr;
+    const int lo = slice * kSlice, hi = min(lo + kSlice, a.V);
+    uint64_t sum = 0, plain = 0;
+    for_row<256>(a, p, q, lo, hi, [&](int v, float pv, float qv) {
+        double r = positive((double)pv);
+        plain += (uint64_t)weight(r);
+        if (q) r = residual(pv, qv, mass, m);
+        else for (int k = 0; k < m; ++k) if (a.tokens[r0 + child[k]] == v) r = 0.0;
+        sum += (uint64_t)weight(r);
+    });
+    sum = block_sum<4>(sum, scratch);
+    plain = block_sum<4>(plain, scratch);
+    if (tid == 0) {
+        uint64_t *part = a.part + ((size_t)b * a.n_slices + slice) * 2;
+        part[0] = sum;
+        part[1] = plain;
+    }
+}
+
+// Workgroup = sequence: the next token
+__global__ __launch_bounds__(256) void verify_draw_kernel(VerifyArgs a) {
+    const int b = blockIdx.x, tid = threadIdx.x;
+    const int row = a.stop[2 * b];
+    if (row < 0) {
+        if (tid == 0) a.next_token[b] = -1;
+        return;
+    }
+    __shared__ uint64_t scratch[4], start[2];
+    __shared__ int found[2];
+    int r0, n;
+    tree_rows(a, b, r0, n);
+    int m = a.stop[2 * b + 1];
+    // n_slices <= 256: a thread per slice
+    const uint64_t *part = a.part + (size_t)b * a.n_slices * 2;
+    uint64_t mine = tid < a.n_slices ? part[2 * tid] : 0;
+    uint64_t Z = block_sum<4>(mine, scratch);
+    if (Z == 0) {                                   // nothing is left: from p
+        m = 0;
+        mine = tid < a.n_slices ? part[2 * tid + 1] : 0;
+        Z = block_sum<4>(mine, scratch);
+    }
+    if (Z == 0) {
+        if (tid == 0) a.next_token[b] = -1;
+        return;
+    }
+    const uint64_t t = __umul64hi(a.draw_words[b], Z);
+    auto upto = [&](uint64_t v) {                   // inclusive prefix sum over the workgroup
+        const int lane = tid & 63, wave = tid >> 6;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t l = __shfl_up((uint32_t)v, d, 64), h = __shfl_up((uint32_t)(v >> 32), d, 64);
+            if (lane >= d) v += (uint64_t)h << 32 | l;
+        }
+        __syncthreads();
+        if (lane == 63) scratch[wave] = v;
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) v += scratch[w];
+        return v;
+    };
+    const uint64_t s = upto(mine);
+    if (s > t && s - mine <= t) { found[0] = tid; start[0] = s - mine; }
+    __syncthreads();
+    // within the slice: a thread owns 8 consecutive ids
+    constexpr int PER = kSlice / 256;
+    const int v0 = found[0] * kSlice + tid * PER;
+    const float *p = a.p + (size_t)row * a.p_stride, *q = a.q ? a.q + (size_t)row * a.q_stride : nullptr;
+    uint64_t w[PER], own = 0;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        const int v = v0 + e;
+        w[e] = 0;
+        if (v < a.V) {
+            double r = positive((double)p[v]);
+            if (q) r = residual(p[v], q[v], a.stop_mass + r0, m);
+            else for (int k = 0; k < m; ++k) if (a.stop_token[r0 + k] == v) r = 0.0;
+            w[e] = (uint64_t)weight(r);
+        }
+        own += w[e];
+    }
+    uint64_t c = start[0] + upto(own) - own;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        if (c <= t && c + w[e] > t) a.next_token[b] = v0 + e;
+        c += w[e];
+    }
+}
+
+#define VERIFY_FAIL(code, ...)                          \
+    do {                                                \
+        sjd_set_error(sjd_call_error(), __VA_ARGS__);   \
+        return code;                                    \
+    } while (0)
+#define VERIFY_TRY(expr) SJD_HIP_TRY(sjd_call_error(), expr)
+
+int check_sizes(int32_t n_rows, int32_t n_seqs, int32_t vocab) {
+    if (n_rows < 0 || n_rows > 1 << 29 || n_seqs < 1 || n_seqs > 65535) VERIFY_FAIL(SJD_EINVAL, "n_rows must be 0 .. 2^29, n_seqs 1 .. 65535");
+    if (vocab < 1 || vocab > kMaxVocab) VERIFY_FAIL(SJD_EINVAL, "vocab must be 1 .. %d", kMaxVocab);
+    return SJD_OK;
+}
+size_t up16(size_t b) { return (b + 15) / 16 * 16; }
+// parts of the workspace: mass, stop_mass, part, choice, stop_token, stop
+size_t workspace(VerifyArgs &a, char *base) {
+    size_t at = 0;
+    auto take = [&](size_t bytes) { char *p = base ? base + at : nullptr; at += up16(bytes); return (void *)p; };
+    a.mass = (double *)take((size_t)a.n_rows * 8);
+    a.stop_mass = (double *)take((size_t)a.n_rows * 8);
+    a.part = (uint64_t *)take((size_t)a.n_seqs * a.n_slices * 16);
+    a.choice = (int32_t *)take((size_t)a.n_rows * 4);
+    a.stop_token = (int32_t *)take((size_t)a.n_rows * 4);
+    a.stop = (int32_t *)take((size_t)a.n_seqs * 8);
+    return at;
+}
+
+}  // namespace
+
+extern "C" {
+
+int sjd_op_tree_verify_workspace(int32_t n_rows, int32_t n_seqs, int32_t vocab, uint64_t *bytes) {
+    const int rc = check_sizes(n_rows, n_seqs, vocab);
+    if (rc) return rc;
+    if (!bytes) VERIFY_FAIL(SJD_EINVAL, "null argument");
+    VerifyArgs a = {};
+    a.n_rows = n_rows;
+    a.n_seqs = n_seqs;
+    a.n_slices = ceil_div(vocab, kSlice);
+    *bytes = workspace(a, nullptr);
+    return SJD_OK;
+}
+
+int sjd_op_tree_verify(void *hip_stream, const int32_t *tokens, const int32_t *parents, const int32_t *row_start, const float *p, int64_t p_stride,
+                       const float *q, int64_t q_stride, const uint32_t *accept_words, const uint64_t *draw_words, int32_t *path,
+                       int32_t *path_len, int32_t *next_token, int32_t n_rows, int32_t n_seqs, int32_t vocab, int32_t max_rows,
+                       int32_t max_path, void *ws, uint64_t workspace_bytes) {
+    const int rc = check_sizes(n_rows, n_seqs, vocab);
+    if (rc) return rc;
+    if (max_rows < 1 || max_rows > kMaxNodes) VERIFY_FAIL(SJD_EINVAL, "max_rows must be 1 .. %d", kMaxNodes);
+    if (max_path < 1) VERIFY_FAIL(SJD_EINVAL, "max_path must be positive");
+    if (!row_start || !draw_words || !path || !path_len || !next_token || (n_rows && (!tokens || !parents || !p || !accept_words)))
+        VERIFY_FAIL(SJD_EINVAL, "null argument");
+    if (((uintptr_t)tokens | (uintptr_t)parents | (uintptr_t)row_start | (uintptr_t)p | (uintptr_t)q | (uintptr_t)accept_words | (uintptr_t)path |
+         (uintptr_t)path_len | (uintptr_t)next_token) % 4 || (uintptr_t)draw_words % 8) VERIFY_FAIL(SJD_EINVAL, "an array is not aligned to its elements");
+    VerifyArgs a = {};
+    a.tokens = tokens; a.parents = parents; a.row_start = row_start;
+    a.p = p; a.q = q; a.p_stride = (long)p_stride; a.q_stride = (long)q_stride;
+    a.accept_words = accept_words; a.draw_words = draw_words;
+    a.path = path; a.path_len = path_len; a.next_token = next_token;
+    a.n_rows = n_rows; a.n_seqs = n_seqs; a.max_rows = max_rows; a.max_path = max_path; a.V = vocab;
+    a.n_slices = ceil_div(vocab, kSlice);
+    a.wide = (uintptr_t)p % 16 == 0 && p_stride % 4 == 0 && (uintptr_t)q % 16 == 0 && q_stride % 4 == 0;
+    const size_t need = workspace(a, (char *)ws);
+    if (need > workspace_bytes) VERIFY_FAIL(SJD_ECAPACITY, "the workspace holds %llu bytes, %zu are needed", (unsigned long long)workspace_bytes, need);
+    if (!ws || (uintptr_t)ws % 16) VERIFY_FAIL(SJD_EINVAL, "the workspace must be 16-byte aligned");
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (n_rows) verify_nodes_kernel<<<dim3(max_rows < n_rows ? max_rows : n_rows, n_seqs), kNodeThreads, 0, st>>>(a);
+    VERIFY_TRY(hipGetLastError());
+    verify_walk_kernel<<<dim3(a.n_slices, n_seqs), 256, 0, st>>>(a);
+    VERIFY_TRY(hipGetLastError());
+    verify_draw_kernel<<<n_seqs, 256, 0, st>>>(a);
+    VERIFY_TRY(hipGetLastError());
+    return SJD_OK;
+}
+
+}  // extern "C"
