@@ -339,42 +339,62 @@ def op_philox(seed, row, seq, n):
     return out.cpu().numpy().view(np.uint32).reshape(n, 4)
 
 
-# ---- operators of a step of tree speculation.  They enqueue their work on the current stream of their tensors' device and return.
+# ---- operators of a step of tree speculation.  They enqueue their work on the current stream of their tensors' device and return.  A
+# decoding step makes a handful of such calls a layer, of a few microseconds of work each: what is looked up or allocated here counts
+# (torch.cuda.current_stream() alone takes 2.9 us, the raw handle 0.1).
 
 _CACHE_DTYPES = {"f32": F32, "bf16": BF16, "fp8": FP8}
 _SCALINGS = {"none": 0, "linear": 1, "base": 2, "parts": 3}
 
 
-def _need(ok, message):
-    if not ok:
-        raise SjdError(EINVAL, message)
+def _refuse(message):
+    raise SjdError(EINVAL, message)
 
 
-def _same_device(first, *others):
-    """The device of `first`; the other tensors (None: not given) have to be there too."""
-    _need(first.is_cuda, "tensors must be on a GPU")
-    _need(all(t is None or t.device == first.device for t in others), "tensors are on different devices")
-    return first.device
+def _device_of(first, *others):
+    """Index of the device of `first`; the other tensors (None: not given) have to be there too."""
+    d = first.get_device()
+    if d < 0:
+        _refuse("tensors must be on a GPU")
+    for t in others:
+        if t is not None and t.get_device() != d:
+            _refuse("tensors are on different devices")
+    return d
 
 
-def _index(t, n, name, dtype="int32"):
+def _enqueue(device, function, *args):
+    """function(current stream of the device, *args) with the device current; its errors are raised."""
     import torch
-    _need(t.dtype == getattr(torch, dtype) and t.dim() == 1 and t.is_contiguous() and (n is None or t.numel() == n),
-          f"{name} must be a contiguous {dtype} vector" + ("" if n is None else f" of {n}"))
+    if torch._C._cuda_getDevice() == device:
+        rc = function(torch._C._cuda_getCurrentRawStream(device), *args)
+    else:
+        with torch.cuda.device(device):
+            rc = function(torch._C._cuda_getCurrentRawStream(device), *args)
+    if rc:
+        _check(rc)
 
 
-def _heads_of(x, heads, hd, name):
-    """x [rows, heads, hd] with contiguous heads: its row stride."""
+def _vector(t, n, dtype, name):
+    if t.dtype is not dtype or t.dim() != 1 or (n is not None and t.shape[0] != n) or not t.is_contiguous():
+        _refuse(f"{name} must be a contiguous vector of {dtype}" + ("" if n is None else f" with {n} elements"))
+    return t.data_ptr()
+
+
+def _row_code(t, name):
     import torch
-    _need(x.dtype in (torch.float32, torch.bfloat16), f"{name} must be float32 or bfloat16")
-    _need(x.dim() == 3 and x.shape[1] == heads and x.shape[2] == hd, f"{name} must be [rows, {heads}, {hd}]")
-    _need(x.numel() == 0 or ((hd == 1 or x.stride(2) == 1) and (heads == 1 or x.stride(1) == hd)), f"{name}: the heads of a row must be contiguous")
-    return x.stride(0) if x.shape[0] > 1 else heads * hd
+    if t.dtype is torch.bfloat16:
+        return BF16
+    return F32 if t.dtype is torch.float32 else _refuse(f"{name} must be float32 or bfloat16")
 
 
-def _on(device):
-    import torch
-    return torch.cuda.device(device)
+def _row_stride(x, heads, hd, name):
+    """Row stride of x [rows, heads, hd], whose heads have to be contiguous within a row."""
+    shape, stride = x.shape, x.stride()
+    if len(shape) != 3 or shape[1] != heads or shape[2] != hd:
+        _refuse(f"{name} must be [rows, {heads}, {hd}]")
+    if (stride[2] != 1 and hd != 1) or (stride[1] != hd and heads != 1):
+        _refuse(f"{name}: the heads of a row must be contiguous")
+    return stride[0] if shape[0] > 1 else heads * hd
 
 
 class KvCache:
@@ -383,70 +403,70 @@ class KvCache:
 
     def __init__(self, dtype, n_pages, page_tokens, n_kv_heads, head_dim, page_table):
         import torch
-        _need(dtype in _CACHE_DTYPES, "dtype must be f32, bf16 or fp8")
-        _need(page_table.is_cuda and page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.is_contiguous(),
-              "page_table must be a contiguous int32 CUDA matrix")
+        if dtype not in _CACHE_DTYPES:
+            _refuse("dtype must be f32, bf16 or fp8")
+        if not (page_table.is_cuda and page_table.dtype is torch.int32 and page_table.dim() == 2 and page_table.is_contiguous()):
+            _refuse("page_table must be a contiguous int32 CUDA matrix")
+        if n_pages < 1:
+            _refuse("n_pages must be positive")
         self.dtype, self.n_kv_heads, self.head_dim, self.page_table = dtype, n_kv_heads, head_dim, page_table
         self.n_seqs, self.device = page_table.shape[0], page_table.device
         self.desc = KvCacheDesc(None, page_table.data_ptr(), n_pages, page_tokens, n_kv_heads, head_dim, _CACHE_DTYPES[dtype], *page_table.shape)
+        self.ref = C.byref(self.desc)
         n = C.c_uint64(0)
-        _check(lib().sjd_cache_page_bytes(C.byref(self.desc), C.byref(n)))
-        _need(n_pages >= 1, "n_pages must be positive")
+        _check(lib().sjd_cache_page_bytes(self.ref, C.byref(n)))
         self.pages = torch.zeros(n_pages * n.value, dtype=torch.uint8, device=self.device)
         self.desc.pages = self.pages.data_ptr()
-
-    def ref(self):
-        return C.byref(self.desc)
+        self.workspaces = {}    # bytes of op_tree_attention's workspace, by the sizes that they follow from
 
 
 def op_cache_write(cache, k, v, row_start, first_pos):
     """Writes k and v [rows, n_kv_heads, head_dim] (float32 or bfloat16; rows may be strided) to positions first_pos[b] + i of sequence b =
     rows row_start[b] + i.  row_start int32 [n_seqs + 1], first_pos int32 [n_seqs]."""
-    _same_device(cache.page_table, k, v, row_start, first_pos)
-    ks, vs = _heads_of(k, cache.n_kv_heads, cache.head_dim, "k"), _heads_of(v, cache.n_kv_heads, cache.head_dim, "v")
-    _need(k.dtype == v.dtype and k.shape == v.shape, "k and v must have one dtype and shape")
-    _index(row_start, cache.n_seqs + 1, "row_start")
-    _index(first_pos, cache.n_seqs, "first_pos")
-    with _on(cache.device):
-        _check(lib().sjd_op_cache_write(_stream_ptr(), cache.ref(), _dtype_code(k), k.data_ptr(), ks, v.data_ptr(), vs, row_start.data_ptr(),
-                                        first_pos.data_ptr(), k.shape[0]))
+    import torch
+    device = _device_of(cache.page_table, k, v, row_start, first_pos)
+    code, n = _row_code(k, "k"), k.shape[0]
+    ks, vs = _row_stride(k, cache.n_kv_heads, cache.head_dim, "k"), _row_stride(v, cache.n_kv_heads, cache.head_dim, "v")
+    if v.dtype is not k.dtype or v.shape[0] != n:
+        _refuse("k and v must have one dtype and number of rows")
+    _enqueue(device, lib().sjd_op_cache_write, cache.ref, code, k.data_ptr(), ks, v.data_ptr(), vs, _vector(row_start, cache.n_seqs + 1, torch.int32, "row_start"),
+             _vector(first_pos, cache.n_seqs, torch.int32, "first_pos"), n)
 
 
 def op_cache_read(cache, row_start, first_pos, n_rows, dtype=None, out=None):
     """-> (k, v) [n_rows, n_kv_heads, head_dim] of `dtype` (bfloat16 unless given): what is stored at positions first_pos[b] + i of sequence
     b, in rows row_start[b] + i.  out: a pair of such tensors to write to.  Rows of no sequence are not written."""
     import torch
-    _same_device(cache.page_table, row_start, first_pos, *(out or ()))
-    _index(row_start, cache.n_seqs + 1, "row_start")
-    _index(first_pos, cache.n_seqs, "first_pos")
-    dtype = dtype or (out[0].dtype if out else torch.bfloat16)
-    _need(dtype in (torch.float32, torch.bfloat16), "dtype must be float32 or bfloat16")
+    device = _device_of(cache.page_table, row_start, first_pos, *(out or ()))
     shape = (n_rows, cache.n_kv_heads, cache.head_dim)
     if out is None:
-        out = tuple(torch.empty(shape, dtype=dtype, device=cache.device) for _ in range(2))
-    _need(all(t.shape == shape and t.dtype == dtype and t.is_contiguous() for t in out), "out must be two contiguous tensors of the result's shape")
-    with _on(cache.device):
-        _check(lib().sjd_op_cache_read(_stream_ptr(), cache.ref(), _dtype_code(out[0]), out[0].data_ptr(), out[1].data_ptr(), row_start.data_ptr(),
-                                       first_pos.data_ptr(), n_rows))
+        if n_rows < 0:
+            _refuse("n_rows must not be negative")
+        k = torch.empty(shape, dtype=dtype or torch.bfloat16, device=cache.device)
+        out = k, torch.empty_like(k)
+    elif any(t.shape != shape or t.dtype is not (dtype or out[0].dtype) or not t.is_contiguous() for t in out):
+        _refuse("out must be two contiguous tensors of the result's shape and dtype")
+    _enqueue(device, lib().sjd_op_cache_read, cache.ref, _row_code(out[0], "dtype"), out[0].data_ptr(), out[1].data_ptr(),
+             _vector(row_start, cache.n_seqs + 1, torch.int32, "row_start"), _vector(first_pos, cache.n_seqs, torch.int32, "first_pos"), n_rows)
     return out
 
 
 def op_cache_compact(cache, first_pos, path, path_len):
     """Moves the entries at positions first_pos[b] + path[b, j] to first_pos[b] + j, j < path_len[b].  path int32 [n_seqs, max_path]."""
     import torch
-    _same_device(cache.page_table, first_pos, path, path_len)
-    _index(first_pos, cache.n_seqs, "first_pos")
-    _index(path_len, cache.n_seqs, "path_len")
-    _need(path.dtype == torch.int32 and path.dim() == 2 and path.shape[0] == cache.n_seqs and path.is_contiguous(), "path must be a contiguous int32 [n_seqs, max_path]")
-    with _on(cache.device):
-        _check(lib().sjd_op_cache_compact(_stream_ptr(), cache.ref(), first_pos.data_ptr(), path.data_ptr(), path_len.data_ptr(), path.shape[1]))
+    device = _device_of(cache.page_table, first_pos, path, path_len)
+    if path.dtype is not torch.int32 or path.dim() != 2 or path.shape[0] != cache.n_seqs or not path.is_contiguous():
+        _refuse("path must be a contiguous int32 [n_seqs, max_path]")
+    _enqueue(device, lib().sjd_op_cache_compact, cache.ref, _vector(first_pos, cache.n_seqs, torch.int32, "first_pos"), path.data_ptr(),
+             _vector(path_len, cache.n_seqs, torch.int32, "path_len"), path.shape[1])
 
 
 def rope_table(rotary_dim, theta=10000.0, scaling="none", factor=1.0, trained_ctx=0.0, low_turns=1.0, high_turns=32.0, device="cuda"):
     """Frequencies for op_rotary (sjd_rope_table) on the device, as the bits of an int64 tensor [rotary_dim / 2].  scaling: "none",
     "linear", "base" or "parts"."""
     import torch
-    _need(scaling in _SCALINGS, "scaling must be none, linear, base or parts")
+    if scaling not in _SCALINGS:
+        _refuse("scaling must be none, linear, base or parts")
     table = np.zeros(max(rotary_dim // 2, 1), dtype=np.uint64)
     _check(lib().sjd_rope_table(rotary_dim, theta, _SCALINGS[scaling], factor, trained_ctx, low_turns, high_turns, table.ctypes.data))
     return torch.from_numpy(table.view(np.int64)).to(device)
@@ -456,23 +476,29 @@ def op_rotary(q, k, positions, table, interleaved=False, magnitude=1.0, out=None
     """Turns q [rows, heads, hd] and k [rows, kv_heads, hd] (or None) by their rows' positions (int32) -> (q', k').  out: tensors to write to, which may
     be q and k themselves."""
     import torch
-    device = _same_device(q, k, positions, table, *(out or ()))
-    rows, hd = q.shape[0], q.shape[-1]
-    xs = [q] if k is None else [q, k]
+    device = _device_of(q, k, positions, table, *(out or ()))
+    code, shape = _row_code(q, "q"), q.shape
+    if len(shape) != 3:
+        _refuse("q must be [rows, heads, head_dim]")
+    rows, heads, hd = shape
     if out is None:
-        out = [torch.empty(x.shape, dtype=x.dtype, device=device) for x in xs]
-    ys = [y for y in out if y is not None]
-    _need(len(ys) == len(xs) and all(y.shape == x.shape for x, y in zip(xs, ys)), "out must have the shapes of q and k")
-    _need(all(t.dtype == q.dtype and t.shape[0] == rows for t in xs + ys), "q, k and out must have one dtype and number of rows")
-    _index(positions, rows, "positions")
-    _index(table, None, "table", "int64")
-    args = [a for x, y in zip(xs, ys) for a in (x.data_ptr(), _heads_of(x, x.shape[1], hd, "q and k"), y.data_ptr(), _heads_of(y, y.shape[1], hd, "out"),
-                                                x.shape[1])]
-    args += [None, 0, None, 0, 0] if k is None else []
-    with _on(device):
-        _check(lib().sjd_op_rotary(_stream_ptr(), _dtype_code(q), 1 if interleaved else 0, table.data_ptr(), 2 * table.numel(), magnitude,
-                                   positions.data_ptr(), rows, hd, *args))
-    return ys[0], ys[1] if k is not None else None
+        # (new tensors are contiguous, whatever the strides of q and k)
+        q_out, k_out = q.new_empty(shape), None if k is None else k.new_empty(k.shape)
+    else:
+        q_out, k_out = out[0], out[1] if len(out) > 1 else None
+        if (k_out is None) != (k is None) or q_out.dtype is not q.dtype or q_out.shape[0] != rows or (k is not None and (k_out.dtype is not q.dtype or k_out.shape != k.shape)):
+            _refuse("out must have the shapes and dtype of q and k")
+    if k is None:
+        keys = (None, 0, None, 0, 0)
+    else:
+        if k.dtype is not q.dtype or k.shape[0] != rows or k.dim() != 3:
+            _refuse("k must have q's dtype and number of rows")
+        n = k.shape[1]
+        keys = (k.data_ptr(), _row_stride(k, n, hd, "k"), k_out.data_ptr(), n * hd if out is None else _row_stride(k_out, n, hd, "out"), n)
+    _enqueue(device, lib().sjd_op_rotary, code, 1 if interleaved else 0, _vector(table, None, torch.int64, "table"), 2 * table.shape[0], magnitude,
+             _vector(positions, rows, torch.int32, "positions"), rows, hd, q.data_ptr(), _row_stride(q, heads, hd, "q"), q_out.data_ptr(),
+             heads * hd if out is None else _row_stride(q_out, heads, hd, "out"), heads, *keys)
+    return q_out, k_out
 
 
 def tree_masks(parents, mask_words=None):
@@ -485,45 +511,55 @@ def tree_masks(parents, mask_words=None):
     return mask, depth
 
 
-def _workspace(given, need, device):
+def _workspace(given, need, like):
+    """-> (pointer, bytes, what to keep until the call is enqueued)"""
     import torch
     if given is None:
-        return torch.empty(need, dtype=torch.uint8, device=device) if need else None
-    _need(given.is_contiguous(), "the workspace must be contiguous")
-    return given
-
-
-def _bytes(t):
-    return 0 if t is None else t.numel() * t.element_size()
+        if not need:
+            return None, 0, None
+        given = torch.empty(need, dtype=torch.uint8, device=like.device)
+        return given.data_ptr(), need, given
+    if not given.is_contiguous():
+        _refuse("the workspace must be contiguous")
+    return given.data_ptr(), given.numel() * given.element_size(), given
 
 
 def op_tree_attention(q, cache, row_start, ctx_len, mask=None, max_rows=None, max_ctx=None, scale=0.0, out=None, workspace=None):
     """Attention of q [rows, heads, head_dim] over the cache: row row_start[b] + i (position ctx_len[b] + i) sees positions [0, ctx_len[b])
     and the nodes whose bits are set in its row of mask, int32 or uint32 [rows, words]; without a mask nodes 0 .. i.  max_rows: no tree has more
-    (default: all rows); max_ctx: what ctx_len is expected to reach (default: what the page table holds).  -> out like q; rows of no sequence are not written."""
+    (default: all rows); max_ctx: what ctx_len is expected to reach (default: what the page table holds).  -> out like q; rows of no sequence
+    are not written."""
     import torch
-    device = _same_device(cache.page_table, q, row_start, ctx_len, mask, out, workspace)
-    _need(q.dim() == 3, "q must be [rows, heads, head_dim]")
-    rows, heads = q.shape[0], q.shape[1]
-    stride = _heads_of(q, heads, cache.head_dim, "q")
-    _index(row_start, cache.n_seqs + 1, "row_start")
-    _index(ctx_len, cache.n_seqs, "ctx_len")
+    device = _device_of(cache.page_table, q, row_start, ctx_len, mask, out, workspace)
+    code, shape, hd = _row_code(q, "q"), q.shape, cache.head_dim
+    if len(shape) != 3:
+        _refuse("q must be [rows, heads, head_dim]")
+    rows, heads = shape[0], shape[1]
+    stride = _row_stride(q, heads, hd, "q")
+    mask_ptr, words = None, 0
     if mask is not None:
-        _need(mask.dtype in (torch.int32, torch.uint32) and mask.dim() == 2 and mask.shape[0] == rows and mask.is_contiguous(),
-              "mask must be a contiguous int32 or uint32 [rows, words]")
+        if mask.dtype not in (torch.int32, torch.uint32) or mask.dim() != 2 or mask.shape[0] != rows or not mask.is_contiguous():
+            _refuse("mask must be a contiguous int32 or uint32 [rows, words]")
+        mask_ptr, words = mask.data_ptr(), mask.shape[1]
     if out is None:
-        out = torch.empty((rows, heads, cache.head_dim), dtype=q.dtype, device=device)
-    _need(out.dtype == q.dtype and out.shape == q.shape, "out must be like q")
-    max_rows = max(rows, 1) if max_rows is None else max_rows
-    max_ctx = cache.desc.pages_per_seq * cache.desc.page_tokens if max_ctx is None else max_ctx
-    with _on(device):
-        need = C.c_uint64(0)
-        _check(lib().sjd_op_tree_attention_workspace(cache.ref(), heads, max_rows, max_ctx, C.byref(need)))
-        workspace = _workspace(workspace, need.value, device)
-        _check(lib().sjd_op_tree_attention(_stream_ptr(), cache.ref(), _dtype_code(q), q.data_ptr(), stride, out.data_ptr(),
-                                           _heads_of(out, heads, cache.head_dim, "out"), row_start.data_ptr(), ctx_len.data_ptr(),
-                                           None if mask is None else mask.data_ptr(), 0 if mask is None else mask.shape[1], rows, heads, scale, max_rows,
-                                           max_ctx, None if workspace is None else workspace.data_ptr(), _bytes(workspace)))
+        out, out_stride = q.new_empty(shape), heads * hd
+    else:
+        if out.dtype is not q.dtype or out.shape != shape:
+            _refuse("out must be like q")
+        out_stride = _row_stride(out, heads, hd, "out")
+    if max_rows is None:
+        max_rows = max(rows, 1)
+    if max_ctx is None:
+        max_ctx = cache.desc.pages_per_seq * cache.desc.page_tokens
+    need = cache.workspaces.get((heads, max_rows, max_ctx))
+    if need is None:
+        n = C.c_uint64(0)
+        _check(lib().sjd_op_tree_attention_workspace(cache.ref, heads, max_rows, max_ctx, C.byref(n)))
+        need = cache.workspaces[heads, max_rows, max_ctx] = n.value
+    at, size, keep = _workspace(workspace, need, q)
+    _enqueue(device, lib().sjd_op_tree_attention, cache.ref, code, q.data_ptr(), stride, out.data_ptr(), out_stride,
+             _vector(row_start, cache.n_seqs + 1, torch.int32, "row_start"), _vector(ctx_len, cache.n_seqs, torch.int32, "ctx_len"), mask_ptr, words, rows, heads, scale,
+             max_rows, max_ctx, at, size)
     return out
 
 
@@ -532,28 +568,27 @@ def op_tree_verify(tokens, parents, row_start, p, q, accept_words, draw_words, m
     [rows], the bits of 32-bit words (int32 or uint32); draw_words [n_seqs], of 64-bit words.  -> (path int32 [n_seqs, max_path], path_len int32
     [n_seqs], next_token int32 [n_seqs])."""
     import torch
-    device = _same_device(p, tokens, parents, row_start, q, accept_words, draw_words, workspace)
-    rows, seqs = tokens.shape[0], row_start.shape[0] - 1
-    _index(tokens, rows, "tokens")
-    _index(parents, rows, "parents")
-    _index(row_start, seqs + 1, "row_start")
+    device = _device_of(p, tokens, parents, row_start, q, accept_words, draw_words, workspace)
+    rows, seqs, shape = tokens.shape[0], row_start.shape[0] - 1, p.shape
     for t in (p,) if q is None else (p, q):
-        _need(t.dtype == torch.float32 and t.dim() == 2 and t.shape[0] == rows and t.shape[1] == p.shape[1] and (t.shape[1] == 1 or t.stride(1) == 1),
-              "p and q must be float32 [rows, vocab] with contiguous rows")
-    _index(accept_words, rows, "accept_words", "uint32" if accept_words.dtype == torch.uint32 else "int32")
-    _index(draw_words, seqs, "draw_words", "uint64" if draw_words.dtype == torch.uint64 else "int64")
-    max_rows = min(max(rows, 1), 1024) if max_rows is None else max_rows
-    max_path = max_rows if max_path is None else max_path
-    _need(max_path >= 1, "max_path must be positive")
-    strides = [0 if t is None else t.stride(0) if rows > 1 else t.shape[1] for t in (p, q)]
-    path = torch.empty((seqs, max_path), dtype=torch.int32, device=device)
-    path_len, token = (torch.empty(seqs, dtype=torch.int32, device=device) for _ in range(2))
-    with _on(device):
-        need = C.c_uint64(0)
-        _check(lib().sjd_op_tree_verify_workspace(rows, seqs, p.shape[1], C.byref(need)))
-        workspace = _workspace(workspace, need.value, device)
-        _check(lib().sjd_op_tree_verify(_stream_ptr(), tokens.data_ptr(), parents.data_ptr(), row_start.data_ptr(), p.data_ptr(), strides[0],
-                                        None if q is None else q.data_ptr(), strides[1], accept_words.data_ptr(), draw_words.data_ptr(), path.data_ptr(),
-                                        path_len.data_ptr(), token.data_ptr(), rows, seqs, p.shape[1], max_rows, max_path, workspace.data_ptr(),
-                                        _bytes(workspace)))
+        if t.dtype is not torch.float32 or t.dim() != 2 or t.shape != shape or shape[0] != rows or (shape[1] != 1 and t.stride(1) != 1):
+            _refuse("p and q must be float32 [rows, vocab] with contiguous rows")
+    if max_rows is None:
+        max_rows = min(max(rows, 1), 1024)
+    if max_path is None:
+        max_path = max_rows
+    if max_path < 1:
+        _refuse("max_path must be positive")
+    path = torch.empty((seqs, max_path), dtype=torch.int32, device=p.device)
+    path_len = path.new_empty(seqs)
+    token = path.new_empty(seqs)
+    n = C.c_uint64(0)
+    _check(lib().sjd_op_tree_verify_workspace(rows, seqs, shape[1], C.byref(n)))
+    at, size, keep = _workspace(workspace, n.value, p)
+    _enqueue(device, lib().sjd_op_tree_verify, _vector(tokens, rows, torch.int32, "tokens"), _vector(parents, rows, torch.int32, "parents"),
+             _vector(row_start, seqs + 1, torch.int32, "row_start"), p.data_ptr(), p.stride(0) if rows > 1 else shape[1], None if q is None else q.data_ptr(),
+             0 if q is None else q.stride(0) if rows > 1 else shape[1],
+             _vector(accept_words, rows, torch.uint32 if accept_words.dtype is torch.uint32 else torch.int32, "accept_words"),
+             _vector(draw_words, seqs, torch.uint64 if draw_words.dtype is torch.uint64 else torch.int64, "draw_words"), path.data_ptr(), path_len.data_ptr(),
+             token.data_ptr(), rows, seqs, shape[1], max_rows, max_path, at, size)
     return path, path_len, token
