@@ -86,10 +86,10 @@ constexpr uint32_t tree_visible(const uint32_t *mask, int mask_words, int ctx, i
     return ((nodes & ~cached) | cached) & there;
 }
 
-// Blocks of 32 tokens [first, last) that split `split` of n_splits goes through, of a tile whose last row is node last_node
+// Blocks of 32 tokens [first, last) that split `split` of n_splits goes through, of rows the last of which is node last_node
 struct TreeBlocks { int first, last; };
 constexpr TreeBlocks tree_blocks(bool mask, int ctx, int n_tot, int last_node, int split, int n_splits) {
-    // a window's rows see no node behind the tile's last one
+    // a window's rows see no node behind the last one
     const int n_vis = mask || ctx + last_node + 1 > n_tot ? n_tot : ctx + last_node + 1;
     const int blocks = (n_vis + 31) >> 5, chunk = (blocks + n_splits - 1) / n_splits;
     TreeBlocks r{split * chunk, split * chunk + chunk};

@@ -15,30 +15,14 @@ struct TreeArgs {
     long q_stride, out_stride;
     const int32_t *row_start, *ctx_len;
     const uint32_t *mask;      // [n_rows][mask_words], NULL: a window
-    int mask_words, n_rows, max_rows, H, G, tiles, n_splits;
+    int mask_words, n_rows, max_rows, H, G;
+    int tiles, groups;         // of rows: tiles of 32, and of as many tiles as a workgroup takes
+    int n_splits;              // of every sequence's context
     float scale_log2e;
-    float *part_o;             // [group][tile][32][hd]   unnormalised, group = (sequence, kv head, split)
-    float *part_ml;            // [group][tile][2][32]    running maximum (base 2), running sum
+    float *part_o;             // [sequence][kv head][split][tiles][32 * hd]  unnormalised, order of tree_part_index
+    float *part_ml;            // [sequence][kv head][split][tiles][2][32]    running maximum (base 2), running sum
     bool q_wide, out_wide;     // rows 16-byte (out: 4 elements) aligned
 };
-
-// What a workgroup of the launch works on
-struct TreeWork { int b, kvh, tile, split; };
-// tiles of one (sequence, kv head, split) read the same keys and values: they run on one XCD (workgroups go round the 8 XCDs), near each other in time
-SJD_D TreeWork tree_work(const TreeArgs &a, unsigned id) {
-    const unsigned xcd = id & 7, rest = id >> 3;
-    const unsigned tile = rest % a.tiles, group = (rest / a.tiles) * 8 + xcd;
-    TreeWork w;
-    w.tile = tile;
-    w.split = group % a.n_splits;
-    w.kvh = (group / a.n_splits) % a.c.n_kv;
-    w.b = group / a.n_splits / a.c.n_kv;
-    return w;
-}
-inline unsigned tree_grid(const TreeArgs &a) { return (unsigned)(ceil_div_sz((size_t)a.c.n_seqs * a.c.n_kv * a.n_splits, 8) * 8 * a.tiles); }
-SJD_D size_t tree_slot(const TreeArgs &a, int b, int kvh, int split, int tile) {
-    return ((((size_t)b * a.c.n_kv + kvh) * a.n_splits + split) * a.tiles + tile);
-}
 
 // Rows and length of sequence b
 struct TreeSeq { int r0, n, ctx, n_tot; };
@@ -51,6 +35,55 @@ SJD_D TreeSeq tree_seq(const TreeArgs &a, int b) {
     s.n_tot = min(s.ctx + s.n, cap);
     return s;
 }
+
+// What a workgroup of the launch works on: a group of row tiles, of a split of a (sequence, kv head).  The groups of a split read the same keys and
+// values: they run on one XCD (workgroups go round the 8 XCDs), near each other in time.
+struct TreeWork { int b, kvh, split, group; };
+SJD_D TreeWork tree_work(const TreeArgs &a, unsigned id) {
+    const unsigned xcd = id & 7, rest = id >> 3, share = rest / a.groups * 8 + xcd;
+    TreeWork w;
+    w.group = rest % a.groups;
+    w.split = share % a.n_splits;
+    w.kvh = share / a.n_splits % a.c.n_kv;
+    w.b = share / a.n_splits / a.c.n_kv;
+    return w;
+}
+inline unsigned tree_grid(const TreeArgs &a) { return (unsigned)(ceil_div_sz((size_t)a.c.n_seqs * a.c.n_kv * a.n_splits, 8) * 8 * a.groups); }
+SJD_D size_t tree_slot(const TreeArgs &a, int b, int kvh, int split, int tile) { return ((((size_t)b * a.c.n_kv + kvh) * a.n_splits + split) * a.tiles + tile); }
+
+// The pages of a sequence, block by block: the lanes hold 64 entries of its table at a time, so that a block's address does not wait for one
+struct TreePages {
+    const int32_t *table;
+    int per_seq, page_tokens, n_pages, idx, slot, base, held;
+    SJD_D TreePages(const TreeArgs &a, int b, int blk)
+        : table(a.c.page_table + (size_t)b * a.c.pages_per_seq), per_seq(a.c.pages_per_seq), page_tokens(a.c.page_tokens), n_pages(a.c.n_pages) {
+        idx = 32 * blk / page_tokens;
+        slot = 32 * blk - idx * page_tokens;
+        hold();
+    }
+    SJD_D void hold() {
+        base = idx;
+        const int i = idx + (int)(threadIdx.x & 63);
+        held = i < per_seq ? table[i] : -1;
+    }
+    // page of the block (its first token: slot), -1 where there is none
+    SJD_D int page() {
+        if (idx - base >= 64) hold();
+        const int p = __builtin_amdgcn_readlane(held, idx - base);
+        return (unsigned)p < (unsigned)n_pages ? p : -1;
+    }
+    SJD_D void advance(int blocks) {
+        slot += 32 * blocks;
+        while (slot >= page_tokens) { slot -= page_tokens; ++idx; }
+    }
+};
+// Registers that are loaded ahead of a loop: waits for them there.  (Where the first use is in the loop the compiler's wait is, too, and is one
+// for everything that the loop has asked for since.)
+template <int N> SJD_D void arrived(u32x4 (&x)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i]));
+}
+
 // ------------------------------------------------------------------------------------------------ one block of 32 tokens
 // by value: __builtin_bit_cast of an element of a vector that is named in place takes the vector's first element, whichever is meant
 SJD_D float as_float(uint32_t u) { return __builtin_bit_cast(float, u); }
@@ -193,6 +226,22 @@ template <int HD> struct TreeState {
     }
 };
 
+// The state is rescaled only when a row's maximum has grown by more than a factor of 2^8: until then its probabilities are up to 2^8 in
+// place of 1, which costs neither fp32 sums nor bf16 operands a bit.
+template <int HD> SJD_D void tree_rescale(TreeState<HD> &st, float mx) {
+    if (!__ballot(mx > st.m + 8.0f)) return;
+    const float m = fmaxf(st.m, mx);
+    const float alpha = __builtin_amdgcn_exp2f(st.m - (m == -INFINITY ? 0.0f : m));     // (not (-inf) - (-inf))
+    st.m = m;
+    st.l *= alpha;
+#pragma unroll
+    for (int db = 0; db < HD / 32; ++db) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) st.o[db][v] *= alpha;
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
 // Softmax of a block's scores into p (and, but for F32, its bf16 operand pb), and the rescaling of the state.  `vis`: bit k = this lane's
 // row sees token k of the block.
 template <int KIND, int HD>
@@ -207,21 +256,15 @@ SJD_D void tree_softmax(const TreeFrag<KIND, HD> &f, f32x16 s, bool masked, uint
 #pragma unroll
     for (int v = 1; v < 16; ++v) mx = fmaxf(mx, s[v]);
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * scale_log2e;
-    const float m_new = fmaxf(st.m, mx);
-    const float m_use = m_new == -INFINITY ? 0.0f : m_new;  // a row that has seen nothing so far: not (-inf) - (-inf)
-    const float alpha = __builtin_amdgcn_exp2f(st.m - m_use);
+    tree_rescale<HD>(st, mx);
+    const float m_use = st.m == -INFINITY ? 0.0f : st.m;    // a row that has seen nothing so far: not (-inf) - (-inf)
     float sum = 0.0f;
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
         p[v] = __builtin_amdgcn_exp2f(fmaf(s[v], scale_log2e, -m_use));
         sum += p[v];
     }
-    st.l = st.l * alpha + sum;
-    st.m = m_new;
-#pragma unroll
-    for (int db = 0; db < HD / 32; ++db)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) st.o[db][v] *= alpha;
+    st.l += sum;
     if constexpr (KIND != SJD_F32) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -248,7 +291,7 @@ template <int KIND, int HD> SJD_D float tree_value(const TreeFrag<KIND, HD> &f, 
     else return (f.v[db][m] >> (8 * e) & 0x7Fu) == 0x7Fu ? __builtin_nanf("") : 0.0f;
 }
 template <int KIND, int HD>
-SJD_D void tree_take_wild(TreeFrag<KIND, HD> &f, uint32_t vis, uint32_t (&wild)[3][HD], int lane) {
+SJD_D void tree_note_wild(const TreeFrag<KIND, HD> &f, uint32_t vis, uint32_t (&wild)[3][HD], int lane) {
 #pragma unroll
     for (int m = 0; m < 4; ++m)
 #pragma unroll
@@ -261,7 +304,6 @@ SJD_D void tree_take_wild(TreeFrag<KIND, HD> &f, uint32_t vis, uint32_t (&wild)[
                 if (cls != VALUE_FINITE && rows) atomicOr(&wild[cls - 1][db * 32 + (lane & 31)], rows);
             }
         }
-    tree_values_tame<KIND, HD>(f);
 }
 // what the noted elements make of dimension j of a row
 template <int HD> SJD_D float tree_add_wild(float x, const uint32_t (&wild)[3][HD], int row, int j) {
@@ -316,9 +358,26 @@ template <int KIND> SJD_D void tree_store(const TreeArgs &a, size_t row, int h, 
     }
 }
 
+// Partial results lie in the order in which the lanes hold them: a wavefront's store is 1 KiB
+SJD_D int tree_part_index(int row, int j) { return ((j >> 3) * 64 + ((j >> 2) & 1) * 32 + row) * 4; }
+
+// what the noted wild elements and the norm make of the quad of dimensions j of a row, and where it goes: to the output, or to a partial result
+template <int KIND, int HD>
+SJD_D void tree_finish(const TreeArgs &a, const TreeSeq &s, int kvh, size_t slot, int tile, int row, int j, float norm, bool any_wild, const uint32_t (&wild)[3][HD], f32x4 t) {
+    const int rho = 32 * tile + row, node = rho / a.G;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        t[e] = norm == 0.0f ? 0.0f : t[e] * norm;
+        if (any_wild) t[e] = tree_add_wild<HD>(t[e], wild, row, j + e);
+    }
+    if (node >= s.n) return;
+    if (a.n_splits > 1) *reinterpret_cast<f32x4 *>(a.part_o + slot * 32 * HD + tree_part_index(row, j)) = t;
+    else tree_store<KIND>(a, (size_t)s.r0 + node, kvh * a.G + rho - node * a.G, HD, j, t);
+}
+
 // --------------------------------------------------------------------------------------------------- wavefronts over tokens
-// Workgroup = (sequence, kv head, tile of 32 rows, split of the context); its wavefronts take the split's blocks in turn and merge
-// through LDS.  For few rows: what bounds it is the stream of keys and values.
+// Workgroup = tile of 32 rows, of a split; its wavefronts take the blocks in turn and merge through LDS.  For few rows: what bounds it is
+// the stream of keys and values.
 constexpr int kTreeWaves = 4;
 
 // A lane's registers hold its queries, keys, values and output: from 40 (fp8 heads of 32) to 512 of 512 (fp32 heads of 256).  Wide heads
@@ -332,35 +391,36 @@ constexpr int tree_waves_per_simd(int kind, int hd) {
 template <int KIND, int HD>
 __global__ __launch_bounds__(kTreeWaves * 64, tree_waves_per_simd(KIND, HD)) void tree_attention_kernel(TreeArgs a) {
     constexpr int DB = HD / 32, NW = kTreeWaves;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 31;
+    __shared__ uint32_t wild[3][HD], any_wild;
+    __shared__ float ml[NW][2][32];
+    __shared__ f32x4 red[NW][4][64];
+    constexpr int NL = kTreeQueriesInLds<KIND, HD> ? TreeFrag<KIND, HD>::NQ : 1;
+    __shared__ u32x4 q_lds[NL][64];
     const TreeWork w = tree_work(a, blockIdx.x);
     if (w.b >= a.c.n_seqs) return;
+    const int tile = w.group, kvh = w.kvh;
     const TreeSeq s = tree_seq(a, w.b);
-    if (32 * w.tile >= s.n * a.G) return;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const TreeBlocks range = tree_blocks(a.mask, s.ctx, s.n_tot, min((32 * w.tile + 31) / a.G, s.n - 1), w.split, a.n_splits);
-    const int rho = 32 * w.tile + (lane & 31), node = rho / a.G;
+    if (32 * tile >= s.n * a.G) return;
+    const TreeBlocks range = tree_blocks(a.mask, s.ctx, s.n_tot, min((32 * tile + 31) / a.G, s.n - 1), w.split, a.n_splits);
+    const int first = range.first, last = range.last;
+    const int rho = 32 * tile + row, node = rho / a.G;
     const bool live = node < s.n;
     const uint32_t *mask = a.mask && live ? a.mask + (size_t)(s.r0 + node) * a.mask_words : nullptr;
     TreeState<HD> st;
     st.clear();
     TreeFrag<KIND, HD> f;
     u32x4 q[TreeFrag<KIND, HD>::NQ];
-    const int32_t *table = a.c.page_table + (size_t)w.b * a.c.pages_per_seq;
-    auto page_of = [&](int blk) {
-        const int page = table[32 * blk / a.c.page_tokens];      // a block lies below n_tot, hence within the table
-        return (unsigned)page < (unsigned)a.c.n_pages ? page : -1;
-    };
-    int blk = range.first + wave, page = blk < range.last ? page_of(blk) : -1;
+    TreePages pages(a, w.b, min(first + wave, last));
+    int blk = first + wave, page = blk < last ? pages.page() : -1;
+    tree_load_q<KIND, HD>(a, s, kvh, tile, lane, q);
     if (page >= 0) {
-        f.load_k(a, cache_block(a.c, page, w.kvh), 32 * blk % a.c.page_tokens, lane);
-        if (!kTreeLateLoads<KIND, HD>) f.load_v(a, cache_block(a.c, page, w.kvh), 32 * blk % a.c.page_tokens, lane);
+        f.load_k(a, cache_block(a.c, page, kvh), pages.slot, lane);
+        if (!kTreeLateLoads<KIND, HD>) f.load_v(a, cache_block(a.c, page, kvh), pages.slot, lane);
     }
-    tree_load_q<KIND, HD>(a, s, w.kvh, w.tile, lane, q);
-    __shared__ uint32_t wild[3][HD], any_wild;
+    arrived(q);
     for (int i = threadIdx.x; i < 3 * HD; i += NW * 64) (&wild[0][0])[i] = 0u;
     if (threadIdx.x == 0) any_wild = 0u;
-    constexpr int NL = kTreeQueriesInLds<KIND, HD> ? TreeFrag<KIND, HD>::NQ : 1;
-    __shared__ u32x4 q_lds[NL][64];
     if constexpr (kTreeQueriesInLds<KIND, HD>) {
         if (wave == 0)
 #pragma unroll
@@ -371,11 +431,11 @@ __global__ __launch_bounds__(kTreeWaves * 64, tree_waves_per_simd(KIND, HD)) voi
         if constexpr (kTreeQueriesInLds<KIND, HD>) return q_lds[n][lane];
         else return q[n];
     };
-    while (blk < range.last) {
-        const int next = blk + NW;
-        const int next_page = next < range.last ? page_of(next) : -1;
-        const unsigned char *next_block = next_page >= 0 ? cache_block(a.c, next_page, w.kvh) : nullptr;
-        const int next_slot = 32 * next % a.c.page_tokens, t0 = 32 * blk;
+    while (blk < last) {
+        const int next = blk + NW, t0 = 32 * blk;
+        pages.advance(NW);
+        const int next_page = next < last ? pages.page() : -1, next_slot = pages.slot;
+        const unsigned char *next_block = next_page >= 0 ? cache_block(a.c, next_page, kvh) : nullptr;
         if (page >= 0) {
             const bool masked = t0 + 32 > s.ctx;
             uint32_t vis = 0xFFFFFFFFu;
@@ -383,14 +443,15 @@ __global__ __launch_bounds__(kTreeWaves * 64, tree_waves_per_simd(KIND, HD)) voi
             const f32x16 sc = tree_scores<KIND, HD>(f, query);
             if (kTreeLateLoads<KIND, HD>) {
                 __builtin_amdgcn_sched_barrier(0);
-                f.load_v(a, cache_block(a.c, page, w.kvh), t0 % a.c.page_tokens, lane);
+                f.load_v(a, cache_block(a.c, page, kvh), t0 % a.c.page_tokens, lane);
             } else if (next_page >= 0) f.load_k(a, next_block, next_slot, lane);
             float p[16];
             u32x4 pb[2];
             tree_softmax<KIND, HD>(f, sc, masked, vis, a.scale_log2e, st, lane, p, pb);
             if (masked && __ballot(tree_values_wild<KIND, HD>(f))) {
                 if (lane == 0) any_wild = 1;
-                tree_take_wild<KIND, HD>(f, vis, wild, lane);
+                tree_note_wild<KIND, HD>(f, vis, wild, lane);
+                tree_values_tame<KIND, HD>(f);
             }
 #pragma unroll
             for (int db = 0; db < DB; ++db) st.o[db] = tree_product<KIND, HD>(f, db, p, pb, st.o[db]);
@@ -408,9 +469,6 @@ __global__ __launch_bounds__(kTreeWaves * 64, tree_waves_per_simd(KIND, HD)) voi
     st.l += __shfl_xor(st.l, 32, 64);
 
     // merge: out = sum_w 2^(m_w - m) O_w / sum_w 2^(m_w - m) l_w, 32 dimensions at a time
-    __shared__ float ml[NW][2][32];
-    __shared__ f32x4 red[NW][4][64];
-    const int row = lane & 31;
     if (lane < 32) {
         ml[wave][0][row] = st.m;
         ml[wave][1][row] = st.l;
@@ -424,13 +482,14 @@ __global__ __launch_bounds__(kTreeWaves * 64, tree_waves_per_simd(KIND, HD)) voi
 #pragma unroll
     for (int i = 0; i < NW; ++i) denom += __builtin_amdgcn_exp2f(ml[i][0][row] - m_use) * ml[i][1][row];
     const float mine = __builtin_amdgcn_exp2f(st.m - m_use);
-    const bool split = a.n_splits > 1;
-    const size_t slot = tree_slot(a, w.b, w.kvh, w.split, w.tile);
     // (denom is NaN, and so is the row, where a score is; it is 0 where the row saw nothing)
+    const size_t slot = tree_slot(a, w.b, kvh, w.split, tile);
+    const bool split = a.n_splits > 1;
     const float norm = split ? 1.0f : denom == 0.0f ? 0.0f : 1.0f / denom;
     if (split && wave == 0 && lane < 32) {
-        a.part_ml[slot * 64 + row] = m_all;
-        a.part_ml[slot * 64 + 32 + row] = denom;
+        float *part = a.part_ml + slot * 64 + row;
+        part[0] = m_all;
+        part[32] = denom;
     }
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
@@ -442,20 +501,272 @@ __global__ __launch_bounds__(kTreeWaves * 64, tree_waves_per_simd(KIND, HD)) voi
         f32x4 t = red[0][wave][lane];      // NW == 4 quads: wavefront u adds quad u
 #pragma unroll
         for (int i = 1; i < NW; ++i) t += red[i][wave][lane];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) t[e] = norm == 0.0f ? 0.0f : t[e] * norm;
-        const int j = db * 32 + 8 * wave + 4 * (lane >> 5);
-        if (any_wild)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) t[e] = tree_add_wild<HD>(t[e], wild, row, j + e);
-        if (live && split) *reinterpret_cast<f32x4 *>(a.part_o + (slot * 32 + row) * HD + j) = t;
-        if (live && !split) tree_store<KIND>(a, (size_t)s.r0 + node, w.kvh * a.G + rho - node * a.G, HD, j, t);
+        tree_finish<KIND, HD>(a, s, kvh, slot, tile, row, db * 32 + 8 * wave + 4 * (lane >> 5), norm, any_wild, wild, t);
     }
 }
 static_assert(kTreeWaves == 4, "a wavefront adds one quad of a lane's 16 accumulators");
 
-// Joins the splits of every row: out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  A thread owns four dimensions of a row.  Rows of
-// splits without a block have m = -inf and l = 0; their (unwritten or zero) O is not read.
+// ------------------------------------------------------------------------------------------------------ wavefronts over rows
+// Workgroup = tiles of 32 rows, one a wavefront, of a split: every pair of blocks is fetched once for all of them, turned into bf16 (fp8: keys
+// times their scales; the values' scales go to the probabilities) on its way to LDS, in the layout of a bf16 page, and read from there by
+// every wavefront.  Two buffers: while one pair is worked on, the next is on its way through registers.  Bound by the softmax's arithmetic and
+// the matrix cores.
+constexpr int kTreePair = 2;     // blocks of 32 tokens between two barriers
+constexpr int tree_row_waves(int hd) { return hd <= 128 ? 8 : 4; }
+
+template <int HD> struct TreeLds {
+    u32x4 k[2][kTreePair][HD * 4], v[2][kTreePair][HD * 4];
+    float v_scale[2][kTreePair][32];
+    // infinities and NaN among the values: bit t of map[class - 1][dimension] for token t of a block; of this pair, the next one (which a wavefront
+    // ahead of the others writes) and the last one
+    uint32_t map[3][kTreePair][3][HD], mapped[3];
+    uint32_t wild[tree_row_waves(HD)][3][HD], any_wild[tree_row_waves(HD)];
+};
+
+// 8 values of dimension 32 db + lane % 32, tokens 8 (2 i + e / 4) + 4 (lane / 32) + e % 4: infinities and NaN become 0 and are noted
+template <int HD> SJD_D void tree_tame(u32x4 &x, int i, int db, int lane, uint32_t (&map)[3][HD], uint32_t &mapped) {
+    bool wild = false;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) wild |= (x[d] & 0x7F80u) == 0x7F80u || (x[d] & 0x7F800000u) == 0x7F800000u;
+    if (!wild) return;
+    mapped = 1u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int cls = value_class(bf16_to_float((bf16_t)(x[e >> 1] >> (16 * (e & 1)))));
+        if (cls == VALUE_FINITE) continue;
+        atomicOr(&map[cls - 1][db * 32 + (lane & 31)], 1u << (8 * (2 * i + (e >> 2)) + 4 * (lane >> 5) + (e & 3)));
+        x[e >> 1] &= e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+    }
+}
+
+// A thread's 16-byte pieces of a pair of blocks on their way to LDS.  A block that is not there (page < 0) becomes zeros.
+template <int KIND, int HD> struct TreeStage {
+    static constexpr int THREADS = 64 * tree_row_waves(HD), SIZE = KIND == SJD_BF16 ? 2 : 1;
+    static constexpr int BLOCK = 2 * HD * SIZE, PIECES = kTreePair * BLOCK, PER = (PIECES + THREADS - 1) / THREADS;
+    u32x4 k[PER], v[PER];
+    uint32_t ks[PER], vs;
+    SJD_D static bool has(int n) { return PIECES % THREADS == 0 || n < PIECES; }
+    SJD_D void load(const TreeArgs &a, const unsigned char *const (&block)[kTreePair], const int (&slot)[kTreePair], int tid) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int n = tid + THREADS * i, sub = n / BLOCK;
+            k[i] = v[i] = u32x4{0u, 0u, 0u, 0u};
+            ks[i] = 127u;
+            const unsigned char *p = sub ? block[1] : block[0];
+            const int at = sub ? slot[1] : slot[0];
+            if (!has(n) || !p) continue;
+            const u32x4 *kp = reinterpret_cast<const u32x4 *>(p + (size_t)at * HD * SIZE);
+            const u32x4 *vp = reinterpret_cast<const u32x4 *>(p + ((size_t)a.c.page_tokens + at) * HD * SIZE);
+            k[i] = kp[n % BLOCK];
+            v[i] = vp[n % BLOCK];
+            if (KIND == SJD_FP8) ks[i] = p[2 * (size_t)a.c.page_tokens * HD + at + (n & 31)];
+        }
+        if (KIND == SJD_FP8 && tid < 32 * kTreePair) {
+            const unsigned char *p = tid >> 5 ? block[1] : block[0];
+            vs = p ? p[(2 * (size_t)HD + 1) * a.c.page_tokens + (tid >> 5 ? slot[1] : slot[0]) + (tid & 31)] : 127u;
+        }
+    }
+    SJD_D void store(TreeLds<HD> &l, int buf, int note, bool tame, int tid) const {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int n = tid + THREADS * i, sub = n / BLOCK, r = n % BLOCK, frag = r >> 6, lane = r & 63;
+            if (!has(n)) continue;
+            if constexpr (KIND == SJD_BF16) {
+                u32x4 x = v[i];
+                if (tame) tree_tame<HD>(x, frag / (HD / 32), frag % (HD / 32), lane, l.map[note][sub], l.mapped[note]);
+                l.k[buf][sub][r] = k[i];
+                l.v[buf][sub][r] = x;
+            } else {
+                // fragment `frag` of fp8 holds the bf16 pieces 2 frag and 2 frag + 1 of keys, the halves 0 and 1 of 32 dimensions of values
+                const float s = scale_of(ks[i]);
+                l.k[buf][sub][(2 * frag) * 64 + lane] = __builtin_bit_cast(u32x4, fp8_to_bf16(k[i][0], k[i][1], s));
+                l.k[buf][sub][(2 * frag + 1) * 64 + lane] = __builtin_bit_cast(u32x4, fp8_to_bf16(k[i][2], k[i][3], s));
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    u32x4 x = __builtin_bit_cast(u32x4, fp8_to_bf16(v[i][2 * h], v[i][2 * h + 1], 1.0f));
+                    if (tame) tree_tame<HD>(x, h, frag, lane, l.map[note][sub], l.mapped[note]);
+                    l.v[buf][sub][(h * (HD / 32) + frag) * 64 + lane] = x;
+                }
+            }
+        }
+        if (KIND == SJD_FP8 && tid < 32 * kTreePair) l.v_scale[buf][tid >> 5][tid & 31] = scale_of(vs);
+    }
+};
+
+template <int KIND, int HD>
+__global__ __launch_bounds__(64 * tree_row_waves(HD), tree_row_waves(HD) / 4) void tree_attention_rows_kernel(TreeArgs a) {
+    constexpr int DB = HD / 32, NQ = HD / 16, NW = tree_row_waves(HD), THREADS = 64 * NW;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 31, tid = threadIdx.x;
+    __shared__ TreeLds<HD> l;
+    const TreeWork w = tree_work(a, blockIdx.x);
+    if (w.b >= a.c.n_seqs) return;
+    const TreeSeq s = tree_seq(a, w.b);
+    if (32 * NW * w.group >= s.n * a.G) return;
+    const int tile = w.group * NW + wave, node = (32 * tile + row) / a.G;
+    const bool live = node < s.n, busy = 32 * tile < s.n * a.G;     // (a wavefront without rows helps to fetch)
+    const uint32_t *mask = a.mask && live ? a.mask + (size_t)(s.r0 + node) * a.mask_words : nullptr;
+    const TreeBlocks range = tree_blocks(a.mask, s.ctx, s.n_tot, min((32 * NW * (w.group + 1) - 1) / a.G, s.n - 1), w.split, a.n_splits);
+    TreePages pages(a, w.b, range.first);
+    TreeState<HD> st;
+    st.clear();
+    u32x4 q[NQ];
+    tree_load_q<SJD_BF16, HD>(a, s, w.kvh, tile, lane, q);
+    TreeStage<KIND, HD> stage;
+    // asks for the pair of blocks from blk on; -> whether some row may not see all of it
+    auto fetch = [&](int blk, uint32_t (&there)[kTreePair]) {
+        const unsigned char *block[kTreePair];
+        int slot[kTreePair];
+        bool part = 32 * (blk + kTreePair) > s.ctx;
+#pragma unroll
+        for (int u = 0; u < kTreePair; ++u) {
+            const int page = blk + u < range.last ? pages.page() : -1;
+            there[u] = page >= 0;
+            block[u] = page >= 0 ? cache_block(a.c, page, w.kvh) : nullptr;
+            slot[u] = pages.slot;
+            part |= page < 0;
+            pages.advance(1);
+        }
+        stage.load(a, block, slot, tid);
+        return part;
+    };
+    for (int i = tid; i < 3 * kTreePair * 3 * HD; i += THREADS) (&l.map[0][0][0][0])[i] = 0u;
+    for (int i = tid; i < NW * 3 * HD; i += THREADS) (&l.wild[0][0][0])[i] = 0u;
+    if (tid < 3) l.mapped[tid] = 0u;
+    if (tid < NW) l.any_wild[tid] = 0u;
+    __syncthreads();
+    // blocks that are there, and whether some row may not see all of them: of the pair worked on, and of the one in registers
+    uint32_t there[kTreePair] = {0u, 0u}, next_there[kTreePair] = {0u, 0u};
+    bool part = false, next_part = false;
+    if (range.first < range.last) {
+        part = fetch(range.first, there);
+        stage.store(l, 0, 0, part, tid);
+        if (range.first + kTreePair < range.last) next_part = fetch(range.first + kTreePair, next_there);
+    }
+    arrived(q);
+    for (int blk = range.first, buf = 0, note = 0; blk < range.last; blk += kTreePair, buf ^= 1) {
+        const int next_note = note == 2 ? 0 : note + 1, last_note = note == 0 ? 2 : note - 1;
+        __syncthreads();
+        if (l.mapped[last_note]) {       // (rare; the same for all threads: nobody writes it between two barriers)
+            __syncthreads();
+            for (int i = tid; i < kTreePair * 3 * HD; i += THREADS) (&l.map[last_note][0][0][0])[i] = 0u;
+            if (tid == 0) l.mapped[last_note] = 0u;
+            __syncthreads();
+        }
+        // the next pair, asked for a whole round ago, goes to LDS, and the one after it is asked for
+        const bool store_part = next_part;
+        uint32_t store_there[kTreePair];
+#pragma unroll
+        for (int u = 0; u < kTreePair; ++u) store_there[u] = next_there[u];
+        if (blk + kTreePair < range.last) {
+            stage.store(l, buf ^ 1, next_note, store_part, tid);
+            if (blk + 2 * kTreePair < range.last) next_part = fetch(blk + 2 * kTreePair, next_there);
+        }
+        if (busy) {
+            // operands are asked for a block ahead of the products that take them: a wavefront that waits for each of its own leaves the matrix
+            // cores idle (200 us in place of XXX)
+            f32x16 sc[kTreePair];
+            u32x4 f[kTreePair][NQ];
+#pragma unroll
+            for (int u = 0; u < kTreePair; ++u)
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) f[u][n] = l.k[buf][u][n * 64 + lane];
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int u = 0; u < kTreePair; ++u) {
+#pragma unroll
+                for (int v = 0; v < 16; ++v) sc[u][v] = 0.0f;
+#pragma unroll
+                for (int n = 0; n < NQ; ++n)
+                    sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[u][n]), __builtin_bit_cast(bf16x8, q[n]), sc[u], 0, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) f[0][n] = l.v[buf][0][n * 64 + lane];
+            __builtin_amdgcn_sched_barrier(0);
+            if (part) {
+#pragma unroll
+                for (int u = 0; u < kTreePair; ++u) {
+                    const uint32_t vis = live && there[u] ? tree_visible(mask, a.mask_words, s.ctx, s.n_tot, node, 32 * (blk + u)) : 0u;
+                    const uint32_t mine = vis >> (4 * (lane >> 5));
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) sc[u][v] = mine >> (8 * (v >> 2) + (v & 3)) & 1u ? sc[u][v] : -INFINITY;
+                    if (l.mapped[note]) {
+                        if (lane == 0) l.any_wild[wave] = 1u;
+#pragma unroll 1
+                        for (int i = 0; i < 3 * HD; ++i) {
+                            const uint32_t rows = (uint32_t)__ballot(vis & (&l.map[note][u][0][0])[i]);
+                            if (lane == 0) (&l.wild[wave][0][0])[i] |= rows;
+                        }
+                    }
+                }
+            }
+            float mx = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < kTreePair; ++u)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) mx = fmaxf(mx, sc[u][v]);
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * a.scale_log2e;
+            tree_rescale<HD>(st, mx);
+            const float m_use = st.m == -INFINITY ? 0.0f : st.m;
+            float sum = 0.0f;
+#pragma unroll
+            for (int u = 0; u < kTreePair; ++u) {
+                if (u + 1 < kTreePair) {
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) f[u + 1][n] = l.v[buf][u + 1][n * 64 + lane];
+                }
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    sc[u][v] = __builtin_amdgcn_exp2f(fmaf(sc[u][v], a.scale_log2e, -m_use));
+                    sum += sc[u][v];
+                }
+                if constexpr (KIND == SJD_FP8) {           // the values' scales, exact: the product takes plain codes
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) {
+                        const f32x4 vs = *reinterpret_cast<const f32x4 *>(&l.v_scale[buf][u][8 * m + 4 * (lane >> 5)]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sc[u][4 * m + e] *= vs[e];
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    u32x4 p;
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) p[d] = pack_bf16(sc[u][8 * i + 2 * d], sc[u][8 * i + 2 * d + 1]);
+#pragma unroll
+                    for (int db = 0; db < DB; ++db)
+                        st.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[u][i * DB + db]), __builtin_bit_cast(bf16x8, p), st.o[db], 0, 0, 0);
+                }
+            }
+            st.l += sum;
+        }
+        part = store_part;
+#pragma unroll
+        for (int u = 0; u < kTreePair; ++u) there[u] = store_there[u];
+        note = next_note;
+    }
+    if (!busy) return;
+    const float sum = st.l + __shfl_xor(st.l, 32, 64);
+    const bool split = a.n_splits > 1;
+    const float norm = split ? 1.0f : sum == 0.0f ? 0.0f : 1.0f / sum;
+    const size_t slot = tree_slot(a, w.b, w.kvh, w.split, tile);
+    if (split && lane < 32) {
+        float *part_ml = a.part_ml + slot * 64 + row;
+        part_ml[0] = st.m;
+        part_ml[32] = sum;
+    }
+    const bool any = l.any_wild[wave];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            tree_finish<SJD_BF16, HD>(a, s, w.kvh, slot, tile, row, db * 32 + 8 * u + 4 * (lane >> 5), norm, any, l.wild[wave],
+                                      f32x4{st.o[db][4 * u], st.o[db][4 * u + 1], st.o[db][4 * u + 2], st.o[db][4 * u + 3]});
+}
+
+// ------------------------------------------------------------------------------------------------------------------ joining
+// Joins the splits of every row: out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  A thread owns four dimensions of a row.  Where a split
+// saw nothing of a row l = 0.
 template <int KIND>
 __global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a) {
     const int quads = a.c.hd >> 2, per = 32 * quads;
@@ -464,7 +775,7 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a) {
     const int u = (blockIdx.x % wgs) * 256 + threadIdx.x;
     const int tile = pair % a.tiles, kvh = (pair / a.tiles) % a.c.n_kv, b = pair / a.tiles / a.c.n_kv;
     if (u >= per) return;
-    const int row = u / quads, j = (u - row * quads) * 4;
+    const int row = u & 31, j = (u >> 5) * 4;
     const TreeSeq s = tree_seq(a, b);
     const int rho = 32 * tile + row, node = rho / a.G;
     if (node >= s.n) return;
@@ -480,7 +791,7 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a) {
         const size_t slot = slot0 + i * step;
         const float l = a.part_ml[slot * 64 + 32 + row];
         const float w = __builtin_amdgcn_exp2f(a.part_ml[slot * 64 + row] - m_use);
-        const f32x4 o = *reinterpret_cast<const f32x4 *>(a.part_o + (slot * 32 + row) * a.c.hd + j);
+        const f32x4 o = *reinterpret_cast<const f32x4 *>(a.part_o + slot * per * 4 + tree_part_index(row, j));
         denom += w * l;
 #pragma unroll
         for (int e = 0; e < 4; ++e) t[e] += l == 0.0f ? 0.0f : finite_f(o[e]) ? w * o[e] : o[e];   // (w may be 0: not 0 * inf)

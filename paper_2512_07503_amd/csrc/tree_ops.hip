@@ -72,20 +72,24 @@ int check_rows(const sjd_kv_cache *cache, int32_t dtype, const void *k, const vo
 }
 
 // ------------------------------------------------------------------------------------------------------------- attention
-struct TreePlan { int tiles, n_splits; size_t part_o, part_ml; };
+struct TreePlan { int tiles, groups, n_splits; bool by_rows; size_t part_o, part_ml; };
 
-// How many ways a sequence's context is split: until there are two workgroups for each of the 256 CUs, but no split with less than two
-// blocks of 32 tokens for each of a workgroup's wavefronts, on which its merge would weigh more than its share of the stream.
+// Which kernel, and how many ways a context is split.  Up to two tiles of 32 rows a kv head: wavefronts over tokens, two workgroups a CU; more:
+// wavefronts over rows, one.
 TreePlan tree_plan(const sjd_kv_cache *c, int n_heads, int max_rows, int max_ctx) {
     TreePlan p;
     const int G = n_heads / c->n_kv_heads;
     p.tiles = (int)ceil_div_sz((size_t)max_rows * G, 32);
-    const size_t pairs = (size_t)c->n_seqs * c->n_kv_heads * p.tiles;
-    const size_t blocks = ceil_div_sz((size_t)max_ctx + max_rows, 32);
+    p.by_rows = c->dtype != SJD_F32 && p.tiles > 2;
+    const int per_group = p.by_rows ? tree_row_waves(c->head_dim) : 1;
+    p.groups = ceil_div(p.tiles, per_group);
+    p.tiles = p.groups * per_group;
+    const size_t work = (size_t)c->n_seqs * c->n_kv_heads * p.groups, blocks = ceil_div_sz((size_t)max_ctx + max_rows, 32);
+    const size_t want = ceil_div_sz(p.by_rows ? 1024 : 512, work);
+    // no split with less than two blocks for each of a workgroup's wavefronts, on which its merge would weigh more than its share of the stream
     const size_t most = blocks / (2 * kTreeWaves) ? blocks / (2 * kTreeWaves) : 1;
-    const size_t want = ceil_div_sz(512, pairs);
     p.n_splits = (int)(want < most ? want : most);
-    const size_t slots = p.n_splits > 1 ? pairs * p.n_splits : 0;
+    const size_t slots = p.n_splits > 1 ? (size_t)c->n_seqs * c->n_kv_heads * p.n_splits * p.tiles : 0;
     p.part_o = slots * 32 * c->head_dim * sizeof(float);
     p.part_ml = slots * 64 * sizeof(float);
     return p;
@@ -99,17 +103,22 @@ int check_attention(const sjd_kv_cache *c, int32_t n_heads, int32_t max_rows, in
     return SJD_OK;
 }
 
-template <int KIND, int HD> void run_tree(hipStream_t st, const TreeArgs &a) {
+template <int KIND, int HD> void run_tree(hipStream_t st, const TreeArgs &a, bool by_rows) {
+    if constexpr (KIND != SJD_F32)
+        if (by_rows) {
+            tree_attention_rows_kernel<KIND, HD><<<tree_grid(a), 64 * tree_row_waves(HD), 0, st>>>(a);
+            return;
+        }
     tree_attention_kernel<KIND, HD><<<tree_grid(a), kTreeWaves * 64, 0, st>>>(a);
 }
-template <int KIND> void run_tree_kind(hipStream_t st, const TreeArgs &a) {
+template <int KIND> void run_tree_kind(hipStream_t st, const TreeArgs &a, bool by_rows) {
     switch (a.c.hd) {
-    case 32: run_tree<KIND, 32>(st, a); break;
-    case 64: run_tree<KIND, 64>(st, a); break;
-    case 96: run_tree<KIND, 96>(st, a); break;
-    case 128: run_tree<KIND, 128>(st, a); break;
-    case 192: run_tree<KIND, 192>(st, a); break;
-    default: run_tree<KIND, 256>(st, a); break;
+    case 32: run_tree<KIND, 32>(st, a, by_rows); break;
+    case 64: run_tree<KIND, 64>(st, a, by_rows); break;
+    case 96: run_tree<KIND, 96>(st, a, by_rows); break;
+    case 128: run_tree<KIND, 128>(st, a, by_rows); break;
+    case 192: run_tree<KIND, 192>(st, a, by_rows); break;
+    default: run_tree<KIND, 256>(st, a, by_rows); break;
     }
 }
 
@@ -291,16 +300,16 @@ int sjd_op_tree_attention(void *hip_stream, const sjd_kv_cache *cache, int32_t d
     a.q = q; a.out = out; a.q_stride = q_stride; a.out_stride = out_stride;
     a.row_start = row_start; a.ctx_len = ctx_len; a.mask = mask;
     a.mask_words = mask_words; a.n_rows = n_rows; a.max_rows = max_rows; a.H = n_heads; a.G = n_heads / cache->n_kv_heads;
-    a.tiles = p.tiles; a.n_splits = p.n_splits;
+    a.tiles = p.tiles; a.groups = p.groups; a.n_splits = p.n_splits;
     a.scale_log2e = (float)(1.4426950408889634 * (scale > 0.0f ? (double)scale : 1.0 / sqrt((double)cache->head_dim)));
     a.part_o = (float *)workspace;
     a.part_ml = (float *)((char *)workspace + p.part_o);
     a.q_wide = wide(q, q_stride, size, 16);
     a.out_wide = wide(out, out_stride, size, 4 * size);
     hipStream_t st = (hipStream_t)hip_stream;
-    if (cache->dtype == SJD_F32) run_tree_kind<SJD_F32>(st, a);
-    else if (cache->dtype == SJD_BF16) run_tree_kind<SJD_BF16>(st, a);
-    else run_tree_kind<SJD_FP8>(st, a);
+    if (cache->dtype == SJD_F32) run_tree_kind<SJD_F32>(st, a, p.by_rows);
+    else if (cache->dtype == SJD_BF16) run_tree_kind<SJD_BF16>(st, a, p.by_rows);
+    else run_tree_kind<SJD_FP8>(st, a, p.by_rows);
     TREE_TRY(hipGetLastError());
     if (a.n_splits > 1) {
         const unsigned grid = (unsigned)((size_t)cache->n_seqs * cache->n_kv_heads * p.tiles * ceil_div(8 * cache->head_dim, 256));
