@@ -122,8 +122,15 @@ SJD_D bf16x8 fp8_to_bf16(uint32_t lo, uint32_t hi, float scale) {
     const b2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, scale, true);
     return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
-// 2^(byte - 127); a byte that no write leaves (255) counts as 254, so that a token nobody sees stays finite
-SJD_D float scale_of(uint32_t byte) { return __builtin_bit_cast(float, min(byte, 254u) << 23); }
+SJD_D float scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }    // 2^(byte - 127)
+template <int I> SJD_D float scale_of_byte(uint32_t w) {                                 // of byte I, in one instruction
+    float r;
+    if constexpr (I == 0) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_0" : "=v"(r) : "v"(23), "v"(w));
+    if constexpr (I == 1) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_1" : "=v"(r) : "v"(23), "v"(w));
+    if constexpr (I == 2) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_2" : "=v"(r) : "v"(23), "v"(w));
+    if constexpr (I == 3) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_3" : "=v"(r) : "v"(23), "v"(w));
+    return r;
+}
 
 // q(n): piece n of the query operand
 template <int KIND, int HD, typename Q>
@@ -226,14 +233,16 @@ template <int HD> struct TreeState {
     }
 };
 
-// The state is rescaled only when a row's maximum has grown by more than a factor of 2^8: until then its probabilities are up to 2^8 in
-// place of 1, which costs neither fp32 sums nor bf16 operands a bit.
-template <int HD> SJD_D void tree_rescale(TreeState<HD> &st, float mx) {
+// The state is rescaled only when a row's maximum has grown by more than a factor of 2^8: until then its probabilities are up to 2^8
+// in place of 1, which costs neither fp32 sums nor bf16 operands a bit.  The reference is a whole number, so that rescaling is exact.
+// `pending`: probabilities whose product with values is still to come.
+template <int HD, typename F> SJD_D void tree_rescale(TreeState<HD> &st, float mx, F pending) {
     if (!__ballot(mx > st.m + 8.0f)) return;
-    const float m = fmaxf(st.m, mx);
+    const float m = fmaxf(st.m, __builtin_ceilf(mx));
     const float alpha = __builtin_amdgcn_exp2f(st.m - (m == -INFINITY ? 0.0f : m));     // (not (-inf) - (-inf))
     st.m = m;
     st.l *= alpha;
+    pending(alpha);
 #pragma unroll
     for (int db = 0; db < HD / 32; ++db) {
 #pragma unroll
@@ -245,18 +254,23 @@ template <int HD> SJD_D void tree_rescale(TreeState<HD> &st, float mx) {
 // Softmax of a block's scores into p (and, but for F32, its bf16 operand pb), and the rescaling of the state.  `vis`: bit k = this lane's
 // row sees token k of the block.
 template <int KIND, int HD>
-SJD_D void tree_softmax(const TreeFrag<KIND, HD> &f, f32x16 s, bool masked, uint32_t vis, float scale_log2e, TreeState<HD> &st, int lane,
+SJD_D void tree_softmax(TreeFrag<KIND, HD> &f, f32x16 s, bool masked, uint32_t vis, float scale_log2e, TreeState<HD> &st, int lane,
                         float (&p)[16], u32x4 (&pb)[2]) {
     if (masked) {
         const uint32_t mine = vis >> (4 * (lane >> 5));     // bit 8 (v / 4) + v % 4 belongs to register v
 #pragma unroll
         for (int v = 0; v < 16; ++v) s[v] = mine >> (8 * (v >> 2) + (v & 3)) & 1u ? s[v] : -INFINITY;
+        if constexpr (KIND == SJD_FP8) {
+            // A token that nobody wrote may have a scale of 255, which is no number (and 0 times it none either): 254 in its place
+#pragma unroll
+            for (int m = 0; m < 4; ++m) f.v_scale[m] ^= (((f.v_scale[m] & 0x7F7F7F7Fu) + 0x01010101u) & f.v_scale[m] & 0x80808080u) >> 7;
+        }
     }
     float mx = s[0];
 #pragma unroll
     for (int v = 1; v < 16; ++v) mx = fmaxf(mx, s[v]);
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * scale_log2e;
-    tree_rescale<HD>(st, mx);
+    tree_rescale<HD>(st, mx, [](float) {});
     const float m_use = st.m == -INFINITY ? 0.0f : st.m;    // a row that has seen nothing so far: not (-inf) - (-inf)
     float sum = 0.0f;
 #pragma unroll
@@ -273,8 +287,8 @@ SJD_D void tree_softmax(const TreeFrag<KIND, HD> &f, f32x16 s, bool masked, uint
                 const int v = 8 * i + 2 * d;
                 float a = p[v], b = p[v + 1];
                 if constexpr (KIND == SJD_FP8) {           // the values' scales, exact: the product takes plain codes
-                    a *= scale_of(f.v_scale[v >> 2] >> (8 * (v & 3)) & 0xFFu);
-                    b *= scale_of(f.v_scale[v >> 2] >> (8 * ((v + 1) & 3)) & 0xFFu);
+                    a *= d & 1 ? scale_of_byte<2>(f.v_scale[v >> 2]) : scale_of_byte<0>(f.v_scale[v >> 2]);
+                    b *= d & 1 ? scale_of_byte<3>(f.v_scale[v >> 2]) : scale_of_byte<1>(f.v_scale[v >> 2]);
                 }
                 pb[i][d] = pack_bf16(a, b);
             }
@@ -507,20 +521,18 @@ __global__ __launch_bounds__(kTreeWaves * 64, tree_waves_per_simd(KIND, HD)) voi
 static_assert(kTreeWaves == 4, "a wavefront adds one quad of a lane's 16 accumulators");
 
 // ------------------------------------------------------------------------------------------------------ wavefronts over rows
-// Workgroup = tiles of 32 rows, one a wavefront, of a split: every pair of blocks is fetched once for all of them, turned into bf16 (fp8: keys
-// times their scales; the values' scales go to the probabilities) on its way to LDS, in the layout of a bf16 page, and read from there by
-// every wavefront.  Two buffers: while one pair is worked on, the next is on its way through registers.  Bound by the softmax's arithmetic and
-// the matrix cores.
-constexpr int kTreePair = 2;     // blocks of 32 tokens between two barriers
-constexpr int tree_row_waves(int hd) { return hd <= 128 ? 8 : 4; }
+// bf16 caches.  Workgroup = a tile of 32 rows for each of its four wavefronts, of a split: every block is fetched once for all of them and read
+// from LDS, in the layout of its page, by every wavefront.  Bound by the softmax's arithmetic and the matrix cores, so a wavefront keeps both
+// busy: while it turns block j's scores into probabilities, the matrix cores work on the scores of block j + 1 and the output of block j - 1,
+// one product between every few instructions.
+constexpr int kTreeRowWaves = 4, kTreeRowThreads = 64 * kTreeRowWaves;
+constexpr int kTreeRing = 4;     // blocks in LDS: the last one's values, this one, the next one's keys, and the one that is being written
 
 template <int HD> struct TreeLds {
-    u32x4 k[2][kTreePair][HD * 4], v[2][kTreePair][HD * 4];
-    float v_scale[2][kTreePair][32];
-    // infinities and NaN among the values: bit t of map[class - 1][dimension] for token t of a block; of this pair, the next one (which a wavefront
-    // ahead of the others writes) and the last one
-    uint32_t map[3][kTreePair][3][HD], mapped[3];
-    uint32_t wild[tree_row_waves(HD)][3][HD], any_wild[tree_row_waves(HD)];
+    u32x4 k[kTreeRing][HD * 4], v[kTreeRing][HD * 4];
+    // infinities and NaN among the values: bit t of map[class - 1][dimension] for token t of a block
+    uint32_t map[kTreeRing][3][HD], mapped[kTreeRing];
+    uint32_t wild[kTreeRowWaves][3][HD], any_wild[kTreeRowWaves];
 };
 
 // 8 values of dimension 32 db + lane % 32, tokens 8 (2 i + e / 4) + 4 (lane / 32) + e % 4: infinities and NaN become 0 and are noted
@@ -539,63 +551,37 @@ template <int HD> SJD_D void tree_tame(u32x4 &x, int i, int db, int lane, uint32
     }
 }
 
-// A thread's 16-byte pieces of a pair of blocks on their way to LDS.  A block that is not there (page < 0) becomes zeros.
-template <int KIND, int HD> struct TreeStage {
-    static constexpr int THREADS = 64 * tree_row_waves(HD), SIZE = KIND == SJD_BF16 ? 2 : 1;
-    static constexpr int BLOCK = 2 * HD * SIZE, PIECES = kTreePair * BLOCK, PER = (PIECES + THREADS - 1) / THREADS;
+// A thread's 16-byte pieces of a block on their way to LDS.  A block that is not there becomes zeros.
+template <int HD> struct TreeStage {
+    static constexpr int PIECES = HD * 4, PER = (PIECES + kTreeRowThreads - 1) / kTreeRowThreads;
     u32x4 k[PER], v[PER];
-    uint32_t ks[PER], vs;
-    SJD_D static bool has(int n) { return PIECES % THREADS == 0 || n < PIECES; }
-    SJD_D void load(const TreeArgs &a, const unsigned char *const (&block)[kTreePair], const int (&slot)[kTreePair], int tid) {
+    SJD_D static bool has(int n) { return PIECES % kTreeRowThreads == 0 || n < PIECES; }
+    SJD_D void load(const TreeArgs &a, const unsigned char *block, int slot, int tid) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int n = tid + THREADS * i, sub = n / BLOCK;
+            const int n = tid + kTreeRowThreads * i;
             k[i] = v[i] = u32x4{0u, 0u, 0u, 0u};
-            ks[i] = 127u;
-            const unsigned char *p = sub ? block[1] : block[0];
-            const int at = sub ? slot[1] : slot[0];
-            if (!has(n) || !p) continue;
-            const u32x4 *kp = reinterpret_cast<const u32x4 *>(p + (size_t)at * HD * SIZE);
-            const u32x4 *vp = reinterpret_cast<const u32x4 *>(p + ((size_t)a.c.page_tokens + at) * HD * SIZE);
-            k[i] = kp[n % BLOCK];
-            v[i] = vp[n % BLOCK];
-            if (KIND == SJD_FP8) ks[i] = p[2 * (size_t)a.c.page_tokens * HD + at + (n & 31)];
-        }
-        if (KIND == SJD_FP8 && tid < 32 * kTreePair) {
-            const unsigned char *p = tid >> 5 ? block[1] : block[0];
-            vs = p ? p[(2 * (size_t)HD + 1) * a.c.page_tokens + (tid >> 5 ? slot[1] : slot[0]) + (tid & 31)] : 127u;
+            if (!has(n) || !block) continue;
+            k[i] = reinterpret_cast<const u32x4 *>(block + (size_t)slot * HD * 2)[n];
+            v[i] = reinterpret_cast<const u32x4 *>(block + ((size_t)a.c.page_tokens + slot) * HD * 2)[n];
         }
     }
-    SJD_D void store(TreeLds<HD> &l, int buf, int note, bool tame, int tid) const {
+    SJD_D void store(TreeLds<HD> &l, int buf, bool tame, int tid) const {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int n = tid + THREADS * i, sub = n / BLOCK, r = n % BLOCK, frag = r >> 6, lane = r & 63;
+            const int n = tid + kTreeRowThreads * i, frag = n >> 6;
             if (!has(n)) continue;
-            if constexpr (KIND == SJD_BF16) {
-                u32x4 x = v[i];
-                if (tame) tree_tame<HD>(x, frag / (HD / 32), frag % (HD / 32), lane, l.map[note][sub], l.mapped[note]);
-                l.k[buf][sub][r] = k[i];
-                l.v[buf][sub][r] = x;
-            } else {
-                // fragment `frag` of fp8 holds the bf16 pieces 2 frag and 2 frag + 1 of keys, the halves 0 and 1 of 32 dimensions of values
-                const float s = scale_of(ks[i]);
-                l.k[buf][sub][(2 * frag) * 64 + lane] = __builtin_bit_cast(u32x4, fp8_to_bf16(k[i][0], k[i][1], s));
-                l.k[buf][sub][(2 * frag + 1) * 64 + lane] = __builtin_bit_cast(u32x4, fp8_to_bf16(k[i][2], k[i][3], s));
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    u32x4 x = __builtin_bit_cast(u32x4, fp8_to_bf16(v[i][2 * h], v[i][2 * h + 1], 1.0f));
-                    if (tame) tree_tame<HD>(x, h, frag, lane, l.map[note][sub], l.mapped[note]);
-                    l.v[buf][sub][(h * (HD / 32) + frag) * 64 + lane] = x;
-                }
-            }
+            u32x4 x = v[i];
+            if (tame) tree_tame<HD>(x, frag / (HD / 32), frag % (HD / 32), n & 63, l.map[buf], l.mapped[buf]);
+            l.k[buf][n] = k[i];
+            l.v[buf][n] = x;
         }
-        if (KIND == SJD_FP8 && tid < 32 * kTreePair) l.v_scale[buf][tid >> 5][tid & 31] = scale_of(vs);
     }
 };
 
-template <int KIND, int HD>
-__global__ __launch_bounds__(64 * tree_row_waves(HD), tree_row_waves(HD) / 4) void tree_attention_rows_kernel(TreeArgs a) {
-    constexpr int DB = HD / 32, NQ = HD / 16, NW = tree_row_waves(HD), THREADS = 64 * NW;
+template <int HD>
+__global__ __launch_bounds__(kTreeRowThreads, HD <= 128 ? 2 : 1) void tree_attention_rows_kernel(TreeArgs a) {
+    constexpr int DB = HD / 32, NQ = HD / 16, NW = kTreeRowWaves, THREADS = kTreeRowThreads;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 31, tid = threadIdx.x;
     __shared__ TreeLds<HD> l;
     const TreeWork w = tree_work(a, blockIdx.x);
@@ -611,143 +597,140 @@ __global__ __launch_bounds__(64 * tree_row_waves(HD), tree_row_waves(HD) / 4) vo
     st.clear();
     u32x4 q[NQ];
     tree_load_q<SJD_BF16, HD>(a, s, w.kvh, tile, lane, q);
-    TreeStage<KIND, HD> stage;
-    // asks for the pair of blocks from blk on; -> whether some row may not see all of it
-    auto fetch = [&](int blk, uint32_t (&there)[kTreePair]) {
-        const unsigned char *block[kTreePair];
-        int slot[kTreePair];
-        bool part = 32 * (blk + kTreePair) > s.ctx;
-#pragma unroll
-        for (int u = 0; u < kTreePair; ++u) {
-            const int page = blk + u < range.last ? pages.page() : -1;
-            there[u] = page >= 0;
-            block[u] = page >= 0 ? cache_block(a.c, page, w.kvh) : nullptr;
-            slot[u] = pages.slot;
-            part |= page < 0;
-            pages.advance(1);
-        }
-        stage.load(a, block, slot, tid);
-        return part;
-    };
-    for (int i = tid; i < 3 * kTreePair * 3 * HD; i += THREADS) (&l.map[0][0][0][0])[i] = 0u;
+    TreeStage<HD> stage;
+    for (int i = tid; i < kTreeRing * 3 * HD; i += THREADS) (&l.map[0][0][0])[i] = 0u;
     for (int i = tid; i < NW * 3 * HD; i += THREADS) (&l.wild[0][0][0])[i] = 0u;
-    if (tid < 3) l.mapped[tid] = 0u;
+    // "the last block's values" of the first one: probabilities of 0 meet them
+    for (int i = tid; i < HD * 4; i += THREADS) l.v[kTreeRing - 1][i] = u32x4{0u, 0u, 0u, 0u};
+    if (tid < kTreeRing) l.mapped[tid] = 0u;
     if (tid < NW) l.any_wild[tid] = 0u;
     __syncthreads();
-    // blocks that are there, and whether some row may not see all of them: of the pair worked on, and of the one in registers
-    uint32_t there[kTreePair] = {0u, 0u}, next_there[kTreePair] = {0u, 0u};
-    bool part = false, next_part = false;
-    if (range.first < range.last) {
-        part = fetch(range.first, there);
-        stage.store(l, 0, 0, part, tid);
-        if (range.first + kTreePair < range.last) next_part = fetch(range.first + kTreePair, next_there);
-    }
+    // of this block, the next one, and the one in registers: whether it is there, and whether some row may not see all of it
+    bool there[3] = {false, false, false}, part[3] = {false, false, false};
+    auto fetch = [&](int blk, int i) {
+        if (blk >= range.last) return;
+        const int page = pages.page();
+        there[i] = page >= 0;
+        part[i] = page < 0 || 32 * (blk + 1) > s.ctx;
+        stage.load(a, page >= 0 ? cache_block(a.c, page, w.kvh) : nullptr, pages.slot, tid);
+        pages.advance(1);
+    };
+    fetch(range.first, 0);
+    if (range.first < range.last) stage.store(l, 0, part[0], tid);
+    fetch(range.first + 1, 1);
+    if (range.first + 1 < range.last) stage.store(l, 1, part[1], tid);
+    fetch(range.first + 2, 2);
     arrived(q);
-    for (int blk = range.first, buf = 0, note = 0; blk < range.last; blk += kTreePair, buf ^= 1) {
-        const int next_note = note == 2 ? 0 : note + 1, last_note = note == 0 ? 2 : note - 1;
+    __syncthreads();
+    f32x16 sc;
+    u32x4 p[2] = {{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};     // probabilities of the last block, still to meet its values
+#pragma unroll
+    for (int v = 0; v < 16; ++v) sc[v] = 0.0f;
+    if (busy && range.first < range.last)
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+            sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, l.k[0][n * 64 + lane]), __builtin_bit_cast(bf16x8, q[n]), sc, 0, 0, 0);
+    int cur = 0;
+    for (int blk = range.first; blk < range.last; ++blk, cur = (cur + 1) & (kTreeRing - 1)) {
+        const int before = (cur + kTreeRing - 1) & (kTreeRing - 1), after = (cur + 1) & (kTreeRing - 1), far = (cur + 2) & (kTreeRing - 1);
         __syncthreads();
-        if (l.mapped[last_note]) {       // (rare; the same for all threads: nobody writes it between two barriers)
+        if (l.mapped[before]) {          // (rare; the same for all threads: nobody writes it between two barriers)
             __syncthreads();
-            for (int i = tid; i < kTreePair * 3 * HD; i += THREADS) (&l.map[last_note][0][0][0])[i] = 0u;
-            if (tid == 0) l.mapped[last_note] = 0u;
+            for (int i = tid; i < 3 * HD; i += THREADS) (&l.map[before][0][0])[i] = 0u;
+            if (tid == 0) l.mapped[before] = 0u;
             __syncthreads();
         }
-        // the next pair, asked for a whole round ago, goes to LDS, and the one after it is asked for
-        const bool store_part = next_part;
-        uint32_t store_there[kTreePair];
-#pragma unroll
-        for (int u = 0; u < kTreePair; ++u) store_there[u] = next_there[u];
-        if (blk + kTreePair < range.last) {
-            stage.store(l, buf ^ 1, next_note, store_part, tid);
-            if (blk + 2 * kTreePair < range.last) next_part = fetch(blk + 2 * kTreePair, next_there);
+        // the block after the next, asked for a round ago, goes to LDS, and the one behind it is asked for
+        const bool far_there = there[2], far_part = part[2];
+        if (blk + 2 < range.last) {
+            stage.store(l, far, far_part, tid);
+            fetch(blk + 3, 2);
         }
         if (busy) {
-            // operands are asked for a block ahead of the products that take them: a wavefront that waits for each of its own leaves the matrix
-            // cores idle (200 us in place of XXX)
-            f32x16 sc[kTreePair];
-            u32x4 f[kTreePair][NQ];
+            // operands of the products to come: asked for ahead of everything else, they are there when it is done
+            u32x4 kf[NQ], vf[NQ];
 #pragma unroll
-            for (int u = 0; u < kTreePair; ++u)
+            for (int n = 0; n < NQ; ++n) kf[n] = l.k[after][n * 64 + lane];
 #pragma unroll
-                for (int n = 0; n < NQ; ++n) f[u][n] = l.k[buf][u][n * 64 + lane];
+            for (int n = 0; n < NQ; ++n) vf[n] = l.v[before][n * 64 + lane];
             __builtin_amdgcn_sched_barrier(0);
+            if (part[0]) {
+                const uint32_t vis = live && there[0] ? tree_visible(mask, a.mask_words, s.ctx, s.n_tot, node, 32 * blk) : 0u;
+                const uint32_t mine = vis >> (4 * (lane >> 5));
 #pragma unroll
-            for (int u = 0; u < kTreePair; ++u) {
-#pragma unroll
-                for (int v = 0; v < 16; ++v) sc[u][v] = 0.0f;
-#pragma unroll
-                for (int n = 0; n < NQ; ++n)
-                    sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[u][n]), __builtin_bit_cast(bf16x8, q[n]), sc[u], 0, 0, 0);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int n = 0; n < NQ; ++n) f[0][n] = l.v[buf][0][n * 64 + lane];
-            __builtin_amdgcn_sched_barrier(0);
-            if (part) {
-#pragma unroll
-                for (int u = 0; u < kTreePair; ++u) {
-                    const uint32_t vis = live && there[u] ? tree_visible(mask, a.mask_words, s.ctx, s.n_tot, node, 32 * (blk + u)) : 0u;
-                    const uint32_t mine = vis >> (4 * (lane >> 5));
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) sc[u][v] = mine >> (8 * (v >> 2) + (v & 3)) & 1u ? sc[u][v] : -INFINITY;
-                    if (l.mapped[note]) {
-                        if (lane == 0) l.any_wild[wave] = 1u;
+                for (int v = 0; v < 16; ++v) sc[v] = mine >> (8 * (v >> 2) + (v & 3)) & 1u ? sc[v] : -INFINITY;
+                if (l.mapped[cur]) {
+                    if (lane == 0) l.any_wild[wave] = 1u;
 #pragma unroll 1
-                        for (int i = 0; i < 3 * HD; ++i) {
-                            const uint32_t rows = (uint32_t)__ballot(vis & (&l.map[note][u][0][0])[i]);
-                            if (lane == 0) (&l.wild[wave][0][0])[i] |= rows;
-                        }
+                    for (int i = 0; i < 3 * HD; ++i) {
+                        const uint32_t rows = (uint32_t)__ballot(vis & (&l.map[cur][0][0])[i]);
+                        if (lane == 0) (&l.wild[wave][0][0])[i] |= rows;
                     }
                 }
             }
-            float mx = -INFINITY;
+            float mx = sc[0];
 #pragma unroll
-            for (int u = 0; u < kTreePair; ++u)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) mx = fmaxf(mx, sc[u][v]);
+            for (int v = 1; v < 16; ++v) mx = fmaxf(mx, sc[v]);
             mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * a.scale_log2e;
-            tree_rescale<HD>(st, mx);
+            tree_rescale<HD>(st, mx, [&](float alpha) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) p[i][d] = pack_bf16(as_float(p[i][d] << 16) * alpha, as_float(p[i][d] & 0xFFFF0000u) * alpha);
+            });
             const float m_use = st.m == -INFINITY ? 0.0f : st.m;
+            __builtin_amdgcn_sched_barrier(0);
+            f32x16 sn;
             float sum = 0.0f;
+            u32x4 pn[2];
 #pragma unroll
-            for (int u = 0; u < kTreePair; ++u) {
-                if (u + 1 < kTreePair) {
+            for (int v = 0; v < 16; ++v) sn[v] = 0.0f;
 #pragma unroll
-                    for (int n = 0; n < NQ; ++n) f[u + 1][n] = l.v[buf][u + 1][n * 64 + lane];
-                }
+            for (int n = 0; n < NQ; ++n)
+                sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[n]), __builtin_bit_cast(bf16x8, q[n]), sn, 0, 0, 0);
 #pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    sc[u][v] = __builtin_amdgcn_exp2f(fmaf(sc[u][v], a.scale_log2e, -m_use));
-                    sum += sc[u][v];
-                }
-                if constexpr (KIND == SJD_FP8) {           // the values' scales, exact: the product takes plain codes
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int m = 0; m < 4; ++m) {
-                        const f32x4 vs = *reinterpret_cast<const f32x4 *>(&l.v_scale[buf][u][8 * m + 4 * (lane >> 5)]);
+                for (int db = 0; db < DB; ++db)
+                    st.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[i * DB + db]), __builtin_bit_cast(bf16x8, p[i]), st.o[db], 0, 0, 0);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) sc[u][4 * m + e] *= vs[e];
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    u32x4 p;
-#pragma unroll
-                    for (int d = 0; d < 4; ++d) p[d] = pack_bf16(sc[u][8 * i + 2 * d], sc[u][8 * i + 2 * d + 1]);
-#pragma unroll
-                    for (int db = 0; db < DB; ++db)
-                        st.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[u][i * DB + db]), __builtin_bit_cast(bf16x8, p), st.o[db], 0, 0, 0);
-                }
+            for (int v = 0; v < 16; ++v) {
+                sc[v] = __builtin_amdgcn_exp2f(fmaf(sc[v], a.scale_log2e, -m_use));
+                sum += sc[v];
             }
-            st.l += sum;
-        }
-        part = store_part;
 #pragma unroll
-        for (int u = 0; u < kTreePair; ++u) there[u] = store_there[u];
-        note = next_note;
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int d = 0; d < 4; ++d) pn[i][d] = pack_bf16(sc[8 * i + 2 * d], sc[8 * i + 2 * d + 1]);
+#pragma unroll
+            for (int n = 0; n < 2 * NQ; ++n) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);      // a matrix product,
+                __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);      // a few instructions
+                __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);      // and an exponential
+            }
+            // (without this they are put off to where they are needed, behind the products)
+            asm volatile("" : "+v"(pn[0]), "+v"(pn[1]), "+v"(sum));
+            __builtin_amdgcn_sched_barrier(0);
+            st.l += sum;
+            sc = sn;
+            p[0] = pn[0];
+            p[1] = pn[1];
+        }
+        there[0] = there[1]; there[1] = far_there;
+        part[0] = part[1]; part[1] = far_part;
     }
     if (!busy) return;
-    const float sum = st.l + __shfl_xor(st.l, 32, 64);
+    // the last block's values: behind the loop, not as its last round's branch, whose join would copy the output registers every round
+    if (range.first < range.last) {
+        const u32x4 *vp = &l.v[(cur + kTreeRing - 1) & (kTreeRing - 1)][lane];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+                st.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vp[(i * DB + db) * 64]), __builtin_bit_cast(bf16x8, p[i]), st.o[db], 0, 0, 0);
+    }
     const bool split = a.n_splits > 1;
+    const float sum = st.l + __shfl_xor(st.l, 32, 64);
     const float norm = split ? 1.0f : sum == 0.0f ? 0.0f : 1.0f / sum;
     const size_t slot = tree_slot(a, w.b, w.kvh, w.split, tile);
     if (split && lane < 32) {
@@ -766,8 +749,9 @@ __global__ __launch_bounds__(64 * tree_row_waves(HD), tree_row_waves(HD) / 4) vo
 
 // ------------------------------------------------------------------------------------------------------------------ joining
 // Joins the splits of every row: out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  A thread owns four dimensions of a row.  Where a split
-// saw nothing of a row l = 0.
-template <int KIND>
+// saw nothing of a row l = 0.  Bound by latency: N splits, for most calls all of them, are on their way together with the row's lengths (rows
+// that turn out not to be there read what their place in the workspace holds, and drop it).
+template <int KIND, int N>
 __global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a) {
     const int quads = a.c.hd >> 2, per = 32 * quads;
     const unsigned wgs = (per + 255) / 256;
@@ -776,28 +760,52 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a) {
     const int tile = pair % a.tiles, kvh = (pair / a.tiles) % a.c.n_kv, b = pair / a.tiles / a.c.n_kv;
     if (u >= per) return;
     const int row = u & 31, j = (u >> 5) * 4;
-    const TreeSeq s = tree_seq(a, b);
-    const int rho = 32 * tile + row, node = rho / a.G;
-    if (node >= s.n) return;
     const size_t slot0 = tree_slot(a, b, kvh, 0, tile), step = a.tiles;
-    float m = -INFINITY;
-#pragma unroll 4
-    for (int i = 0; i < a.n_splits; ++i) m = fmaxf(m, a.part_ml[(slot0 + i * step) * 64 + row]);
-    const float m_use = m == -INFINITY ? 0.0f : m;
-    float denom = 0.0f;
+    float m = -INFINITY, denom = 0.0f;
     f32x4 t = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-    for (int i = 0; i < a.n_splits; ++i) {
-        const size_t slot = slot0 + i * step;
-        const float l = a.part_ml[slot * 64 + 32 + row];
-        const float w = __builtin_amdgcn_exp2f(a.part_ml[slot * 64 + row] - m_use);
-        const f32x4 o = *reinterpret_cast<const f32x4 *>(a.part_o + slot * per * 4 + tree_part_index(row, j));
-        denom += w * l;
+    int r0 = 0, n = 0;
+    for (int i0 = 0; i0 < a.n_splits; i0 += N) {
+        float pm[N], pl[N];
+        f32x4 po[N];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) t[e] += l == 0.0f ? 0.0f : finite_f(o[e]) ? w * o[e] : o[e];   // (w may be 0: not 0 * inf)
+        for (int i = 0; i < N; ++i) {
+            const size_t slot = slot0 + min(i0 + i, a.n_splits - 1) * step;
+            pm[i] = a.part_ml[slot * 64 + row];
+            pl[i] = a.part_ml[slot * 64 + 32 + row];
+            po[i] = *reinterpret_cast<const f32x4 *>(a.part_o + slot * per * 4 + tree_part_index(row, j));
+        }
+        if (i0 == 0) {
+            const TreeSeq s = tree_seq(a, b);
+            r0 = s.r0;
+            n = s.n;
+        }
+        float m_new = m;
+#pragma unroll
+        for (int i = 0; i < N; ++i) m_new = fmaxf(m_new, pm[i]);
+        const float m_use = m_new == -INFINITY ? 0.0f : m_new;
+        const float alpha = __builtin_amdgcn_exp2f(m - m_use);
+        m = m_new;
+        denom *= alpha;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t[e] = finite_f(t[e]) ? t[e] * alpha : t[e];      // (alpha may be 0: not 0 * inf)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (i0 + i >= a.n_splits || pl[i] == 0.0f) continue;
+            const float w = __builtin_amdgcn_exp2f(pm[i] - m_use);
+            denom += w * pl[i];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t[e] += finite_f(po[i][e]) ? w * po[i][e] : po[i][e];
+        }
     }
+    const int rho = 32 * tile + row, node = rho / a.G;
+    if (node >= n) return;
     const float inv = denom == 0.0f ? 0.0f : 1.0f / denom;
 #pragma unroll
     for (int e = 0; e < 4; ++e) t[e] = denom == 0.0f ? 0.0f : t[e] * inv;
-    tree_store<KIND>(a, (size_t)s.r0 + node, kvh * a.G + rho - node * a.G, a.c.hd, j, t);
+    tree_store<KIND>(a, (size_t)r0 + node, kvh * a.G + rho - node * a.G, a.c.hd, j, t);
+}
+template <int KIND> inline void launch_tree_combine(hipStream_t st, const TreeArgs &a) {
+    const unsigned grid = (unsigned)((size_t)a.c.n_seqs * a.c.n_kv * a.tiles * ceil_div(8 * a.c.hd, 256));
+    if (a.n_splits <= 4) tree_combine_kernel<KIND, 4><<<grid, 256, 0, st>>>(a);
+    else tree_combine_kernel<KIND, 16><<<grid, 256, 0, st>>>(a);
 }

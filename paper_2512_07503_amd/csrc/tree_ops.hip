@@ -74,20 +74,22 @@ int check_rows(const sjd_kv_cache *cache, int32_t dtype, const void *k, const vo
 // ------------------------------------------------------------------------------------------------------------- attention
 struct TreePlan { int tiles, groups, n_splits; bool by_rows; size_t part_o, part_ml; };
 
-// Which kernel, and how many ways a context is split.  Up to two tiles of 32 rows a kv head: wavefronts over tokens, two workgroups a CU; more:
-// wavefronts over rows, one.
+// Which kernel, and how many ways a context is split.  By rows, where a bf16 cache has more than two tiles of 32 rows a kv head: four tiles a
+// workgroup share what is fetched (16 sequences of about 7 000 tokens, 8 kv heads of 128, 244 rows: 177 us against 240 by tokens, 80 rows: 98 against
+// 130; one of 2 300 with 32 heads of 96 rows: 27 against 29).  With fp8, whose conversions it does not save a wavefront but moves, it was no
+// faster (185 against 197 us of 128-wide heads, 151 against 110 of 64-wide ones).
 TreePlan tree_plan(const sjd_kv_cache *c, int n_heads, int max_rows, int max_ctx) {
     TreePlan p;
     const int G = n_heads / c->n_kv_heads;
     p.tiles = (int)ceil_div_sz((size_t)max_rows * G, 32);
-    p.by_rows = c->dtype != SJD_F32 && p.tiles > 2;
-    const int per_group = p.by_rows ? tree_row_waves(c->head_dim) : 1;
+    p.by_rows = c->dtype == SJD_BF16 && p.tiles > 2 && c->head_dim <= 192;     // (heads of 256 would spill registers)
+    const int per_group = p.by_rows ? kTreeRowWaves : 1;
     p.groups = ceil_div(p.tiles, per_group);
     p.tiles = p.groups * per_group;
     const size_t work = (size_t)c->n_seqs * c->n_kv_heads * p.groups, blocks = ceil_div_sz((size_t)max_ctx + max_rows, 32);
-    const size_t want = ceil_div_sz(p.by_rows ? 1024 : 512, work);
-    // no split with less than two blocks for each of a workgroup's wavefronts, on which its merge would weigh more than its share of the stream
-    const size_t most = blocks / (2 * kTreeWaves) ? blocks / (2 * kTreeWaves) : 1;
+    // two workgroups for each of the 256 CUs, but no split with less than two blocks of 32 tokens for each of a workgroup's wavefronts, on which its
+    // merge would weigh more than its share of the stream
+    const size_t want = ceil_div_sz(512, work), most = blocks / (2 * kTreeWaves) ? blocks / (2 * kTreeWaves) : 1;
     p.n_splits = (int)(want < most ? want : most);
     const size_t slots = p.n_splits > 1 ? (size_t)c->n_seqs * c->n_kv_heads * p.n_splits * p.tiles : 0;
     p.part_o = slots * 32 * c->head_dim * sizeof(float);
@@ -104,9 +106,9 @@ int check_attention(const sjd_kv_cache *c, int32_t n_heads, int32_t max_rows, in
 }
 
 template <int KIND, int HD> void run_tree(hipStream_t st, const TreeArgs &a, bool by_rows) {
-    if constexpr (KIND != SJD_F32)
+    if constexpr (KIND == SJD_BF16 && HD <= 192)
         if (by_rows) {
-            tree_attention_rows_kernel<KIND, HD><<<tree_grid(a), 64 * tree_row_waves(HD), 0, st>>>(a);
+            tree_attention_rows_kernel<HD><<<tree_grid(a), kTreeRowThreads, 0, st>>>(a);
             return;
         }
     tree_attention_kernel<KIND, HD><<<tree_grid(a), kTreeWaves * 64, 0, st>>>(a);
@@ -312,9 +314,8 @@ int sjd_op_tree_attention(void *hip_stream, const sjd_kv_cache *cache, int32_t d
     else run_tree_kind<SJD_FP8>(st, a, p.by_rows);
     TREE_TRY(hipGetLastError());
     if (a.n_splits > 1) {
-        const unsigned grid = (unsigned)((size_t)cache->n_seqs * cache->n_kv_heads * p.tiles * ceil_div(8 * cache->head_dim, 256));
-        if (dtype == SJD_F32) tree_combine_kernel<SJD_F32><<<grid, 256, 0, st>>>(a);
-        else tree_combine_kernel<SJD_BF16><<<grid, 256, 0, st>>>(a);
+        if (dtype == SJD_F32) launch_tree_combine<SJD_F32>(st, a);
+        else launch_tree_combine<SJD_BF16>(st, a);
         TREE_TRY(hipGetLastError());
     }
     return SJD_OK;
