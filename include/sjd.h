@@ -422,8 +422,8 @@ int sjd_op_tree_attention(void *hip_stream, const sjd_kv_cache *cache, int32_t d
  * S_{k+1} = sum rho_{k+1}.  Where no child is accepted, or max_path nodes are reached, next_token is drawn from the last rho
  * (from p, where that is all 0): the first id whose cumulated weight exceeds the share draw_words[b] / 2^64 of all.  In distribution the
  * accepted tokens and the next one are what the target alone would have produced.  All of it is specified bit for bit: double
- * precision, the products in the order (r q) S and S q, sums of trunc(min(rho, 1) 2^44); p and q that are NaN count as 0 where they
- * are tested or drawn.  A token outside [0, vocab) is rejected.
+ * precision, the products in the order (r q) S and S q, sums of trunc(min(rho, 1) 2^44); a p that is negative or NaN is 0, and so is rho
+ * from the rejection on that a NaN of q takes part in.  A token outside [0, vocab) is rejected.
  * Outputs: path [n_seqs][max_path], the nodes reached, node 0 first, -1 behind them; path_len [n_seqs] (accepted drafts + 1; 0 for a
  * sequence without rows); next_token [n_seqs] (-1 without rows, or where p is all 0).  path and path_len are what
  * sjd_op_cache_compact takes.  max_rows <= 1024, vocab <= 524288; rows of a tree behind max_rows are ignored.  The workspace

@@ -48,12 +48,14 @@ SJD_D void tree_rows(const VerifyArgs &a, int b, int &r0, int &n) {
     r0 = rows_first(a.row_start, b, a.n_rows);
     n = min(rows_count(a.row_start, b, a.n_rows), a.max_rows);
 }
-SJD_D double positive(double x) { return x > 0.0 ? x : 0.0; }                  // NaN -> 0
-SJD_D double weight(double y) { return __builtin_trunc((y < 1.0 ? y : 1.0) * 0x1p44); }
-// rho after `m` rejections
-SJD_D double residual(double p, double q, const double *mass, int m) {
-    double r = positive(p);
-    for (int k = 0; k < m; ++k) r = positive(r - mass[k] * q);
+// p of an id as rho_0: NaN and negatives are 0
+SJD_D float target(float p) { return fmaxf(p, 0.0f); }
+SJD_D double positive(double x) { return fmax(x, 0.0); }                       // (NaN -> 0)
+SJD_D double weight(double y) { return __builtin_trunc(fmin(y, 1.0) * 0x1p44); }
+// rho after `m` >= 1 rejections (S_0 = 1)
+SJD_D double residual(float p, float q, const double *mass, int m) {
+    double r = positive((double)target(p) - (double)q);
+    for (int k = 1; k < m; ++k) r = positive(r - mass[k] * (double)q);
     return r;
 }
 SJD_D bool accepts(uint32_t word, double q, double mass, double rho) {
@@ -86,13 +88,12 @@ SJD_D bool first_accepted(const VerifyArgs &a, int r0, int node, int child) {
     if (!known(a, x)) return false;
     const size_t row = (size_t)(r0 + node);
     const double q = a.q ? (double)a.q[row * a.q_stride + x] : 1.0;
-    return accepts(a.accept_words[r0 + child], q, 1.0, positive((double)a.p[row * a.p_stride + x]));
+    return accepts(a.accept_words[r0 + child], q, 1.0, (double)target(a.p[row * a.p_stride + x]));
 }
 
-// f(id, p, q) for every id of a row, a thread's ids in ascending order; 4 ids at a time
-template <int THREADS, typename F> SJD_D void for_row(const VerifyArgs &a, const float *p, const float *q, int lo, int hi, F f) {
+// f(id, p, q) for every id of a row, 4 ids at a time, U times 4 of them on their way (one round trip to memory for all)
+template <int THREADS, int U, typename F> SJD_D void for_row(const VerifyArgs &a, const float *p, const float *q, int lo, int hi, F f) {
     if (a.wide) {
-        constexpr int U = 4;
         for (int v0 = lo + 4 * threadIdx.x; v0 < hi; v0 += 4 * THREADS * U) {
             float4 pv[U], qv[U];
 #pragma unroll
@@ -115,12 +116,41 @@ template <int THREADS, typename F> SJD_D void for_row(const VerifyArgs &a, const
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int v = v0 + 4 * THREADS * u;
+                if (v >= hi) continue;
                 f(v, pv[u].x, qv[u].x); f(v + 1, pv[u].y, qv[u].y); f(v + 2, pv[u].z, qv[u].z); f(v + 3, pv[u].w, qv[u].w);
             }
         }
     } else {
         for (int v = lo + threadIdx.x; v < hi; v += THREADS) f(v, p[v], q ? q[v] : 0.0f);
     }
+}
+
+// A thread's share of sum_v w(rho_m(v)): of integers, at most 512 of up to 2^44, exact in a double.  The first few rejections, which is what nodes
+// have, without a loop per id (16 trees of 61 nodes over 65 536 ids: 36.7 us in place of 45.9 with one).
+template <int M> SJD_D double row_mass_of(const VerifyArgs &a, const float *p, const float *q, const double *mass) {
+    double s[M > 1 ? M : 1], sum = 0.0;
+#pragma unroll
+    for (int k = 1; k < M; ++k) s[k] = mass[k];
+    for_row<kNodeThreads, 8>(a, p, q, 0, a.V, [&](int, float pv, float qv) {
+        double r = (double)target(pv);
+        if (M > 0) r = positive(r - (double)qv);
+#pragma unroll
+        for (int k = 1; k < M; ++k) r = positive(r - s[k] * (double)qv);
+        sum += weight(r);
+    });
+    return sum;
+}
+SJD_D double row_mass(const VerifyArgs &a, const float *p, const float *q, const double *mass, int m) {
+    switch (m) {
+    case 0: return row_mass_of<0>(a, p, q, mass);
+    case 1: return row_mass_of<1>(a, p, q, mass);
+    case 2: return row_mass_of<2>(a, p, q, mass);
+    case 3: return row_mass_of<3>(a, p, q, mass);
+    case 4: return row_mass_of<4>(a, p, q, mass);
+    }
+    double sum = 0.0;
+    for_row<kNodeThreads, 8>(a, p, q, 0, a.V, [&](int, float pv, float qv) { sum += weight(residual(pv, qv, mass, m)); });
+    return sum;
 }
 
 // Workgroup = node of a tree: which of its children is accepted
@@ -130,6 +160,9 @@ __global__ __launch_bounds__(kNodeThreads) void verify_nodes_kernel(VerifyArgs a
     tree_rows(a, b, r0, n);
     if (node >= n) return;
     __shared__ int parent[kMaxNodes], first[kMaxNodes], child[kMaxNodes], wave_count[kNodeThreads / 64], flag;
+    __shared__ int token[kMaxNodes];            // of the children: tokens (-1: outside the vocabulary), test words, p and q of the tokens
+    __shared__ uint32_t word[kMaxNodes];
+    __shared__ float token_p[kMaxNodes], token_q[kMaxNodes];
     __shared__ double mass[kMaxNodes];
     __shared__ uint64_t scratch[kNodeThreads / 64];
     const int mine = tid < n ? a.parents[r0 + tid] : -1;
@@ -151,12 +184,21 @@ __global__ __launch_bounds__(kNodeThreads) void verify_nodes_kernel(VerifyArgs a
         if (tid == 0) *out = -1;
         return;
     }
-    if (tid == 0) flag = first_accepted(a, r0, node, child[0]);
+    const float *p = a.p + (size_t)(r0 + node) * a.p_stride, *q = a.q ? a.q + (size_t)(r0 + node) * a.q_stride : nullptr;
+    // everything that the tests take, of all children at once: two round trips to memory here in place of two a test
+    if (tid < m) {
+        const int x = a.tokens[r0 + child[tid]];
+        word[tid] = a.accept_words[r0 + child[tid]];
+        token[tid] = known(a, x) ? x : -1;
+        token_p[tid] = known(a, x) ? target(p[x]) : 0.0f;
+        token_q[tid] = known(a, x) && q ? q[x] : 1.0f;
+    }
     parent[tid] = tid < n && mine >= 0 && mine < tid ? mine : -1;
     first[tid] = kMaxNodes;
     __syncthreads();
-    if (flag || m == 1) {
-        if (tid == 0) *out = flag ? child[0] : -1;
+    const bool first_fits = token[0] >= 0 && accepts(word[0], (double)token_q[0], 1.0, (double)token_p[0]);
+    if (first_fits || m == 1) {
+        if (tid == 0) *out = first_fits ? child[0] : -1;
         return;
     }
     // Is the node ruled out: on the way up, a first child that is rejected, or another one whose first sibling is accepted
@@ -175,27 +217,23 @@ __global__ __launch_bounds__(kNodeThreads) void verify_nodes_kernel(VerifyArgs a
         if (tid == 0) *out = -1;
         return;
     }
-    const float *p = a.p + (size_t)(r0 + node) * a.p_stride, *q = a.q ? a.q + (size_t)(r0 + node) * a.q_stride : nullptr;
     if (tid == 0) mass[0] = 1.0;
     int accepted = -1;
     uint64_t all = 0;                    // without q: sum of the weights of p
     for (int k = 1; k < m; ++k) {
         __syncthreads();
-        double sum = 0.0;                // of integers, at most 512 of up to 2^44: exact
-        uint64_t total;
         if (q || k == 1) {
-            for_row<kNodeThreads>(a, p, q, 0, a.V, [&](int, float pv, float qv) { sum += weight(q ? residual(pv, qv, mass, k) : positive((double)pv)); });
-            total = block_sum<kNodeThreads / 64>((uint64_t)sum, scratch);
-            all = total;
+            all = block_sum<kNodeThreads / 64>((uint64_t)row_mass(a, p, q, mass, q ? k : 0), scratch);
         }
+        uint64_t total = all;
+        bool gone = false;               // without q: this child's token is a rejected one's
         if (!q) {
             // off comes the weight of every distinct token rejected so far
-            total = all;
             for (int i = 0; i < k; ++i) {
-                const int x = a.tokens[r0 + child[i]];
-                bool again = !known(a, x);
-                for (int j = 0; j < i && !again; ++j) again = a.tokens[r0 + child[j]] == x;
-                if (!again) total -= (uint64_t)weight(positive((double)p[x]));
+                bool again = token[i] < 0;
+                for (int j = 0; j < i && !again; ++j) again = token[j] == token[i];
+                if (!again) total -= (uint64_t)weight((double)token_p[i]);
+                gone |= token[i] == token[k];
             }
         }
         const double s = (double)total * 0x1p-44;
@@ -204,29 +242,34 @@ __global__ __launch_bounds__(kNodeThreads) void verify_nodes_kernel(VerifyArgs a
             a.mass[r0 + child[k - 1]] = s;
         }
         __syncthreads();
-        const int x = a.tokens[r0 + child[k]];
-        if (known(a, x)) {
-            double rho;
-            if (q) rho = residual(p[x], q[x], mass, k);
-            else {
-                rho = positive((double)p[x]);
-                for (int i = 0; i < k; ++i) if (a.tokens[r0 + child[i]] == x) rho = 0.0;
-            }
-            if (accepts(a.accept_words[r0 + child[k]], q ? (double)q[x] : 1.0, s, rho)) { accepted = child[k]; break; }
-        }
+        if (token[k] < 0) continue;
+        const double rho = q ? residual(token_p[k], token_q[k], mass, k) : gone ? 0.0 : (double)token_p[k];
+        if (accepts(word[k], (double)token_q[k], s, rho)) { accepted = child[k]; break; }
     }
     if (tid == 0) *out = accepted;
 }
 
-// Workgroup = slice of the last accepted node's rows: walks the path, sums the slice's weights; slice 0 writes the path
+// rho of an id after m rejections: of drawn children by their masses, of chosen ones by their tokens
+SJD_D double last_rho(int v, float p, float q, bool drawn, const double *mass, const int *token, int m) {
+    if (drawn && m) return residual(p, q, mass, m);
+    double r = (double)target(p);
+    for (int k = 0; k < m && !drawn; ++k) if (token[k] == v) r = 0.0;
+    return r;
+}
+
+// Workgroup = slice of the last accepted node's rows: walks the path (slice 0 writes it) and sums the slice's weights.  (The draw is a launch of its
+// own: done by the last of a sequence's slices behind a device-wide fence it took 23.8 us in place of 17.9 for 16 sequences.)
 __global__ __launch_bounds__(256) void verify_walk_kernel(VerifyArgs a) {
-    const int b = blockIdx.y, slice = blockIdx.x, tid = threadIdx.x;
+    const int b = blockIdx.y, slice = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int r0, n;
     tree_rows(a, b, r0, n);
-    __shared__ int choice[kMaxNodes], child[kMaxNodes], way[2], wave_count[4];
+    __shared__ int choice[kMaxNodes], parent[kMaxNodes], child[kMaxNodes], way, wave_count[4];
     __shared__ double mass[kMaxNodes];
     __shared__ uint64_t scratch[4];
-    for (int i = tid; i < n; i += 256) choice[i] = a.choice[r0 + i];
+    for (int i = tid; i < n; i += 256) {
+        choice[i] = a.choice[r0 + i];
+        parent[i] = a.parents[r0 + i];
+    }
     if (slice == 0) for (int i = tid; i < a.max_path; i += 256) a.path[(size_t)b * a.max_path + i] = -1;
     __syncthreads();
     if (tid == 0) {
@@ -237,20 +280,18 @@ __global__ __launch_bounds__(256) void verify_walk_kernel(VerifyArgs a) {
             if (slice == 0) a.path[(size_t)b * a.max_path + len] = at;
             ++len;
         }
-        way[0] = at;
-        way[1] = len;
+        way = at;
         if (slice == 0) a.path_len[b] = len;
     }
     __syncthreads();
-    const int at = way[0];
+    const int at = way;
     // its rejected children: all of them, unless it is the path's length that ended the walk
     int m = 0;
     if (at >= 0 && choice[at] <= at)
         for (int j0 = at + 1; j0 < n; j0 += 256) {
             const int j = j0 + tid;
-            const bool is_child = j < n && a.parents[r0 + j] == at;
+            const bool is_child = j < n && parent[j] == at;
             const unsigned long long here = __ballot(is_child);
-            const int lane = tid & 63, wave = tid >> 6;
             if (lane == 0) wave_count[wave] = __popcll(here);
             __syncthreads();
             int before = m;
@@ -261,64 +302,61 @@ __global__ __launch_bounds__(256) void verify_walk_kernel(VerifyArgs a) {
             if (is_child) child[before + __popcll(here & ((1ull << lane) - 1ull))] = j;
             __syncthreads();
         }
-    for (int k = tid; k < m; k += 256) mass[k] = k ? a.mass[r0 + child[k - 1]] : 1.0;
+    for (int k = tid; k < m; k += 256) mass[k] = k && a.q ? a.mass[r0 + child[k - 1]] : 1.0;
     __syncthreads();
-    if (slice == 0) {
-        if (tid == 0) { a.stop[2 * b] = at >= 0 ? r0 + at : -1; a.stop[2 * b + 1] = m; }
-        for (int k = tid; k < m; k += 256) {
+    for (int k = tid; k < m; k += 256) {
+        child[k] = a.tokens[r0 + child[k]];     // from here on: their tokens
+        if (slice == 0) {
             a.stop_mass[r0 + k] = mass[k];
-            a.stop_token[r0 + k] = a.tokens[r0 + child[k]];
+            a.stop_token[r0 + k] = child[k];
         }
     }
+    if (slice == 0 && tid == 0) { a.stop[2 * b] = at >= 0 ? r0 + at : -1; a.stop[2 * b + 1] = m; }
     if (at < 0) return;
+    __syncthreads();
     const float *p = a.p + (size_t)(r0 + at) * a.p_stride, *q = a.q ? a.q + (size_t)(r0 + at) * a.q_stride : nullptr;
     const int lo = slice * kSlice, hi = min(lo + kSlice, a.V);
-    uint64_t sum = 0, plain = 0;
-    for_row<256>(a, p, q, lo, hi, [&](int v, float pv, float qv) {
-        double r = positive((double)pv);
-        plain += (uint64_t)weight(r);
-        if (q) r = residual(pv, qv, mass, m);
-        else for (int k = 0; k < m; ++k) if (a.tokens[r0 + child[k]] == v) r = 0.0;
-        sum += (uint64_t)weight(r);
+    double sum = 0.0, plain = 0.0;              // of integers, 8 of up to 2^44 a thread: exact
+    for_row<256, kSlice / 1024>(a, p, q, lo, hi, [&](int v, float pv, float qv) {
+        plain += weight((double)target(pv));
+        sum += weight(last_rho(v, pv, qv, q != nullptr, mass, child, m));
     });
-    sum = block_sum<4>(sum, scratch);
-    plain = block_sum<4>(plain, scratch);
+    const uint64_t total = block_sum<4>((uint64_t)sum, scratch), total_plain = block_sum<4>((uint64_t)plain, scratch);
     if (tid == 0) {
         uint64_t *part = a.part + ((size_t)b * a.n_slices + slice) * 2;
-        part[0] = sum;
-        part[1] = plain;
+        part[0] = total;
+        part[1] = total_plain;
     }
 }
 
 // Workgroup = sequence: the next token
 __global__ __launch_bounds__(256) void verify_draw_kernel(VerifyArgs a) {
-    const int b = blockIdx.x, tid = threadIdx.x;
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    // n_slices <= 256: a thread per slice (asked for along with the row; of a sequence without rows it is not looked at)
+    const uint64_t *part = a.part + (size_t)b * a.n_slices * 2;
+    uint64_t mine = tid < a.n_slices ? part[2 * tid] : 0;
+    const uint64_t mine_plain = tid < a.n_slices ? part[2 * tid + 1] : 0, word = a.draw_words[b];
     const int row = a.stop[2 * b];
+    int m = a.stop[2 * b + 1], r0, n;
+    tree_rows(a, b, r0, n);
     if (row < 0) {
         if (tid == 0) a.next_token[b] = -1;
         return;
     }
-    __shared__ uint64_t scratch[4], start[2];
-    __shared__ int found[2];
-    int r0, n;
-    tree_rows(a, b, r0, n);
-    int m = a.stop[2 * b + 1];
-    // n_slices <= 256: a thread per slice
-    const uint64_t *part = a.part + (size_t)b * a.n_slices * 2;
-    uint64_t mine = tid < a.n_slices ? part[2 * tid] : 0;
+    __shared__ uint64_t scratch[4], start;
+    __shared__ int found;
     uint64_t Z = block_sum<4>(mine, scratch);
     if (Z == 0) {                                   // nothing is left: from p
         m = 0;
-        mine = tid < a.n_slices ? part[2 * tid + 1] : 0;
+        mine = mine_plain;
         Z = block_sum<4>(mine, scratch);
     }
     if (Z == 0) {
         if (tid == 0) a.next_token[b] = -1;
         return;
     }
-    const uint64_t t = __umul64hi(a.draw_words[b], Z);
+    const uint64_t t = __umul64hi(word, Z);
     auto upto = [&](uint64_t v) {                   // inclusive prefix sum over the workgroup
-        const int lane = tid & 63, wave = tid >> 6;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
             const uint32_t l = __shfl_up((uint32_t)v, d, 64), h = __shfl_up((uint32_t)(v >> 32), d, 64);
@@ -331,26 +369,25 @@ __global__ __launch_bounds__(256) void verify_draw_kernel(VerifyArgs a) {
         return v;
     };
     const uint64_t s = upto(mine);
-    if (s > t && s - mine <= t) { found[0] = tid; start[0] = s - mine; }
+    if (s > t && s - mine <= t) { found = tid; start = s - mine; }
     __syncthreads();
     // within the slice: a thread owns 8 consecutive ids
     constexpr int PER = kSlice / 256;
-    const int v0 = found[0] * kSlice + tid * PER;
+    const int v0 = found * kSlice + tid * PER;
     const float *p = a.p + (size_t)row * a.p_stride, *q = a.q ? a.q + (size_t)row * a.q_stride : nullptr;
+    float pv[PER], qv[PER];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        pv[e] = v0 + e < a.V ? p[v0 + e] : 0.0f;
+        qv[e] = v0 + e < a.V && q ? q[v0 + e] : 0.0f;
+    }
     uint64_t w[PER], own = 0;
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
-        const int v = v0 + e;
-        w[e] = 0;
-        if (v < a.V) {
-            double r = positive((double)p[v]);
-            if (q) r = residual(p[v], q[v], a.stop_mass + r0, m);
-            else for (int k = 0; k < m; ++k) if (a.stop_token[r0 + k] == v) r = 0.0;
-            w[e] = (uint64_t)weight(r);
-        }
+        w[e] = v0 + e < a.V ? (uint64_t)weight(last_rho(v0 + e, pv[e], qv[e], q != nullptr, a.stop_mass + r0, a.stop_token + r0, m)) : 0;
         own += w[e];
     }
-    uint64_t c = start[0] + upto(own) - own;
+    uint64_t c = start + upto(own) - own;
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
         if (c <= t && c + w[e] > t) a.next_token[b] = v0 + e;
@@ -371,7 +408,7 @@ int check_sizes(int32_t n_rows, int32_t n_seqs, int32_t vocab) {
     return SJD_OK;
 }
 size_t up16(size_t b) { return (b + 15) / 16 * 16; }
-// parts of the workspace: mass, stop_mass, part, choice, stop_token, stop
+// parts of the workspace
 size_t workspace(VerifyArgs &a, char *base) {
     size_t at = 0;
     auto take = [&](size_t bytes) { char *p = base ? base + at : nullptr; at += up16(bytes); return (void *)p; };
