@@ -74,6 +74,37 @@ def test_write_and_read_ragged_rows(kind, dtype, Hkv, hd, page):
             assert same(got[side], tree_oracle.bf16_store(w) if out == torch.bfloat16 else w), (side, out)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("Hkv,hd", [(9, 32), (5, 64), (3, 96), (5, 128), (2, 192), (2, 256)])
+def test_write_and_read_of_many_sequences(kind, dtype, Hkv, hd):
+    """Enough tiles that a workgroup takes several heads (and a last one fewer), some of whose elements are no numbers; rows aligned and not."""
+    import paper_2512_07503_amd as sjd
+    import torch
+    rng = np.random.default_rng(hd + len(kind))
+    seqs = 2100 // Hkv
+    n = rng.integers(0, 5, seqs)
+    n[::50] = rng.integers(30, 100, len(n[::50]))
+    n[:3] = 64, 32, 33
+    first = rng.integers(0, 70, seqs)
+    first[:3] = 0, 32, 31
+    total = int(n.sum())
+    starts = np.concatenate([[0], np.cumsum(n)])
+    tiles = np.where(n > 0, (first + n - 1) // 32 - first // 32 + 1, 0).sum()
+    bound = min((total + 30 * min(seqs, total)) // 32 + min(seqs, total), total)
+    assert tiles <= bound and 2 * bound * Hkv >= 4096
+    cache, _ = make(kind, 64, Hkv, hd, first + n)
+    k, v = (rows(rng, total, 1, Hkv * hd + 1, dtype)[:, 0] for _ in range(2))
+    k, v = k[:, :Hkv * hd].contiguous().unflatten(1, (Hkv, hd)), v[:, 1:].unflatten(1, (Hkv, hd))
+    bad = torch.tensor([float("nan"), float("inf"), -float("inf")], device="cuda").to(k.dtype)
+    k[5, Hkv - 1, 3:6] = bad
+    v[7, 0, hd - 3:] = bad
+    sjd.op_cache_write(cache, k, v, i32(starts), i32(first))
+    got = sjd.op_cache_read(cache, i32(starts), i32(first), total, dtype=torch.float32)
+    for g, x in zip(got, (k, v)):
+        assert same(g, tree_oracle.store(kind, host(x)))
+
+
 def test_fp8_codes_at_their_edges():
     """Halfway cases, smallest codes, powers of two around the scale's steps, zeros, the largest floats, infinities and NaN."""
     import paper_2512_07503_amd as sjd
