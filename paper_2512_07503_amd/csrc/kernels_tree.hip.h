@@ -251,6 +251,12 @@ template <int HD, typename F> SJD_D void tree_rescale(TreeState<HD> &st, float m
     }
 }
 
+// sum + the two bf16 numbers of a pair, in fp32: what the products take is what the sums add, so that the weights of a row add up to 1 whatever their
+// rounding (a row that sees one token gives its value, exactly), and one instruction where two additions of unrounded numbers were.
+SJD_D float tree_add_pair(float sum, uint32_t pair) {
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(cache_bf16x2, pair), __builtin_bit_cast(cache_bf16x2, 0x3F803F80u), sum, false);
+}
+
 // Softmax of a block's scores into p (and, but for F32, its bf16 operand pb), and the rescaling of the state.  `vis`: bit k = this lane's
 // row sees token k of the block.
 template <int KIND, int HD>
@@ -276,9 +282,8 @@ SJD_D void tree_softmax(TreeFrag<KIND, HD> &f, f32x16 s, bool masked, uint32_t v
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
         p[v] = __builtin_amdgcn_exp2f(fmaf(s[v], scale_log2e, -m_use));
-        sum += p[v];
+        if (KIND == SJD_F32) sum += p[v];
     }
-    st.l += sum;
     if constexpr (KIND != SJD_F32) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -286,6 +291,7 @@ SJD_D void tree_softmax(TreeFrag<KIND, HD> &f, f32x16 s, bool masked, uint32_t v
             for (int d = 0; d < 4; ++d) {
                 const int v = 8 * i + 2 * d;
                 float a = p[v], b = p[v + 1];
+                sum = tree_add_pair(sum, pack_bf16(a, b));
                 if constexpr (KIND == SJD_FP8) {           // the values' scales, exact: the product takes plain codes
                     a *= d & 1 ? scale_of_byte<2>(f.v_scale[v >> 2]) : scale_of_byte<0>(f.v_scale[v >> 2]);
                     b *= d & 1 ? scale_of_byte<3>(f.v_scale[v >> 2]) : scale_of_byte<1>(f.v_scale[v >> 2]);
@@ -293,6 +299,7 @@ SJD_D void tree_softmax(TreeFrag<KIND, HD> &f, f32x16 s, bool masked, uint32_t v
                 pb[i][d] = pack_bf16(a, b);
             }
     }
+    st.l += sum;
 }
 
 // Values some of which are infinite or NaN, of tokens that not every row sees: in O += V P their 0 * inf would reach the rows that do
@@ -694,14 +701,14 @@ __global__ __launch_bounds__(kTreeRowThreads, HD <= 128 ? 2 : 1) void tree_atten
                 for (int db = 0; db < DB; ++db)
                     st.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[i * DB + db]), __builtin_bit_cast(bf16x8, p[i]), st.o[db], 0, 0, 0);
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                sc[v] = __builtin_amdgcn_exp2f(fmaf(sc[v], a.scale_log2e, -m_use));
-                sum += sc[v];
-            }
+            for (int v = 0; v < 16; ++v) sc[v] = __builtin_amdgcn_exp2f(fmaf(sc[v], a.scale_log2e, -m_use));
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int d = 0; d < 4; ++d) pn[i][d] = pack_bf16(sc[8 * i + 2 * d], sc[8 * i + 2 * d + 1]);
+                for (int d = 0; d < 4; ++d) {
+                    pn[i][d] = pack_bf16(sc[8 * i + 2 * d], sc[8 * i + 2 * d + 1]);
+                    sum = tree_add_pair(sum, pn[i][d]);
+                }
 #pragma unroll
             for (int n = 0; n < 2 * NQ; ++n) {
                 __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);      // a matrix product,
