@@ -357,7 +357,7 @@ int sjd_cache_page_bytes(const sjd_kv_cache *cache, uint64_t *bytes);
 int sjd_op_cache_write(void *hip_stream, const sjd_kv_cache *cache, int32_t src_dtype, const void *k, int64_t k_stride, const void *v,
                        int64_t v_stride, const int32_t *row_start, const int32_t *first_pos, int32_t n_rows);
 
-/* The way back: k and v [n_rows][n_kv_heads][head_dim] (contiguous) of dst_dtype receive what is stored at positions first_pos[b] + i:
+/* The way back: k and v [n_rows][n_kv_heads][head_dim] (contiguous, apart) of dst_dtype receive what is stored at positions first_pos[b] + i:
  * for SJD_FP8 code * 2^e, exact in either type. */
 int sjd_op_cache_read(void *hip_stream, const sjd_kv_cache *cache, int32_t dst_dtype, void *k, void *v, const int32_t *row_start,
                       const int32_t *first_pos, int32_t n_rows);
@@ -384,7 +384,7 @@ int sjd_rope_table(int32_t rotary_dim, double theta, int32_t scaling, double fac
 /* Turns pairs of the first rotary_dim dimensions of every head by positions[row] * f_i and multiplies them by `magnitude`; the
  * other dimensions are copied.  Pairs are (i, i + rotary_dim / 2), or (2i, 2i + 1) with `interleaved`.  x and y [n_rows][heads][head_dim]
  * of `dtype` (heads contiguous, rows a stride apart), in one call for queries (n_heads) and keys (n_kv_heads; 0: none).  y may
- * be x with the same stride, and may not overlap it otherwise.  Angles are exact to 2^-33 turns at any position; a negative position
+ * be x with the same stride, and may not overlap it otherwise.  Angles are less than 2^-32 turns off at any position; a negative position
  * turns back.  head_dim <= 512. */
 int sjd_op_rotary(void *hip_stream, int32_t dtype, int32_t interleaved, const uint64_t *table, int32_t rotary_dim, float magnitude,
                   const int32_t *positions, int32_t n_rows, int32_t head_dim, const void *q, int64_t q_stride, void *q_out,
@@ -402,7 +402,8 @@ int sjd_tree_masks(const int32_t *parents, int32_t n, int32_t mask_words, uint32
  * n_heads / n_kv_heads query heads; a row that sees nothing gets zeros.  Keys and values that a row does not see do not touch it,
  * infinities and NaN included.
  * q and out [n_rows][n_heads][head_dim] of `dtype`: SJD_F32 for an SJD_F32 cache, SJD_BF16 for the others.  Probabilities are rounded
- * to bf16 for the product with values there; sums and the softmax are fp32.  scale > 0, or 0 for 1 / sqrt(head_dim).
+ * to bf16 there, for the products with values and for the sum that divides; the sums are fp32.  out may be q with the same stride, and may not
+ * overlap it otherwise.  scale > 0, or 0 for 1 / sqrt(head_dim).
  * max_rows: no tree has more rows (those behind are left as they were).  max_ctx: what ctx_len is expected to reach; it only
  * chooses how the work is divided, and with it the order of sums.  The workspace (16-byte aligned) has at least the bytes that
  * sjd_op_tree_attention_workspace writes to *bytes (HOST; may be 0, then it may be NULL) for the same arguments.  SJD_ECAPACITY: it is smaller. */

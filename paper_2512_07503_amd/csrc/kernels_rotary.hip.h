@@ -1,7 +1,8 @@
 // Rotary positions: pairs of dimensions turned by position * frequency.
 //
 // The angle is a fixed-point fraction of a turn: position (32 bits) * frequency (2^-64 turns) modulo 2^64, an integer product that is
-// exact at any position, where a float angle of a far position has no fraction left.  Its top 32 bits are split into the nearest quarter
+// exact at any position, where a float angle of a far position has no fraction left.  It is rounded to 32 bits (2^-33 turns; the frequency's
+// rounding is another 2^-34 at most), which are split into the nearest quarter
 // turn and a rest of at most an eighth, whose sine and cosine are the Taylor polynomials to x^9 and x^10 (|x| <= pi / 4: the next terms
 // are below 2^-29 and 2^-33).  Bound by memory: a row's sines and cosines are computed once, in LDS, for all its heads.
 #pragma once
@@ -21,7 +22,7 @@ struct RotaryArgs {
 };
 
 SJD_D void sincos_turns(uint64_t turns, float &sn, float &cs) {
-    const uint32_t t = (uint32_t)(turns >> 32);
+    const uint32_t t = (uint32_t)((turns + 0x80000000ull) >> 32);
     const uint32_t quarter = (t + 0x20000000u) >> 30;
     const float x = (float)(int32_t)(t - (quarter << 30)) * 0x1.921fb6p-30f;    // 2 pi / 2^32
     const float x2 = x * x;

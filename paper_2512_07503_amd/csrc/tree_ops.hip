@@ -67,6 +67,17 @@ int head_group(const sjd_kv_cache *c, int n_rows) {
 }
 unsigned head_groups(const sjd_kv_cache *c, int group) { return (unsigned)(c->n_kv_heads + group - 1) / group; }
 
+// Do n_rows rows of x and of y, x_row and y_row elements long, have no element in common?  (Rows with the same stride may interleave: parts of a
+// fused projection.)
+bool rows_apart(const void *x, long x_stride, long x_row, const void *y, long y_stride, long y_row, int n_rows, int size) {
+    const uintptr_t x0 = (uintptr_t)x, x1 = x0 + ((uintptr_t)(n_rows - 1) * x_stride + x_row) * size;
+    const uintptr_t y0 = (uintptr_t)y, y1 = y0 + ((uintptr_t)(n_rows - 1) * y_stride + y_row) * size;
+    if (x1 <= y0 || y1 <= x0) return true;
+    if (n_rows == 1 || x_stride != y_stride || x_stride <= 0) return false;
+    const long d = ((long)(y0 - x0) / size % x_stride + x_stride) % x_stride;   // where y's row starts within x's
+    return d >= x_row && d + y_row <= x_stride;
+}
+
 int check_rows(const sjd_kv_cache *cache, int32_t dtype, const void *k, const void *v, const int32_t *row_start, const int32_t *first_pos, int32_t n_rows) {
     const int rc = check_cache(cache);
     if (rc) return rc;
@@ -163,6 +174,7 @@ int sjd_op_cache_read(void *hip_stream, const sjd_kv_cache *cache, int32_t dst_d
     if (!n_rows) return SJD_OK;
     const int size = dst_dtype == SJD_F32 ? 4 : 2;
     const long stride = (long)cache->n_kv_heads * cache->head_dim;
+    if (!rows_apart(k, stride, stride, v, stride, stride, n_rows, size)) TREE_FAIL(SJD_EINVAL, "k and v overlap");
     const CacheRowsArgs a = {view(cache), row_start, first_pos, k, v, stride, stride, n_rows, head_group(cache, n_rows), wide(k, stride, size, 16), wide(v, stride, size, 16)};
     TREE_TRY(launch_rows<ReadRows>((hipStream_t)hip_stream, dim3((unsigned)cache_max_tiles(n_rows, cache->n_seqs), head_groups(cache, a.group), 2), cache->dtype,
                                    dst_dtype, a));
@@ -230,19 +242,11 @@ int sjd_op_rotary(void *hip_stream, int32_t dtype, int32_t interleaved, const ui
         if (n_rows > 1 && a.y_stride[s] < row) TREE_FAIL(SJD_EINVAL, "output rows overlap");
         if (n_rows > 1 && a.x_stride[s] < 0) TREE_FAIL(SJD_EINVAL, "negative stride");
         w = w && wide(a.x[s], a.x_stride[s], size, 16) && wide(a.y[s], a.y_stride[s], size, 16);
-        const uintptr_t x0 = (uintptr_t)a.x[s], x1 = x0 + ((uintptr_t)(n_rows - 1) * a.x_stride[s] + row) * size;
         for (int o = 0; o < 2; ++o) {
             const long out_row = (long)a.heads[o] * head_dim;
-            if (!out_row) continue;
-            const uintptr_t y0 = (uintptr_t)a.y[o], y1 = y0 + ((uintptr_t)(n_rows - 1) * a.y_stride[o] + out_row) * size;
-            // (rows with the same stride may interleave: queries and keys of a fused projection, turned in place)
-            const bool same = o == s && x0 == y0 && (a.x_stride[s] == a.y_stride[s] || n_rows == 1);
-            bool apart = x1 <= y0 || y1 <= x0;
-            if (!apart && a.x_stride[s] == a.y_stride[o] && a.x_stride[s] > 0) {
-                const long d = ((long)(y0 - x0) / size % a.x_stride[s] + a.x_stride[s]) % a.x_stride[s];   // where y's row starts within x's
-                apart = d >= row && d + out_row <= a.x_stride[s];
-            }
-            if (!same && !apart) TREE_FAIL(SJD_EINVAL, "an output overlaps an input");
+            const bool same = o == s && a.x[s] == a.y[s] && (a.x_stride[s] == a.y_stride[s] || n_rows == 1);
+            if (out_row && !same && !rows_apart(a.x[s], a.x_stride[s], row, a.y[o], a.y_stride[o], out_row, n_rows, size))
+                TREE_FAIL(SJD_EINVAL, "an output overlaps an input");
         }
     }
     if (!n_rows) return SJD_OK;
@@ -299,7 +303,12 @@ int sjd_op_tree_attention(void *hip_stream, const sjd_kv_cache *cache, int32_t d
     const int size = dtype == SJD_F32 ? 4 : 2;
     if ((uintptr_t)q % size || (uintptr_t)out % size) TREE_FAIL(SJD_EINVAL, "rows are not aligned to their elements");
     if (n_rows > 1 && out_stride < (int64_t)n_heads * cache->head_dim) TREE_FAIL(SJD_EINVAL, "output rows overlap");
+    if (n_rows > 1 && q_stride < 0) TREE_FAIL(SJD_EINVAL, "negative stride");
     if (!n_rows) return SJD_OK;
+    // in place: a workgroup has read its queries when it writes their results
+    const long row = (long)n_heads * cache->head_dim;
+    if (!(q == out && (q_stride == out_stride || n_rows == 1)) && !rows_apart(q, q_stride, row, out, out_stride, row, n_rows, size))
+        TREE_FAIL(SJD_EINVAL, "the output overlaps the queries");
     const TreePlan p = tree_plan(cache, n_heads, max_rows, max_ctx);
     if (p.part_o + p.part_ml > workspace_bytes)
         TREE_FAIL(SJD_ECAPACITY, "the workspace holds %llu bytes, %zu are needed", (unsigned long long)workspace_bytes, p.part_o + p.part_ml);

@@ -219,6 +219,22 @@ def test_strides_outputs_and_scale():
         assert (o[9:12] == 9.0).all() and not (o[4:9] == 9.0).all()
 
 
+@pytest.mark.parametrize("kind", ["fp8", "bf16", "f32"])
+def test_in_place_and_beside_the_queries(kind):
+    """Results over the queries that they come from, and between them in the rows of one buffer: split and whole, few rows and many."""
+    import paper_2512_07503_amd as sjd
+    import torch
+    for ctx, n in (([5, 90], [3, 8]), ([3000, 40], [2, 5]), ([300, 40], [40, 90])):
+        c = Case(kind, 4, 2, 64, 64, ctx, n, trees(n))
+        kw = dict(mask=c.mask, max_rows=max(n), max_ctx=max(ctx))
+        want, q = c.run(), c.q.clone()
+        assert torch.equal(sjd.op_tree_attention(q, c.cache, i32(c.starts), i32(ctx), out=q, **kw), want)
+        both = torch.empty((sum(n), 2, 4, 64), dtype=c.q.dtype, device="cuda")
+        both[:, 0] = c.q
+        sjd.op_tree_attention(both[:, 0], c.cache, i32(c.starts), i32(ctx), out=both[:, 1], **kw)
+        assert torch.equal(both[:, 1], want) and torch.equal(both[:, 0], c.q)
+
+
 def test_large_scores():
     """Scores in the thousands: one token takes all, without overflow."""
     for kind in ("fp8", "bf16", "f32"):

@@ -56,6 +56,8 @@ def test_cache_rows():
                     dict(n=(1 << 29) + 1), dict(k=ODD), dict(v=ODD)] + [dict(cache=desc(**b)) for b in BAD_CACHES]:
             refused(call(**bad))
         assert call(n=0, k=NULL, v=NULL) == sjd.OK             # nothing to do
+    for v in (64, 64 + 4, 64 + 5 * 2 * 64 * 4 - 4):            # keys and values on each other
+        refused(read(v=C.c_void_p(v)))
 
 
 def test_cache_compact():
@@ -135,6 +137,10 @@ def test_tree_attention():
                 dict(scale=math.inf), dict(max_rows=0), dict(max_rows=65537), dict(max_ctx=-1)] + [dict(cache=desc(**b)) for b in BAD_CACHES]:
         refused(call(**bad))
     assert call(n=0, q=NULL, out=NULL) == sjd.OK
+    # an output that overlaps the queries, but for the same rows; a stride that goes back
+    for bad in [dict(out=C.c_void_p(64 + 2)), dict(os=1024), dict(out=C.c_void_p(64 + 5 * 1024 + 2)), dict(qs=1024, os=1024, out=C.c_void_p(64 + 1022)),
+                dict(n=1, out=C.c_void_p(64 + 1022)), dict(qs=-512)]:
+        refused(call(**bad))
     long = dict(cache=desc(pages_per_seq=2000), max_ctx=100000)      # split: needs a workspace
     assert L.sjd_op_tree_attention_workspace(long["cache"], 8, 4, 100000, C.byref(need)) == 0 and need.value > 0
     refused(call(**long, wsb=need.value - 1), sjd.ECAPACITY)
