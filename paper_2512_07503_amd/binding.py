@@ -1,5 +1,6 @@
 """ctypes binding of include/sjd.h.  Same names as the C ABI; torch is used for device memory and streams only."""
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -563,6 +564,13 @@ def op_tree_attention(q, cache, row_start, ctx_len, mask=None, max_rows=None, ma
     return out
 
 
+@functools.lru_cache(maxsize=256)
+def _verify_bytes(rows, seqs, vocab):
+    n = C.c_uint64(0)
+    _check(lib().sjd_op_tree_verify_workspace(rows, seqs, vocab, C.byref(n)))
+    return n.value
+
+
 def op_tree_verify(tokens, parents, row_start, p, q, accept_words, draw_words, max_rows=None, max_path=None, workspace=None):
     """Verifies trees of drafted tokens: tokens, parents int32 [rows]; p (and q, or None) float32 [rows, vocab], rows may be strided; accept_words
     [rows], the bits of 32-bit words (int32 or uint32); draw_words [n_seqs], of 64-bit words.  -> (path int32 [n_seqs, max_path], path_len int32
@@ -582,9 +590,7 @@ def op_tree_verify(tokens, parents, row_start, p, q, accept_words, draw_words, m
     path = torch.empty((seqs, max_path), dtype=torch.int32, device=p.device)
     path_len = path.new_empty(seqs)
     token = path.new_empty(seqs)
-    n = C.c_uint64(0)
-    _check(lib().sjd_op_tree_verify_workspace(rows, seqs, shape[1], C.byref(n)))
-    at, size, keep = _workspace(workspace, n.value, p)
+    at, size, keep = _workspace(workspace, _verify_bytes(rows, seqs, shape[1]), p)
     _enqueue(device, lib().sjd_op_tree_verify, _vector(tokens, rows, torch.int32, "tokens"), _vector(parents, rows, torch.int32, "parents"),
              _vector(row_start, seqs + 1, torch.int32, "row_start"), p.data_ptr(), p.stride(0) if rows > 1 else shape[1], None if q is None else q.data_ptr(),
              0 if q is None else q.stride(0) if rows > 1 else shape[1],
