@@ -420,9 +420,10 @@ int sjd_op_tree_attention(void *hip_stream, const sjd_kv_cache *cache, int32_t d
  * not drawn but chosen (a model's likeliest tokens), each a proposal of probability 1.
  * From node 0 on, the children x of the node reached, in the order of their indices:  with rho_0 = p and S_0 = 1, child k is
  * accepted where r q(x) S_k < rho_k(x), r = (accept_words[its row] + 1/2) 2^-32; if not, rho_{k+1} = max(0, rho_k - S_k q) and
- * S_{k+1} = sum rho_{k+1}.  Where no child is accepted, or max_path nodes are reached, next_token is drawn from the last rho
- * (from p, where that is all 0): the first id whose cumulated weight exceeds the share draw_words[b] / 2^64 of all.  In distribution the
- * accepted tokens and the next one are what the target alone would have produced.  All of it is specified bit for bit: double
+ * S_{k+1} = sum rho_{k+1}.  Where no child is accepted next_token is drawn from the last rho (from p, where that is all 0).  Where
+ * max_path nodes are reached it is drawn from the last one's p, and that node's children are not tested.  Drawn is the first id
+ * whose cumulated weight exceeds the share draw_words[b] / 2^64 of all.  In distribution the accepted tokens and the
+ * next one are what the target alone would have produced, whatever max_path is.  All of it is specified bit for bit: double
  * precision, the products in the order (r q) S and S q, sums of trunc(min(rho, 1) 2^44); a p that is negative or NaN is 0, and so is rho
  * from the rejection on that a NaN of q takes part in.  A token outside [0, vocab) is rejected.
  * Outputs: path [n_seqs][max_path], the nodes reached, node 0 first, -1 behind them; path_len [n_seqs] (accepted drafts + 1; 0 for a

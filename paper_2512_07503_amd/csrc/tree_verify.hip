@@ -265,7 +265,7 @@ __global__ __launch_bounds__(256) void verify_walk_kernel(VerifyArgs a) {
     const int b = blockIdx.y, slice = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int r0, n;
     tree_rows(a, b, r0, n);
-    __shared__ int choice[kMaxNodes], parent[kMaxNodes], child[kMaxNodes], way, wave_count[4];
+    __shared__ int choice[kMaxNodes], parent[kMaxNodes], child[kMaxNodes], way, way_len, wave_count[4];
     __shared__ double mass[kMaxNodes];
     __shared__ uint64_t scratch[4];
     for (int i = tid; i < n; i += 256) {
@@ -283,13 +283,15 @@ __global__ __launch_bounds__(256) void verify_walk_kernel(VerifyArgs a) {
             ++len;
         }
         way = at;
+        way_len = len;
         if (slice == 0) a.path_len[b] = len;
     }
     __syncthreads();
     const int at = way;
-    // its rejected children: all of them, unless it is the path's length that ended the walk
+    // its rejected children: all of them, but none of the last node that the path has room for, whose children do not count: a draw that took its
+    // residual where they are rejected, and its p where one is accepted, would not be the target's
     int m = 0;
-    if (at >= 0 && choice[at] <= at)
+    if (at >= 0 && way_len < a.max_path)
         for (int j0 = at + 1; j0 < n; j0 += 256) {
             const int j = j0 + tid;
             const bool is_child = j < n && parent[j] == at;
