@@ -327,7 +327,8 @@ int sjd_op_philox(void *hip_stream, uint64_t seed, uint32_t row, uint32_t seq, u
  *
  * Ragged rows: rows [row_start[b], row_start[b + 1]) of the arrays are sequence b's, b < n_seqs (row_start has n_seqs + 1
  * entries, ascending; what lies outside [0, n_rows] is cut off), and row row_start[b] + i belongs to position
- * first_pos[b] + i of its cache.  Outputs of rows of no sequence are left as they were.
+ * first_pos[b] + i of its cache.  Outputs of rows of no sequence are left as they were.  A sequence whose first_pos is negative or above
+ * 2^30 lies outside its cache as a whole, whichever of its rows would come to stand inside.
  *
  * Sizes and pointers are checked on the host (SJD_EINVAL, nothing enqueued).  What is in device memory is checked by the kernels:
  * a page table entry outside [0, n_pages), or a position outside [0, pages_per_seq * page_tokens), is never
@@ -364,7 +365,7 @@ int sjd_op_cache_read(void *hip_stream, const sjd_kv_cache *cache, int32_t dst_d
 
 /* Keeps a path of a tree: of the rows at positions first_pos[b] + 0, 1, ..., those of nodes path[b][0 .. path_len[b] - 1] move to
  * positions first_pos[b] + 0 .. path_len[b] - 1, bit for bit.  path [n_seqs][max_path]; its nodes ascend, and what comes
- * from the first that does not (or is negative) is ignored. */
+ * from the first that does not (or is negative) is ignored.  Where the old or the new position is outside nothing moves. */
 int sjd_op_cache_compact(void *hip_stream, const sjd_kv_cache *cache, const int32_t *first_pos, const int32_t *path,
                          const int32_t *path_len, int32_t max_path);
 

@@ -57,8 +57,13 @@ constexpr int rows_count(const int32_t *row_start, int b, int n_rows) {
     return n > 0 ? n : 0;
 }
 
+// First position of a sequence's rows as a write or a read takes it.  One that is negative or beyond 2^30 is outside, and with it the whole
+// sequence: its rows stand where no table reaches (a sequence has at most 2^30 positions), so that writes drop them and reads give zeros.
+constexpr int kCacheOutside = 1 << 30;
+constexpr int cache_first(int first) { return first < 0 || first > kCacheOutside ? kCacheOutside : first; }
+
 // tiles of 32 positions that n rows from position `first` on touch
-constexpr int cache_tiles(int first, int n) { return n > 0 && first >= 0 && first <= 1 << 30 ? ((first + n - 1) >> 5) - (first >> 5) + 1 : 0; }
+constexpr int cache_tiles(int first, int n) { return n > 0 && first >= 0 && first <= kCacheOutside ? ((first + n - 1) >> 5) - (first >> 5) + 1 : 0; }
 // and an upper bound over n_rows rows of n_seqs sequences: n >= 1 rows touch at most 1 + (n + 30) / 32 of them, and no more than n
 constexpr long cache_max_tiles(int n_rows, int n_seqs) {
     const long s = n_seqs < n_rows ? n_seqs : n_rows, t = (n_rows + 30 * s) / 32 + s;

@@ -36,7 +36,7 @@ SJD_D CacheTile cache_find_tile(const int32_t *row_start, const int32_t *first_p
         if (b < n_seqs) {
             r0 = rows_first(row_start, b, n_rows);
             n = rows_count(row_start, b, n_rows);
-            first = first_pos[b];
+            first = cache_first(first_pos[b]);
         }
         const int tiles = cache_tiles(first, n);
         int upto = tiles;
