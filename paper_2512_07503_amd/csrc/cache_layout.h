@@ -91,6 +91,10 @@ constexpr uint32_t tree_visible(const uint32_t *mask, int mask_words, int ctx, i
     return ((nodes & ~cached) | cached) & there;
 }
 
+// The node that a walk through a tree of n nodes goes on to from node `at`, whose accepted child is said to be `choice`; -1: it ends there.  (Where row_start does not
+// ascend, sequences share rows, and what one of them says of its nodes may have been written for the larger tree of another.)
+constexpr int tree_step(int choice, int at, int n) { return choice > at && choice < n ? choice : -1; }
+
 // Blocks of 32 tokens [first, last) that split `split` of n_splits goes through, of rows the last of which is node last_node
 struct TreeBlocks { int first, last; };
 constexpr TreeBlocks tree_blocks(bool mask, int ctx, int n_tot, int last_node, int split, int n_splits) {

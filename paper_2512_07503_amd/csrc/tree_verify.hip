@@ -277,8 +277,10 @@ __global__ __launch_bounds__(256) void verify_walk_kernel(VerifyArgs a) {
     if (tid == 0) {
         int at = n > 0 ? 0 : -1, len = n > 0 ? 1 : 0;
         if (slice == 0 && len) a.path[(size_t)b * a.max_path] = 0;
-        while (at >= 0 && len < a.max_path && choice[at] > at) {
-            at = choice[at];
+        while (at >= 0 && len < a.max_path) {
+            const int next = tree_step(choice[at], at, n);
+            if (next < 0) break;
+            at = next;
             if (slice == 0) a.path[(size_t)b * a.max_path + len] = at;
             ++len;
         }
@@ -360,6 +362,7 @@ __global__ __launch_bounds__(256) void verify_draw_kernel(VerifyArgs a) {
         return;
     }
     const uint64_t t = __umul64hi(word, Z);
+    if (tid == 0) a.next_token[b] = -1;             // (stays where sequences that share rows have left each other's rejections here)
     auto upto = [&](uint64_t v) {                   // inclusive prefix sum over the workgroup
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {

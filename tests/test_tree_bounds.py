@@ -35,3 +35,29 @@ def test_first_positions_outside(tmp_path):
             }
     for (int first : {0, 1, 31, 1000, (1 << 30) - 1}) CHECK(cache_first(first) == first);
 """)
+
+
+def test_walks_stay_within_their_trees(tmp_path):
+    """Whatever stands at a tree's rows: here what a larger tree, whose rows they are as well, has left there.  Every node of a walk is read at its index."""
+    play(tmp_path, r"""
+    std::vector<int> choice(1000);
+    for (int i = 0; i < 1000; ++i) choice[i] = i + 50;
+    std::vector<int> mine(choice.begin(), choice.begin() + 100);     // rows 900 .. 999 of these, as the nodes 0 .. 99 of a tree of their own: 850 further on
+    for (int &c : mine) c += 900;
+    CHECK(mine[0] == 950 && tree_step(mine[0], 0, 100) == -1);
+    srand(1);
+    const int odd[] = {INT_MIN, -1, 0, 1, 5, 99, 100, 101, 1023, 1024, INT_MAX};
+    for (int it = 0; it < 2000; ++it) {
+        const int n = 1 + rand() % 100;
+        std::vector<int> c(n);
+        for (int &x : c) x = rand() % 4 ? rand() % (n + 3) : odd[rand() % 11];
+        int at = 0, steps = 0;
+        for (;;) {
+            const int next = tree_step(c.at(at), at, n);
+            CHECK(next == (c[at] > at && c[at] < n ? c[at] : -1));
+            if (next < 0) break;
+            at = next;
+            CHECK(++steps < n);
+        }
+    }
+""")
