@@ -385,8 +385,8 @@ int sjd_rope_table(int32_t rotary_dim, double theta, int32_t scaling, double fac
 /* Turns pairs of the first rotary_dim dimensions of every head by positions[row] * f_i and multiplies them by `magnitude`; the
  * other dimensions are copied.  Pairs are (i, i + rotary_dim / 2), or (2i, 2i + 1) with `interleaved`.  x and y [n_rows][heads][head_dim]
  * of `dtype` (heads contiguous, rows a stride apart), in one call for queries (n_heads) and keys (n_kv_heads; 0: none).  y may
- * be x with the same stride, and may not overlap it otherwise.  Angles are less than 2^-32 turns off at any position; a negative position
- * turns back.  head_dim <= 512. */
+ * be x with the same stride, and may not overlap it otherwise, nor the outputs each other (parts of one buffer's rows may lie between each
+ * other).  Angles are less than 2^-32 turns off at any position; a negative position turns back.  head_dim <= 512. */
 int sjd_op_rotary(void *hip_stream, int32_t dtype, int32_t interleaved, const uint64_t *table, int32_t rotary_dim, float magnitude,
                   const int32_t *positions, int32_t n_rows, int32_t head_dim, const void *q, int64_t q_stride, void *q_out,
                   int64_t q_out_stride, int32_t n_heads, const void *k, int64_t k_stride, void *k_out, int64_t k_out_stride,

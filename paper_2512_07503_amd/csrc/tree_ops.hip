@@ -250,6 +250,8 @@ int sjd_op_rotary(void *hip_stream, int32_t dtype, int32_t interleaved, const ui
         }
     }
     if (!n_rows) return SJD_OK;
+    if (n_kv_heads && !rows_apart(q_out, q_out_stride, (long)n_heads * head_dim, k_out, k_out_stride, (long)n_kv_heads * head_dim, n_rows, size))
+        TREE_FAIL(SJD_EINVAL, "q_out and k_out overlap");
     // Rows a workgroup: their sines and cosines are shared by the heads of a row only, so more rows mean nothing but fewer workgroups;
     // two for each of the 256 CUs, and few rows are split over their heads' units instead.
     while (a.rows_per_wg < 8 && a.rows_per_wg * a.half * 2 <= 8 * kRotaryMaxHalf && n_rows / (2 * a.rows_per_wg) >= 512) a.rows_per_wg *= 2;
