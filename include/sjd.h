@@ -400,7 +400,7 @@ int sjd_tree_masks(const int32_t *parents, int32_t n, int32_t mask_words, uint32
 /* Attention of the rows of trees over a cache that holds them already: node i of sequence b (row row_start[b] + i, position
  * ctx_len[b] + i) attends to positions [0, ctx_len[b]) and to those nodes j of its own tree whose bit j % 32 of
  * mask[row][j / 32] is set; with mask NULL to nodes 0 .. i (a window).  Row by row out = softmax(scale * q k) v with one kv head to
- * n_heads / n_kv_heads query heads; a row that sees nothing gets zeros.  Keys and values that a row does not see do not touch it,
+ * n_heads / n_kv_heads query heads; a row that sees nothing gets zeros, and so do the rows of a sequence whose ctx_len is negative.  Keys and values that a row does not see do not touch it,
  * infinities and NaN included.
  * q and out [n_rows][n_heads][head_dim] of `dtype`: SJD_F32 for an SJD_F32 cache, SJD_BF16 for the others.  Probabilities are rounded
  * to bf16 there, for the products with values and for the sum that divides; the sums are fp32.  out may be q with the same stride, and may not

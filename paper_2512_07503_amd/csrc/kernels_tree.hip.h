@@ -24,15 +24,16 @@ struct TreeArgs {
     bool q_wide, out_wide;     // rows 16-byte (out: 4 elements) aligned
 };
 
-// Rows and length of sequence b
+// Rows and length of sequence b.  One whose length is negative is outside as a whole, like its rows in the cache, and sees nothing.
 struct TreeSeq { int r0, n, ctx, n_tot; };
 SJD_D TreeSeq tree_seq(const TreeArgs &a, int b) {
     TreeSeq s;
     s.r0 = rows_first(a.row_start, b, a.n_rows);
     s.n = min(rows_count(a.row_start, b, a.n_rows), a.max_rows);
     const int cap = a.c.pages_per_seq * a.c.page_tokens;
-    s.ctx = min(max(a.ctx_len[b], 0), cap);
-    s.n_tot = min(s.ctx + s.n, cap);
+    const int ctx = a.ctx_len[b];
+    s.ctx = min(max(ctx, 0), cap);
+    s.n_tot = ctx < 0 ? 0 : min(s.ctx + s.n, cap);
     return s;
 }
 
