@@ -234,12 +234,16 @@ template <int HD> struct TreeState {
     }
 };
 
-// The state is rescaled only when a row's maximum has grown by more than a factor of 2^8: until then its probabilities are up to 2^8
-// in place of 1, which costs neither fp32 sums nor bf16 operands a bit.  The reference is a whole number, so that rescaling is exact.
+// Probabilities are 2^(score - m).  A rescaling puts m 8 above the row's maximum, a whole number, so that it is exact, and the next one comes when the
+// maximum has grown beyond m: until then probabilities are between 2^-9 and 1 at the maximum, never above 1, and so no sum of products with values overflows that would not
+// with the formula's own.  (With m at the maximum and up to 2^8 above it, finite values from 2^120 on became infinite.)  The factor costs neither fp32 sums nor bf16 operands
+// a bit but at the lower end of the exponents: values below 2^-117 make subnormal products, which the matrix cores keep (of values of 2^-124 an fp32 row is
+// 2^-18 off).
 // `pending`: probabilities whose product with values is still to come.
+constexpr float kTreeAhead = 8.0f;
 template <int HD, typename F> SJD_D void tree_rescale(TreeState<HD> &st, float mx, F pending) {
-    if (!__ballot(mx > st.m + 8.0f)) return;
-    const float m = fmaxf(st.m, __builtin_ceilf(mx));
+    if (!__ballot(mx > st.m)) return;
+    const float m = fmaxf(st.m, __builtin_ceilf(mx) + kTreeAhead);
     const float alpha = __builtin_amdgcn_exp2f(st.m - (m == -INFINITY ? 0.0f : m));     // (not (-inf) - (-inf))
     st.m = m;
     st.l *= alpha;
