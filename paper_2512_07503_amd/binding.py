@@ -541,6 +541,8 @@ def op_tree_attention(q, cache, row_start, ctx_len, mask=None, max_rows=None, ma
     if mask is not None:
         if mask.dtype not in (torch.int32, torch.uint32) or mask.dim() != 2 or mask.shape[0] != rows or not mask.is_contiguous():
             _refuse("mask must be a contiguous int32 or uint32 [rows, words]")
+        if rows and not mask.shape[1]:
+            _refuse("a mask needs a word a row (its pointer would be null, as a window's is)")
         mask_ptr, words = mask.data_ptr(), mask.shape[1]
     if out is None:
         out, out_stride = q.new_empty(shape), heads * hd
