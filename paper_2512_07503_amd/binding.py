@@ -400,7 +400,8 @@ def _row_stride(x, heads, hd, name):
 
 class KvCache:
     """A paged key/value cache ("f32", "bf16" or "fp8") and its page table, int32 CUDA [n_seqs, pages_per_seq]; entries outside
-    [0, n_pages) are unused.  Owns its pages (zeroed); the table is the caller's and may change between calls."""
+    [0, n_pages) are unused.  Owns its pages (zeroed); the table is the caller's, and its contents may change between calls.  Either tensor stays
+    the one that it is: calls take the addresses that the cache was made with."""
 
     def __init__(self, dtype, n_pages, page_tokens, n_kv_heads, head_dim, page_table):
         import torch
@@ -410,22 +411,30 @@ class KvCache:
             _refuse("page_table must be a contiguous int32 CUDA matrix")
         if n_pages < 1:
             _refuse("n_pages must be positive")
-        self.dtype, self.n_kv_heads, self.head_dim, self.page_table = dtype, n_kv_heads, head_dim, page_table
+        self.dtype, self.n_kv_heads, self.head_dim, self._page_table = dtype, n_kv_heads, head_dim, page_table
         self.n_seqs, self.device = page_table.shape[0], page_table.device
         self.desc = KvCacheDesc(None, page_table.data_ptr(), n_pages, page_tokens, n_kv_heads, head_dim, _CACHE_DTYPES[dtype], *page_table.shape)
         self.ref = C.byref(self.desc)
         n = C.c_uint64(0)
         _check(lib().sjd_cache_page_bytes(self.ref, C.byref(n)))
-        self.pages = torch.zeros(n_pages * n.value, dtype=torch.uint8, device=self.device)
-        self.desc.pages = self.pages.data_ptr()
+        self._pages = torch.zeros(n_pages * n.value, dtype=torch.uint8, device=self.device)
+        self.desc.pages = self._pages.data_ptr()
         self.workspaces = {}    # bytes of op_tree_attention's workspace, by the sizes that they follow from
+
+    @property
+    def pages(self):
+        return self._pages
+
+    @property
+    def page_table(self):
+        return self._page_table
 
 
 def op_cache_write(cache, k, v, row_start, first_pos):
     """Writes k and v [rows, n_kv_heads, head_dim] (float32 or bfloat16; rows may be strided) to positions first_pos[b] + i of sequence b =
     rows row_start[b] + i.  row_start int32 [n_seqs + 1], first_pos int32 [n_seqs]."""
     import torch
-    device = _device_of(cache.page_table, k, v, row_start, first_pos)
+    device = _device_of(cache._page_table, k, v, row_start, first_pos)
     code, n = _row_code(k, "k"), k.shape[0]
     ks, vs = _row_stride(k, cache.n_kv_heads, cache.head_dim, "k"), _row_stride(v, cache.n_kv_heads, cache.head_dim, "v")
     if v.dtype is not k.dtype or v.shape[0] != n:
@@ -438,7 +447,7 @@ def op_cache_read(cache, row_start, first_pos, n_rows, dtype=None, out=None):
     """-> (k, v) [n_rows, n_kv_heads, head_dim] of `dtype` (bfloat16 unless given): what is stored at positions first_pos[b] + i of sequence
     b, in rows row_start[b] + i.  out: a pair of such tensors to write to.  Rows of no sequence are not written."""
     import torch
-    device = _device_of(cache.page_table, row_start, first_pos, *(out or ()))
+    device = _device_of(cache._page_table, row_start, first_pos, *(out or ()))
     shape = (n_rows, cache.n_kv_heads, cache.head_dim)
     if out is None:
         if n_rows < 0:
@@ -455,7 +464,7 @@ def op_cache_read(cache, row_start, first_pos, n_rows, dtype=None, out=None):
 def op_cache_compact(cache, first_pos, path, path_len):
     """Moves the entries at positions first_pos[b] + path[b, j] to first_pos[b] + j, j < path_len[b].  path int32 [n_seqs, max_path]."""
     import torch
-    device = _device_of(cache.page_table, first_pos, path, path_len)
+    device = _device_of(cache._page_table, first_pos, path, path_len)
     if path.dtype is not torch.int32 or path.dim() != 2 or path.shape[0] != cache.n_seqs or not path.is_contiguous():
         _refuse("path must be a contiguous int32 [n_seqs, max_path]")
     _enqueue(device, lib().sjd_op_cache_compact, cache.ref, _vector(first_pos, cache.n_seqs, torch.int32, "first_pos"), path.data_ptr(),
@@ -531,7 +540,7 @@ def op_tree_attention(q, cache, row_start, ctx_len, mask=None, max_rows=None, ma
     (default: all rows); max_ctx: what ctx_len is expected to reach (default: what the page table holds).  -> out like q; rows of no sequence
     are not written."""
     import torch
-    device = _device_of(cache.page_table, q, row_start, ctx_len, mask, out, workspace)
+    device = _device_of(cache._page_table, q, row_start, ctx_len, mask, out, workspace)
     code, shape, hd = _row_code(q, "q"), q.shape, cache.head_dim
     if len(shape) != 3:
         _refuse("q must be [rows, heads, head_dim]")

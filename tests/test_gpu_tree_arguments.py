@@ -16,3 +16,21 @@ def test_a_mask_without_words_is_refused():
         with pytest.raises(sjd.SjdError):
             c.run(mask=mask)
     c.check(c.run())
+
+
+def test_a_cache_keeps_its_tensors():
+    """The library holds their addresses: another tensor in their place would be ignored, and the old one's memory given to somebody else."""
+    c = Case("bf16", 4, 2, 64, 64, [40, 3], [5, 1], trees([5, 1]))
+    for name in ("page_table", "pages"):
+        with pytest.raises(AttributeError):
+            setattr(c.cache, name, getattr(c.cache, name).clone())
+    want = c.run()
+    # the table's contents may change: two pages trade places, and so do their bytes
+    per = c.cache.pages.numel() // c.cache.desc.n_pages
+    a, b = int(c.table[0, 0]), int(c.table[1, 0])
+    pages = c.cache.pages.view(-1, per)
+    pages[[a, b]] = pages[[b, a]]
+    table = c.table.copy()
+    table[0, 0], table[1, 0] = b, a
+    c.cache.page_table.copy_(i32(table))
+    assert (c.run() == want).all()
