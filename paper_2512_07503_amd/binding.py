@@ -419,7 +419,7 @@ class KvCache:
         _check(lib().sjd_cache_page_bytes(self.ref, C.byref(n)))
         self._pages = torch.zeros(n_pages * n.value, dtype=torch.uint8, device=self.device)
         self.desc.pages = self._pages.data_ptr()
-        self.workspaces = {}    # bytes of op_tree_attention's workspace, by the sizes that they follow from
+        self.sizes = _CACHE_DTYPES[dtype], page_tokens, n_kv_heads, head_dim, self.n_seqs
 
     @property
     def pages(self):
@@ -534,6 +534,15 @@ def _workspace(given, need, like):
     return given.data_ptr(), given.numel() * given.element_size(), given
 
 
+@functools.lru_cache(maxsize=256)
+def _attention_bytes(sizes, heads, max_rows, max_ctx):
+    """Of op_tree_attention's workspace, for KvCache.sizes."""
+    dtype, page_tokens, n_kv_heads, head_dim, n_seqs = sizes
+    n = C.c_uint64(0)
+    _check(lib().sjd_op_tree_attention_workspace(C.byref(KvCacheDesc(None, None, 0, page_tokens, n_kv_heads, head_dim, dtype, n_seqs, 0)), heads, max_rows, max_ctx, C.byref(n)))
+    return n.value
+
+
 def op_tree_attention(q, cache, row_start, ctx_len, mask=None, max_rows=None, max_ctx=None, scale=0.0, out=None, workspace=None):
     """Attention of q [rows, heads, head_dim] over the cache: row row_start[b] + i (position ctx_len[b] + i) sees positions [0, ctx_len[b])
     and the nodes whose bits are set in its row of mask, int32 or uint32 [rows, words]; without a mask nodes 0 .. i.  max_rows: no tree has more
@@ -563,12 +572,7 @@ def op_tree_attention(q, cache, row_start, ctx_len, mask=None, max_rows=None, ma
         max_rows = max(rows, 1)
     if max_ctx is None:
         max_ctx = cache.desc.pages_per_seq * cache.desc.page_tokens
-    need = cache.workspaces.get((heads, max_rows, max_ctx))
-    if need is None:
-        n = C.c_uint64(0)
-        _check(lib().sjd_op_tree_attention_workspace(cache.ref, heads, max_rows, max_ctx, C.byref(n)))
-        need = cache.workspaces[heads, max_rows, max_ctx] = n.value
-    at, size, keep = _workspace(workspace, need, q)
+    at, size, keep = _workspace(workspace, _attention_bytes(cache.sizes, heads, max_rows, max_ctx), q)
     _enqueue(device, lib().sjd_op_tree_attention, cache.ref, code, q.data_ptr(), stride, out.data_ptr(), out_stride,
              _vector(row_start, cache.n_seqs + 1, torch.int32, "row_start"), _vector(ctx_len, cache.n_seqs, torch.int32, "ctx_len"), mask_ptr, words, rows, heads, scale,
              max_rows, max_ctx, at, size)

@@ -34,3 +34,14 @@ def test_a_cache_keeps_its_tensors():
     table[0, 0], table[1, 0] = b, a
     c.cache.page_table.copy_(i32(table))
     assert (c.run() == want).all()
+
+
+def test_lengths_of_a_long_loop_leave_nothing_behind():
+    """A loop that says at every step how long its contexts are: what a cache and the binding remember of that has a bound."""
+    import paper_2512_07503_amd as sjd
+    c = Case("bf16", 4, 2, 64, 64, [40], [1])
+    q = c.q[:0]
+    for max_ctx in range(2000):
+        sjd.op_tree_attention(q, c.cache, i32([0, 0]), i32([40]), max_rows=1, max_ctx=max_ctx)
+    assert sum(len(x) for x in vars(c.cache).values() if isinstance(x, dict)) <= 256
+    assert sjd.binding._attention_bytes.cache_info().currsize <= 256
