@@ -330,7 +330,8 @@ int sjd_op_philox(void *hip_stream, uint64_t seed, uint32_t row, uint32_t seq, u
  * first_pos[b] + i of its cache.  Outputs of rows of no sequence are left as they were.  A sequence whose first_pos is negative or above
  * 2^30 lies outside its cache as a whole, whichever of its rows would come to stand inside.
  *
- * Sizes and pointers are checked on the host (SJD_EINVAL, nothing enqueued).  What is in device memory is checked by the kernels:
+ * Sizes and pointers are checked on the host (SJD_EINVAL, nothing enqueued; so is a call of more workgroups than a launch has
+ * room for, 2^24 - 1: of the order of 2^24 tiles of rows, or of sequences).  What is in device memory is checked by the kernels:
  * a page table entry outside [0, n_pages), or a position outside [0, pages_per_seq * page_tokens), is never
  * followed: writes to it are dropped, reads of it give zeros, attention does not see it. */
 

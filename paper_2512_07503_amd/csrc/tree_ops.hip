@@ -16,6 +16,9 @@ namespace {
     } while (0)
 #define TREE_TRY(expr) SJD_HIP_TRY(sjd_call_error(), expr)
 
+// A launch has at most 2^32 - 1 work-items a dimension: so many workgroups of 256
+constexpr size_t kMaxWorkgroups = (1u << 24) - 1;
+
 bool wide(const void *p, int64_t stride, int size, int bytes) { return (uintptr_t)p % bytes == 0 && stride * size % bytes == 0; }
 
 int check_shape(const sjd_kv_cache *c) {
@@ -84,6 +87,7 @@ int check_rows(const sjd_kv_cache *cache, int32_t dtype, const void *k, const vo
     if (dtype != SJD_F32 && dtype != SJD_BF16) TREE_FAIL(SJD_EINVAL, "rows are SJD_F32 or SJD_BF16");
     if (n_rows < 0 || n_rows > 1 << 29) TREE_FAIL(SJD_EINVAL, "n_rows must be 0 .. 2^29");
     if (!row_start || !first_pos || (n_rows && (!k || !v))) TREE_FAIL(SJD_EINVAL, "null argument");
+    if ((size_t)cache_max_tiles(n_rows, cache->n_seqs) > kMaxWorkgroups) TREE_FAIL(SJD_EINVAL, "too many rows or sequences for one launch");
     const unsigned size = dtype == SJD_F32 ? 4 : 2;
     if ((uintptr_t)k % size || (uintptr_t)v % size) TREE_FAIL(SJD_EINVAL, "rows are not aligned to their elements");
     return SJD_OK;
@@ -118,8 +122,13 @@ TreePlan tree_plan(const sjd_kv_cache *c, int n_heads, int max_rows, int max_ctx
 int check_attention(const sjd_kv_cache *c, int32_t n_heads, int32_t max_rows, int32_t max_ctx) {
     if (n_heads < 1 || n_heads % c->n_kv_heads || n_heads > 1 << 20) TREE_FAIL(SJD_EINVAL, "n_heads must be a multiple of n_kv_heads");
     if (max_rows < 1 || max_rows > 1 << 16 || max_ctx < 0 || max_ctx > 1 << 30) TREE_FAIL(SJD_EINVAL, "max_rows must be 1 .. 65536, max_ctx 0 .. 2^30");
+    const size_t pairs = (size_t)c->n_seqs * c->n_kv_heads;
+    // (so many at least, of four tiles of 32 rows; what follows stays within its integers)
+    if (pairs > kMaxWorkgroups || (size_t)max_rows * (n_heads / c->n_kv_heads) > kMaxWorkgroups * 128) TREE_FAIL(SJD_EINVAL, "too many rows for one launch");
     const TreePlan p = tree_plan(c, n_heads, max_rows, max_ctx);
-    if ((size_t)c->n_seqs * c->n_kv_heads * p.tiles * 64 > 1u << 30) TREE_FAIL(SJD_EINVAL, "too many rows for one launch");
+    // (of the kernel: its workgroups come in eights, for the XCDs; of the joining of splits: 256 threads own four dimensions each)
+    if (pairs * p.tiles > 1u << 24 || ceil_div_sz(pairs * p.n_splits, 8) * 8 * p.groups > kMaxWorkgroups ||
+        (p.n_splits > 1 && pairs * p.tiles * ceil_div(8 * c->head_dim, 256) > kMaxWorkgroups)) TREE_FAIL(SJD_EINVAL, "too many rows for one launch");
     return SJD_OK;
 }
 
@@ -186,6 +195,7 @@ int sjd_op_cache_compact(void *hip_stream, const sjd_kv_cache *cache, const int3
     const int rc = check_cache(cache);
     if (rc) return rc;
     if (!first_pos || !path || !path_len || max_path < 1) TREE_FAIL(SJD_EINVAL, "null argument or max_path < 1");
+    if ((size_t)cache->n_seqs > kMaxWorkgroups) TREE_FAIL(SJD_EINVAL, "too many sequences for one launch");
     const dim3 grid(cache->n_seqs, cache->n_kv_heads, 2);
     hipStream_t st = (hipStream_t)hip_stream;
     const CacheView c = view(cache);
@@ -256,6 +266,7 @@ int sjd_op_rotary(void *hip_stream, int32_t dtype, int32_t interleaved, const ui
     // two for each of the 256 CUs, and few rows are split over their heads' units instead.
     while (a.rows_per_wg < 8 && a.rows_per_wg * a.half * 2 <= 8 * kRotaryMaxHalf && n_rows / (2 * a.rows_per_wg) >= 512) a.rows_per_wg *= 2;
     const unsigned gx = (unsigned)ceil_div(n_rows, a.rows_per_wg);
+    if (gx > kMaxWorkgroups) TREE_FAIL(SJD_EINVAL, "too many rows for one launch");
     const long units = (long)a.rows_per_wg * (n_heads + n_kv_heads) * (w ? head_dim / 8 : head_dim);
     long gy = gx >= 512 ? 1 : 512 / gx;
     if (gy > (units + 255) / 256) gy = (units + 255) / 256;
