@@ -402,9 +402,10 @@ int sjd_tree_masks(const int32_t *parents, int32_t n, int32_t mask_words, uint32
  * ctx_len[b] + i) attends to positions [0, ctx_len[b]) and to those nodes j of its own tree whose bit j % 32 of
  * mask[row][j / 32] is set; with mask NULL to nodes 0 .. i (a window).  Row by row out = softmax(scale * q k) v with one kv head to
  * n_heads / n_kv_heads query heads; a row that sees nothing gets zeros, and so do the rows of a sequence whose ctx_len is negative.  Keys and values that a row does not see do not touch it,
- * infinities and NaN included.
+ * infinities and NaN included; an infinite value that it does see makes its result infinite, and may make it NaN where its weight is below what fp32 holds.
  * q and out [n_rows][n_heads][head_dim] of `dtype`: SJD_F32 for an SJD_F32 cache, SJD_BF16 for the others.  Probabilities are rounded
- * to bf16 there, for the products with values and for the sum that divides; the sums are fp32.  out may be q with the same stride, and may not
+ * to bf16 there, for the products with values and for the sum that divides, so that weights add up to 1; the sums are fp32.  (The mean error against 64
+ * bits is up to 1.4 times that of a result that is only rounded to bf16 at the end.)  out may be q with the same stride, and may not
  * overlap it otherwise.  scale > 0, or 0 for 1 / sqrt(head_dim).
  * max_rows: no tree has more rows (those behind are left as they were).  max_ctx: what ctx_len is expected to reach; it only
  * chooses how the work is divided, and with it the order of sums.  The workspace (16-byte aligned) has at least the bytes that
@@ -430,7 +431,8 @@ int sjd_op_tree_attention(void *hip_stream, const sjd_kv_cache *cache, int32_t d
  * from the rejection on that a NaN of q takes part in.  A token outside [0, vocab) is rejected.
  * Outputs: path [n_seqs][max_path], the nodes reached, node 0 first, -1 behind them; path_len [n_seqs] (accepted drafts + 1; 0 for a
  * sequence without rows); next_token [n_seqs] (-1 without rows, or where p is all 0).  path and path_len are what
- * sjd_op_cache_compact takes.  max_rows <= 1024, vocab <= 524288; rows of a tree behind max_rows are ignored.  The workspace
+ * sjd_op_cache_compact takes.  max_rows <= 1024, vocab <= 524288; rows of a tree behind max_rows are ignored.  With q, every rejected child of a node
+ * costs a pass over the vocabulary, with a step an id for each one rejected before it.  The workspace
  * (16-byte aligned) as in sjd_op_tree_attention. */
 int sjd_op_tree_verify_workspace(int32_t n_rows, int32_t n_seqs, int32_t vocab, uint64_t *bytes);
 int sjd_op_tree_verify(void *hip_stream, const int32_t *tokens, const int32_t *parents, const int32_t *row_start, const float *p,

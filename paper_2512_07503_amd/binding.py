@@ -445,7 +445,8 @@ def op_cache_write(cache, k, v, row_start, first_pos):
 
 def op_cache_read(cache, row_start, first_pos, n_rows, dtype=None, out=None):
     """-> (k, v) [n_rows, n_kv_heads, head_dim] of `dtype` (bfloat16 unless given): what is stored at positions first_pos[b] + i of sequence
-    b, in rows row_start[b] + i.  out: a pair of such tensors to write to.  Rows of no sequence are not written."""
+    b, in rows row_start[b] + i, and zeros for what is outside the cache.  out: a pair of such tensors to write to.  Rows of no sequence are not
+    written."""
     import torch
     device = _device_of(cache._page_table, row_start, first_pos, *(out or ()))
     shape = (n_rows, cache.n_kv_heads, cache.head_dim)
@@ -546,8 +547,8 @@ def _attention_bytes(sizes, heads, max_rows, max_ctx):
 def op_tree_attention(q, cache, row_start, ctx_len, mask=None, max_rows=None, max_ctx=None, scale=0.0, out=None, workspace=None):
     """Attention of q [rows, heads, head_dim] over the cache: row row_start[b] + i (position ctx_len[b] + i) sees positions [0, ctx_len[b])
     and the nodes whose bits are set in its row of mask, int32 or uint32 [rows, words]; without a mask nodes 0 .. i.  max_rows: no tree has more
-    (default: all rows); max_ctx: what ctx_len is expected to reach (default: what the page table holds).  -> out like q; rows of no sequence
-    are not written."""
+    (default: all rows); max_ctx: what ctx_len is expected to reach (default: what the page table holds).  The work is divided by these two: for several
+    sequences the defaults launch for more than is there, so say them.  -> out like q; rows of no sequence are not written."""
     import torch
     device = _device_of(cache._page_table, q, row_start, ctx_len, mask, out, workspace)
     code, shape, hd = _row_code(q, "q"), q.shape, cache.head_dim
@@ -589,7 +590,8 @@ def _verify_bytes(rows, seqs, vocab):
 def op_tree_verify(tokens, parents, row_start, p, q, accept_words, draw_words, max_rows=None, max_path=None, workspace=None):
     """Verifies trees of drafted tokens: tokens, parents int32 [rows]; p (and q, or None) float32 [rows, vocab], rows may be strided; accept_words
     [rows], the bits of 32-bit words (int32 or uint32); draw_words [n_seqs], of 64-bit words.  -> (path int32 [n_seqs, max_path], path_len int32
-    [n_seqs], next_token int32 [n_seqs])."""
+    [n_seqs], next_token int32 [n_seqs]).  max_rows: no tree has more (default: all rows, at most 1024, with a workgroup launched for each of every sequence);
+    max_path: nodes that a path has room for (default: max_rows)."""
     import torch
     device = _device_of(p, tokens, parents, row_start, q, accept_words, draw_words, workspace)
     rows, seqs, shape = tokens.shape[0], row_start.shape[0] - 1, p.shape

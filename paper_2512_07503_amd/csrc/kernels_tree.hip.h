@@ -403,11 +403,11 @@ SJD_D void tree_finish(const TreeArgs &a, const TreeSeq &s, int kvh, size_t slot
 
 // --------------------------------------------------------------------------------------------------- wavefronts over tokens
 // Workgroup = tile of 32 rows, of a split; its wavefronts take the blocks in turn and merge through LDS.  For few rows: what bounds it is
-// the stream of keys and values.  Four fp8 sequences of 24 000 - 42 000 tokens, 8 kv heads of 128, a token each: 234 MB in 46.1 us, 5.1 TB/s, where a
-// copy reaches 5.5.  Eight bf16 trees of 13 - 53 nodes over 850 - 3 850 tokens, 32 heads of 128: 216 MB in 49.3 us, 4.4 TB/s.  With many rows
-// it is the vector unit: sixteen fp8 trees of 44 - 78 nodes, 4 query heads a kv head, over 5 200 - 11 200 tokens, 94 GFLOP in 178 us, 0.53 PFLOP/s (a
-// large product reaches 1.43): per 32 x 32 scores a lane has 16 exponentials, 8 pairs to round and 64 pairs of codes to widen next to its 16 products, more
-// cycles than the products take.  Tried: one line of all sequences' blocks cut into equal shares, 53.7 us for the first, 67.7 for the second,
+// the stream of keys and values.  Four fp8 sequences of 24 000 - 42 000 tokens, 8 kv heads of 128, a token each: 234 MB in 46.2 us, 5.1 TB/s, where a
+// copy reaches 5.5.  Eight bf16 trees of 13 - 53 nodes over 850 - 3 850 tokens, 32 heads of 128: 216 MB in 49.5 us, 4.4 TB/s.  With many rows it is
+// the order of a block's steps: sixteen fp8 trees of 44 - 78 nodes, 4 query heads a kv head, over 5 200 - 11 200 tokens, 94 GFLOP in 187 us, 0.5 PFLOP/s (a
+// large product reaches 1.41).  Scores, softmax and output follow each other, with two wavefronts a SIMD to fill the gaps: of the cycles in which a CU has work
+// its matrix cores are busy for 31 %, its vector units for 55 %.  Tried: one line of all sequences' blocks cut into equal shares, 53.7 us for the first, 67.7 for the second,
 // as a share then joins several sequences; two tiles of rows a wavefront, 427 us for the third, one wavefront a SIMD and copies between register files.
 constexpr int kTreeWaves = 4;
 
@@ -539,10 +539,10 @@ static_assert(kTreeWaves == 4, "a wavefront adds one quad of a lane's 16 accumul
 
 // ------------------------------------------------------------------------------------------------------ wavefronts over rows
 // bf16 caches.  Workgroup = a tile of 32 rows for each of its four wavefronts, of a split: every block is fetched once for all of them and read
-// from LDS, in the layout of its page, by every wavefront.  Bound by the softmax's arithmetic and the matrix cores, so a wavefront keeps both
-// busy: while it turns block j's scores into probabilities, the matrix cores work on the scores of block j + 1 and the output of block j - 1,
-// one product between every few instructions.  Sixteen bf16 trees of 44 - 78 nodes, 4 query heads a kv head of 128, over 5 200 - 11 200 tokens, 94 GFLOP:
-// 177 - 200 us, 0.5 PFLOP/s (by tokens: 240); the softmax's share of the vector unit is what is left.
+// from LDS, in the layout of its page, by every wavefront.  While a wavefront turns block j's scores into probabilities, the matrix cores work on
+// the scores of block j + 1 and the output of block j - 1, one product between every few instructions.  Sixteen bf16 trees of 44 - 78 nodes, 4 query heads a kv head
+// of 128, over 5 200 - 11 200 tokens, 94 GFLOP: 179 us, 0.53 PFLOP/s (by tokens: 207).  Bound by what comes ahead of that in every round, the barrier and the reads of the
+// operands from LDS: of the cycles in which a CU has work its LDS is busy for 43 %, its vector units for 35 %, its matrix cores for 33 %.
 constexpr int kTreeRowWaves = 4, kTreeRowThreads = 64 * kTreeRowWaves;
 constexpr int kTreeRing = 4;     // blocks in LDS: the last one's values, this one, the next one's keys, and the one that is being written
 

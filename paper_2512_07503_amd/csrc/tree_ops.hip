@@ -97,9 +97,10 @@ int check_rows(const sjd_kv_cache *cache, int32_t dtype, const void *k, const vo
 struct TreePlan { int tiles, groups, n_splits; bool by_rows; size_t part_o, part_ml; };
 
 // Which kernel, and how many ways a context is split.  By rows, where a bf16 cache has more than two tiles of 32 rows a kv head: four tiles a
-// workgroup share what is fetched (16 sequences of about 7 000 tokens, 8 kv heads of 128, 244 rows: 177 us against 240 by tokens, 80 rows: 98 against
-// 130; one of 2 300 with 32 heads of 96 rows: 27 against 29).  With fp8, whose conversions it does not save a wavefront but moves, it was no
-// faster (185 against 197 us of 128-wide heads, 151 against 110 of 64-wide ones).
+// workgroup share what is fetched (by rows against by tokens, calls in turn: 16 sequences of 7 000 tokens, 8 kv heads of 128, 244 rows: 187 us against 225, 80
+// rows: 103 against 126; 5 200 - 11 200 tokens and 176 - 312 rows: 179 against 207; one of 2 300 with 32 heads of 96 rows: 26.9 against 28.2).  A variant by rows for fp8,
+// whose conversions it does not save a wavefront but moves, was slower and is not here any more (185 us against 178 then for the sixteen sequences, with
+// heads of 64 151 against 110).
 TreePlan tree_plan(const sjd_kv_cache *c, int n_heads, int max_rows, int max_ctx) {
     TreePlan p;
     const int G = n_heads / c->n_kv_heads;

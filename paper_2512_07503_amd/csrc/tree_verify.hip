@@ -12,8 +12,8 @@
 // What a node decides follows from its own rows alone, so all nodes are decided at once, and the path is walked afterwards. A first child
 // takes two values; a sum over the vocabulary is needed only for a second child whose first sibling was rejected, at a node that is
 // not ruled out by the first children above it.  Bound by latency: two rows a sequence are all that has to be read, but
-// what a node needs next is known only when its last sum is: 16 trees of 61 nodes over 65 536 ids, 36 + 7.2 + 7.2 us for the three launches; one window of
-// 16 over 16 384 ids, 3.3 + 5.0 + 5.5 us.
+// what a node needs next is known only when its last sum is: 16 trees of 61 nodes over 65 536 ids, 36.4 + 7.2 + 7.4 us for the three launches; one window of
+// 16 over 16 384 ids, 3.4 + 5.0 + 5.6 us.
 //
 // This translation unit must be compiled with -ffp-contract=off.
 #include "cache_layout.h"
