@@ -440,6 +440,52 @@ int sjd_op_tree_verify(void *hip_stream, const int32_t *tokens, const int32_t *p
                        int32_t *path, int32_t *path_len, int32_t *next_token, int32_t n_rows, int32_t n_seqs, int32_t vocab,
                        int32_t max_rows, int32_t max_path, void *workspace, uint64_t workspace_bytes);
 
+/* ---- operators of scoring and prefilling prompts: norms of queries and keys with their rotary positions, attention of packed prompts, log
+ * probabilities of their tokens.  They are called as those of tree speculation above are: nothing is allocated, work is enqueued on `hip_stream`, pointers are DEVICE
+ * pointers on its device, which is the current one, sizes and pointers are checked on the host, and what is in device memory by the kernels. */
+
+/* sjd_op_rotary of heads that are normalised first, in one pass: y = (x - c) / sqrt(mean((x - c)^2) + eps) * gain + bias over the head_dim
+ * elements of a head, c = 0 (SJD_NORM_RMS) or their mean (SJD_NORM_LAYER); then pairs of y are turned, and multiplied by `magnitude`, the other
+ * dimensions are y.  Gains and biases of `dtype`: [head_dim] for all heads, or, with per_head, [heads][head_dim]; a bias may be NULL.  All of it is in fp32, rounded
+ * once at the end; any finite x is right, also where its square is beyond fp32 (eps then counts as nothing); a head with an infinity or NaN has NaN in it.  1e-30 <= eps.  The other arguments and
+ * conditions are those of sjd_op_rotary (in place included); outputs may not overlap gains and biases. */
+enum sjd_head_norm { SJD_NORM_RMS = 0, SJD_NORM_LAYER = 1 };
+int sjd_op_norm_rotary(void *hip_stream, int32_t dtype, int32_t norm, float eps, int32_t per_head, int32_t interleaved, const uint64_t *table,
+                       int32_t rotary_dim, float magnitude, const int32_t *positions, int32_t n_rows, int32_t head_dim, const void *q, int64_t q_stride,
+                       const void *q_gain, const void *q_bias, void *q_out, int64_t q_out_stride, int32_t n_heads, const void *k, int64_t k_stride,
+                       const void *k_gain, const void *k_bias, void *k_out, int64_t k_out_stride, int32_t n_kv_heads);
+
+/* Causal attention of packed prompts.  Sequence b's queries are rows [row_start[b], row_start[b + 1]) of q, its keys and values rows
+ * [kv_start[b], kv_start[b + 1]) of k and v (kv_start NULL: the same rows, and n_kv_rows is not read), of which the last are its queries' own: of n queries and t
+ * keys query i sees keys 0 .. i + t - n, so that a prompt may go on behind what is cached.  (row_start and kv_start have n_seqs + 1 entries, ascending; what lies outside [0, n_rows]
+ * or [0, n_kv_rows] is cut off.)  Row by row out = softmax(scale * q k) v with one kv head to n_heads / n_kv_heads query heads; a query that sees nothing (t < n) gets
+ * zeros.  Keys and values that a query does not see do not touch it, infinities and NaN included; an infinite value that it does see makes its result
+ * infinite, and may make it NaN where its weight is below what fp32 holds.  Rows of no sequence are left as they were.
+ * q and out [n_rows][n_heads][head_dim], k and v [n_kv_rows][n_kv_heads][head_dim] of `dtype` (SJD_F32 or SJD_BF16; a row's heads are contiguous, rows a stride
+ * apart: parts of a fused projection); head_dim 32, 64, 96, 128, 192 or 256.  Sums are fp32; for SJD_BF16 probabilities are rounded to bf16 for the products
+ * with values and for the sum that divides.  out may be q with the same stride, and may not overlap it otherwise, nor k and v.  scale > 0, or 0 for 1 / sqrt(head_dim).
+ * max_rows, max_kv: what a sequence's queries and keys are expected to reach; they only choose how the work is divided, and with it the order of
+ * sums.  Workspace (16-byte aligned): the bytes that sjd_op_prompt_attention_workspace writes to *bytes (HOST; may be 0) for the same
+ * arguments.  SJD_ECAPACITY: it is smaller. */
+int sjd_op_prompt_attention_workspace(int32_t dtype, int32_t n_rows, int32_t n_seqs, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_rows,
+                                      int32_t max_kv, uint64_t *bytes);
+int sjd_op_prompt_attention(void *hip_stream, int32_t dtype, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                            void *out, int64_t out_stride, const int32_t *row_start, const int32_t *kv_start, int32_t n_rows, int32_t n_kv_rows, int32_t n_seqs,
+                            int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, float scale, int32_t max_rows, int32_t max_kv, void *workspace,
+                            uint64_t workspace_bytes);
+
+/* Log probabilities.  Row r of logits [n_rows][vocab] (SJD_F32 or SJD_BF16, rows `stride` elements apart), p = softmax of it:
+ *   logprob[r] = ln p(tokens[r]), rank[r] = number of ids that are likelier, or as likely and lower; for a token outside [0, vocab) -inf and -1;
+ *   entropy[r] = - sum p ln p;
+ *   top_ids, top_logprobs [n_rows][n_top]: the likeliest ids, the lower one first where they are as likely, and their ln p; -1 and -inf behind the last id whose logit
+ *   is above -inf.
+ * Logits may be -inf (masked ids); of a row that is -inf altogether every ln p is -inf and the entropy is 0.  A row that holds a NaN or +inf has NaN for its numbers, -1 for
+ * its top_ids, and no meaning in its rank.  Sums are fp32.  n_top 0 .. 64 (0: top_ids and top_logprobs may be NULL); vocab <= 2^24.  Outputs may not overlap each
+ * other or an input.  Workspace as in sjd_op_prompt_attention. */
+int sjd_op_token_logprobs_workspace(int32_t n_rows, int32_t vocab, int32_t n_top, uint64_t *bytes);
+int sjd_op_token_logprobs(void *hip_stream, int32_t dtype, const void *logits, int64_t stride, const int32_t *tokens, float *logprob, int32_t *rank, float *entropy,
+                          int32_t *top_ids, float *top_logprobs, int32_t n_rows, int32_t vocab, int32_t n_top, void *workspace, uint64_t workspace_bytes);
+
 #ifdef __cplusplus
 }
 #endif

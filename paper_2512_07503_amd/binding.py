@@ -107,6 +107,11 @@ def lib():
         L.sjd_op_tree_attention.argtypes = [P, CP, I, P, I64, P, I64, P, P, P, I, I, I, C.c_float, I, I, P, C.c_uint64]
         L.sjd_op_tree_verify_workspace.argtypes = [I, I, I, U64P]
         L.sjd_op_tree_verify.argtypes = [P, P, P, P, P, I64, P, I64, P, P, P, P, P, I, I, I, I, I, P, C.c_uint64]
+        L.sjd_op_norm_rotary.argtypes = [P, I, I, C.c_float, I, I, P, I, C.c_float, P, I, I, P, I64, P, P, P, I64, I, P, I64, P, P, P, I64, I]
+        L.sjd_op_prompt_attention_workspace.argtypes = [I, I, I, I, I, I, I, I, U64P]
+        L.sjd_op_prompt_attention.argtypes = [P, I, P, I64, P, I64, P, I64, P, I64, P, P, I, I, I, I, I, I, C.c_float, I, I, P, C.c_uint64]
+        L.sjd_op_token_logprobs_workspace.argtypes = [I, I, I, U64P]
+        L.sjd_op_token_logprobs.argtypes = [P, I, P, I64, P, P, P, P, P, P, I, I, I, P, C.c_uint64]
         _lib = L
     return _lib
 
@@ -615,3 +620,129 @@ def op_tree_verify(tokens, parents, row_start, p, q, accept_words, draw_words, m
              _vector(draw_words, seqs, torch.uint64 if draw_words.dtype is torch.uint64 else torch.int64, "draw_words"), path.data_ptr(), path_len.data_ptr(),
              token.data_ptr(), rows, seqs, shape[1], max_rows, max_path, at, size)
     return path, path_len, token
+
+
+# ---- operators of scoring and prefilling prompts
+
+_NORMS = {"rms": 0, "layer": 1}
+
+
+def _head_vector(t, like, heads, hd, name):
+    """-> (pointer, 0: one for all heads or 1: one for each) of a gain or bias."""
+    shape = t.shape
+    if t.dtype is not like.dtype or shape[-1:] != (hd,) or len(shape) > 2 or (len(shape) == 2 and shape[0] != heads) or not t.is_contiguous():
+        _refuse(f"{name} must be a contiguous [{hd}] or [{heads}, {hd}] of the rows' dtype")
+    return t.data_ptr(), len(shape) - 1
+
+
+def op_norm_rotary(q, k, positions, table, q_gain, k_gain=None, q_bias=None, k_bias=None, norm="rms", eps=1e-5, interleaved=False, magnitude=1.0, out=None):
+    """op_rotary of heads that are normalised first: norm "rms" or "layer" (the mean is taken off), gains and biases (a bias may be None) of q's dtype,
+    [hd] for all heads or [heads, hd], all of them alike.  q [rows, heads, hd], k [rows, kv_heads, hd] or None -> (q', k').  out: tensors to write to, which may
+    be q and k themselves."""
+    import torch
+    if norm not in _NORMS:
+        _refuse("norm must be rms or layer")
+    device = _device_of(q, k, positions, table, q_gain, k_gain, q_bias, k_bias, *(out or ()))
+    code, shape = _row_code(q, "q"), q.shape
+    if len(shape) != 3:
+        _refuse("q must be [rows, heads, head_dim]")
+    rows, heads, hd = shape
+    if out is None:
+        q_out, k_out = q.new_empty(shape), None if k is None else k.new_empty(k.shape)
+    else:
+        q_out, k_out = out[0], out[1] if len(out) > 1 else None
+        if (k_out is None) != (k is None) or q_out.dtype is not q.dtype or q_out.shape[0] != rows or (k is not None and (k_out.dtype is not q.dtype or k_out.shape != k.shape)):
+            _refuse("out must have the shapes and dtype of q and k")
+    gain, per_head = _head_vector(q_gain, q, heads, hd, "q_gain")
+    bias, kinds = None, {per_head}
+    if q_bias is not None:
+        bias, kind = _head_vector(q_bias, q, heads, hd, "q_bias")
+        kinds.add(kind)
+    if k is None:
+        if k_gain is not None or k_bias is not None:
+            _refuse("a gain or a bias without k")
+        keys = (None, 0, None, None, None, 0, 0)
+    else:
+        if k.dtype is not q.dtype or k.shape[0] != rows or k.dim() != 3:
+            _refuse("k must have q's dtype and number of rows")
+        if k_gain is None:
+            _refuse("k_gain is missing")
+        n, k_bias_ptr = k.shape[1], None
+        k_gain_ptr, kind = _head_vector(k_gain, q, n, hd, "k_gain")
+        kinds.add(kind)
+        if k_bias is not None:
+            k_bias_ptr, kind = _head_vector(k_bias, q, n, hd, "k_bias")
+            kinds.add(kind)
+        keys = (k.data_ptr(), _row_stride(k, n, hd, "k"), k_gain_ptr, k_bias_ptr, k_out.data_ptr(), n * hd if out is None else _row_stride(k_out, n, hd, "out"), n)
+    if len(kinds) > 1:
+        _refuse("gains and biases must all be [hd] or all [heads, hd]")
+    _enqueue(device, lib().sjd_op_norm_rotary, code, _NORMS[norm], eps, per_head, 1 if interleaved else 0, _vector(table, None, torch.int64, "table"), 2 * table.shape[0],
+             magnitude, _vector(positions, rows, torch.int32, "positions"), rows, hd, q.data_ptr(), _row_stride(q, heads, hd, "q"), gain, bias, q_out.data_ptr(),
+             heads * hd if out is None else _row_stride(q_out, heads, hd, "out"), heads, *keys)
+    return q_out, k_out
+
+
+@functools.lru_cache(maxsize=256)
+def _prompt_bytes(*sizes):
+    n = C.c_uint64(0)
+    _check(lib().sjd_op_prompt_attention_workspace(*sizes, C.byref(n)))
+    return n.value
+
+
+def op_prompt_attention(q, k, v, row_start, kv_start=None, max_rows=None, max_kv=None, scale=0.0, out=None, workspace=None):
+    """Causal attention of packed prompts: q [rows, heads, head_dim], k and v [kv_rows, kv_heads, head_dim] (rows may be strided).  Sequence b's queries are rows
+    row_start[b] .. row_start[b + 1] - 1, its keys rows kv_start[b] .. (the same rows without a kv_start), the last of which are its queries' own: query i of n sees the
+    first i + 1 + t - n of t keys.  row_start, kv_start int32 [n_seqs + 1].  max_rows, max_kv: what a sequence's queries and keys are expected to reach (default: all rows); they
+    only choose how the work is divided.  -> out like q; rows of no sequence are not written."""
+    import torch
+    device = _device_of(q, k, v, row_start, kv_start, out, workspace)
+    code, shape = _row_code(q, "q"), q.shape
+    if len(shape) != 3 or k.dim() != 3 or v.shape != k.shape:
+        _refuse("q must be [rows, heads, head_dim], k and v [rows, kv_heads, head_dim]")
+    if k.dtype is not q.dtype or v.dtype is not q.dtype:
+        _refuse("q, k and v must have one dtype")
+    (rows, heads, hd), (kv_rows, kv_heads, _), seqs = shape, k.shape, row_start.shape[0] - 1
+    if kv_start is None and kv_rows != rows:
+        _refuse("without kv_start k and v have q's rows")
+    strides = _row_stride(q, heads, hd, "q"), _row_stride(k, kv_heads, hd, "k"), _row_stride(v, kv_heads, hd, "v")
+    if out is None:
+        out, out_stride = q.new_empty(shape), heads * hd
+    else:
+        if out.dtype is not q.dtype or out.shape != shape:
+            _refuse("out must be like q")
+        out_stride = _row_stride(out, heads, hd, "out")
+    if max_rows is None:
+        max_rows = rows
+    if max_kv is None:
+        max_kv = kv_rows
+    at, size, keep = _workspace(workspace, _prompt_bytes(code, rows, seqs, heads, kv_heads, hd, max_rows, max_kv), q)
+    _enqueue(device, lib().sjd_op_prompt_attention, code, q.data_ptr(), strides[0], k.data_ptr(), strides[1], v.data_ptr(), strides[2], out.data_ptr(), out_stride,
+             _vector(row_start, seqs + 1, torch.int32, "row_start"), None if kv_start is None else _vector(kv_start, seqs + 1, torch.int32, "kv_start"), rows, kv_rows, seqs,
+             heads, kv_heads, hd, scale, max_rows, max_kv, at, size)
+    return out
+
+
+@functools.lru_cache(maxsize=256)
+def _logprob_bytes(rows, vocab, n_top):
+    n = C.c_uint64(0)
+    _check(lib().sjd_op_token_logprobs_workspace(rows, vocab, n_top, C.byref(n)))
+    return n.value
+
+
+def op_token_logprobs(logits, tokens, n_top=0, workspace=None):
+    """Log probabilities of tokens int32 [rows] under logits [rows, vocab] (float32 or bfloat16, rows may be strided; -inf masks an id) -> (logprob float32 [rows], rank
+    int32 [rows], entropy float32 [rows], top_ids int32 [rows, n_top], top_logprobs float32 [rows, n_top]).  rank: number of likelier ids, of equal ones those that are lower.
+    n_top <= 64.  A token outside the vocabulary has -inf and rank -1; alternatives that there are not, -1 and -inf; rows with a NaN or +inf, NaN."""
+    import torch
+    device = _device_of(logits, tokens, workspace)
+    code, shape = _row_code(logits, "logits"), logits.shape
+    if len(shape) != 2 or (shape[1] != 1 and logits.stride(1) != 1):
+        _refuse("logits must be [rows, vocab] with contiguous rows")
+    rows, vocab = shape
+    tokens_ptr, need = _vector(tokens, rows, torch.int32, "tokens"), _logprob_bytes(rows, vocab, n_top)
+    logprob, rank = torch.empty(rows, dtype=torch.float32, device=logits.device), tokens.new_empty(rows)
+    entropy, ids, top = logprob.new_empty(rows), rank.new_empty((rows, n_top)), logprob.new_empty((rows, n_top))
+    at, size, keep = _workspace(workspace, need, logits)
+    _enqueue(device, lib().sjd_op_token_logprobs, code, logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, tokens_ptr, logprob.data_ptr(), rank.data_ptr(),
+             entropy.data_ptr(), ids.data_ptr(), top.data_ptr(), rows, vocab, n_top, at, size)
+    return logprob, rank, entropy, ids, top

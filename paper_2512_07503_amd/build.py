@@ -15,7 +15,7 @@ COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-
           "-mllvm", "-amdgpu-kernarg-preload-count=14"]
 # (source, extra flags): the decision stage and the verification of trees are specified bit for bit and must not contract a*b+c
 UNITS = [("decide.hip", ["-ffp-contract=off"]), ("sjd_api.hip", []), ("tree_ops.hip", []),
-         ("tree_verify.hip", ["-ffp-contract=off"])]
+         ("tree_verify.hip", ["-ffp-contract=off"]), ("prompt_ops.hip", [])]
 
 
 def build(verbose: bool = False) -> str:

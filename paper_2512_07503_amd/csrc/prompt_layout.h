@@ -1,0 +1,44 @@
+// How attention of packed prompts is divided (kernels_prompt.hip.h).  Plain C++ (constexpr: host and device), so that a test can play
+// it through without a GPU.
+//
+// The query rows (i, h) of one kv head of a sequence, ordered by i, then by the query head h of the group of G, are cut into tiles of `tile` rows.  The keys that a
+// tile sees are cut into blocks, and those of long ones into splits.
+#pragma once
+#include "cache_layout.h"
+
+// keys that come before a sequence's first query's own: query i sees keys 0 .. i + prompt_offset (negative: its first queries see nothing)
+constexpr int prompt_offset(int n, int n_keys) { return n_keys - n; }
+
+// tiles of n rows
+constexpr int prompt_tiles(int n, int G, int tile) { return (int)(((long)n * G + tile - 1) / tile); }
+// and an upper bound over n_rows rows of n_seqs sequences
+constexpr long prompt_max_tiles(long n_rows, long n_seqs, int G, int tile) {
+    return n_rows * G / tile + (n_seqs < n_rows ? n_seqs : n_rows);
+}
+// keys that some row of tile t of a sequence sees: 0 .. prompt_keys - 1
+constexpr int prompt_keys(int t, int n, int n_keys, int G, int tile) {
+    const long last = ((long)(t + 1) * tile - 1) / G;
+    const int i = last < n ? (int)last : n - 1;
+    const int seen = i + 1 + prompt_offset(n, n_keys);
+    return seen < 0 ? 0 : seen;
+}
+// Blocks [first, last) of split `split` of at most n_splits, of `per` blocks each (the last of all takes what is left), and whether there is more than one split
+struct PromptBlocks { int first, last; bool any, several; };
+constexpr PromptBlocks prompt_blocks(int n_keys_seen, int block, int split, int n_splits, int per) {
+    const int blocks = (n_keys_seen + block - 1) / block;
+    PromptBlocks r{0, blocks, split == 0, false};
+    if (n_splits == 1) return r;
+    const int splits = blocks <= per ? 1 : (blocks + per - 1) / per < n_splits ? (blocks + per - 1) / per : n_splits;
+    r.several = splits > 1;
+    r.any = split < splits;
+    r.first = split * per < blocks ? split * per : blocks;
+    if (split + 1 < splits) r.last = r.first + per;
+    return r;
+}
+
+// Where the 16-byte piece c of token t's row of row_bytes lies within a block in LDS: at piece prompt_swizzle(...) of the row.  Reads of a piece of
+// 8 tokens in a row, and of 64 bytes of 4 tokens, then go to different banks; rows of an odd multiple of 64 bytes do so half by themselves.
+constexpr int prompt_swizzle(int t, int c, int row_bytes) {
+    const int s = row_bytes % 128 == 64 ? 0 : row_bytes % 256 == 128 ? (t >> 1) & 1 : t & 3;
+    return c ^ (s << 2 | ((t >> 2) & 3));
+}

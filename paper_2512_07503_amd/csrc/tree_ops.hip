@@ -5,21 +5,10 @@
 #include "kernels_cache.hip.h"
 #include "kernels_rotary.hip.h"
 #include "kernels_tree.hip.h"
+#include "rotary_args.h"
 #include "tree_ops.h"
 
 namespace {
-
-#define TREE_FAIL(code, ...)                            \
-    do {                                                \
-        sjd_set_error(sjd_call_error(), __VA_ARGS__);   \
-        return code;                                    \
-    } while (0)
-#define TREE_TRY(expr) SJD_HIP_TRY(sjd_call_error(), expr)
-
-// A launch has at most 2^32 - 1 work-items a dimension: so many workgroups of 256
-constexpr size_t kMaxWorkgroups = (1u << 24) - 1;
-
-bool wide(const void *p, int64_t stride, int size, int bytes) { return (uintptr_t)p % bytes == 0 && stride * size % bytes == 0; }
 
 int check_shape(const sjd_kv_cache *c) {
     if (!c) TREE_FAIL(SJD_EINVAL, "null cache");
@@ -69,17 +58,6 @@ int head_group(const sjd_kv_cache *c, int n_rows) {
     return 2 * cache_max_tiles(n_rows, c->n_seqs) * c->n_kv_heads >= 4096 ? cache_heads(c->head_dim) : 1;
 }
 unsigned head_groups(const sjd_kv_cache *c, int group) { return (unsigned)(c->n_kv_heads + group - 1) / group; }
-
-// Do n_rows rows of x and of y, x_row and y_row elements long, have no element in common?  (Rows with the same stride may interleave: parts of a
-// fused projection.)
-bool rows_apart(const void *x, long x_stride, long x_row, const void *y, long y_stride, long y_row, int n_rows, int size) {
-    const uintptr_t x0 = (uintptr_t)x, x1 = x0 + ((uintptr_t)(n_rows - 1) * x_stride + x_row) * size;
-    const uintptr_t y0 = (uintptr_t)y, y1 = y0 + ((uintptr_t)(n_rows - 1) * y_stride + y_row) * size;
-    if (x1 <= y0 || y1 <= x0) return true;
-    if (n_rows == 1 || x_stride != y_stride || x_stride <= 0) return false;
-    const long d = ((long)(y0 - x0) / size % x_stride + x_stride) % x_stride;   // where y's row starts within x's
-    return d >= x_row && d + y_row <= x_stride;
-}
 
 int check_rows(const sjd_kv_cache *cache, int32_t dtype, const void *k, const void *v, const int32_t *row_start, const int32_t *first_pos, int32_t n_rows) {
     const int rc = check_cache(cache);
@@ -184,7 +162,7 @@ int sjd_op_cache_read(void *hip_stream, const sjd_kv_cache *cache, int32_t dst_d
     if (!n_rows) return SJD_OK;
     const int size = dst_dtype == SJD_F32 ? 4 : 2;
     const long stride = (long)cache->n_kv_heads * cache->head_dim;
-    if (!rows_apart(k, stride, stride, v, stride, stride, n_rows, size)) TREE_FAIL(SJD_EINVAL, "k and v overlap");
+    if (!rows_apart(k, stride, stride, n_rows, v, stride, stride, n_rows, size)) TREE_FAIL(SJD_EINVAL, "k and v overlap");
     const CacheRowsArgs a = {view(cache), row_start, first_pos, k, v, stride, stride, n_rows, head_group(cache, n_rows), wide(k, stride, size, 16), wide(v, stride, size, 16)};
     TREE_TRY(launch_rows<ReadRows>((hipStream_t)hip_stream, dim3((unsigned)cache_max_tiles(n_rows, cache->n_seqs), head_groups(cache, a.group), 2), cache->dtype,
                                    dst_dtype, a));
@@ -236,42 +214,13 @@ int sjd_op_rotary(void *hip_stream, int32_t dtype, int32_t interleaved, const ui
                   const int32_t *positions, int32_t n_rows, int32_t head_dim, const void *q, int64_t q_stride, void *q_out,
                   int64_t q_out_stride, int32_t n_heads, const void *k, int64_t k_stride, void *k_out, int64_t k_out_stride,
                   int32_t n_kv_heads) {
-    if (dtype != SJD_F32 && dtype != SJD_BF16) TREE_FAIL(SJD_EINVAL, "rows are SJD_F32 or SJD_BF16");
-    if (head_dim < 2 || head_dim > 2 * kRotaryMaxHalf || rotary_dim < 2 || rotary_dim % 2 || rotary_dim > head_dim)
-        TREE_FAIL(SJD_EINVAL, "rotary_dim must be even and 2 .. head_dim, head_dim at most 512");
-    if (n_heads < 1 || n_kv_heads < 0 || n_heads > 1 << 16 || n_kv_heads > 1 << 16 || n_rows < 0 || n_rows > 1 << 29)
-        TREE_FAIL(SJD_EINVAL, "n_heads must be 1 .. 65536, n_kv_heads 0 .. 65536, n_rows 0 .. 2^29");
-    if (!table || (n_rows && (!positions || !q || !q_out || (n_kv_heads && (!k || !k_out))))) TREE_FAIL(SJD_EINVAL, "null argument");
-    const int size = dtype == SJD_F32 ? 4 : 2;
     RotaryArgs a = {table, positions, {q, k}, {q_out, k_out}, {(long)q_stride, (long)k_stride}, {(long)q_out_stride, (long)k_out_stride},
                     {n_heads, n_kv_heads}, n_rows, head_dim, rotary_dim / 2, interleaved ? 1 : 0, 1, magnitude};
-    bool w = interleaved ? head_dim % 8 == 0 : a.half % 8 == 0 && (head_dim - rotary_dim) % 8 == 0;
-    for (int s = 0; s < 2; ++s) {
-        const long row = (long)a.heads[s] * head_dim;
-        if (!row || !n_rows) continue;
-        if ((uintptr_t)a.x[s] % size || (uintptr_t)a.y[s] % size) TREE_FAIL(SJD_EINVAL, "rows are not aligned to their elements");
-        if (n_rows > 1 && a.y_stride[s] < row) TREE_FAIL(SJD_EINVAL, "output rows overlap");
-        if (n_rows > 1 && a.x_stride[s] < 0) TREE_FAIL(SJD_EINVAL, "negative stride");
-        w = w && wide(a.x[s], a.x_stride[s], size, 16) && wide(a.y[s], a.y_stride[s], size, 16);
-        for (int o = 0; o < 2; ++o) {
-            const long out_row = (long)a.heads[o] * head_dim;
-            const bool same = o == s && a.x[s] == a.y[s] && (a.x_stride[s] == a.y_stride[s] || n_rows == 1);
-            if (out_row && !same && !rows_apart(a.x[s], a.x_stride[s], row, a.y[o], a.y_stride[o], out_row, n_rows, size))
-                TREE_FAIL(SJD_EINVAL, "an output overlaps an input");
-        }
-    }
-    if (!n_rows) return SJD_OK;
-    if (n_kv_heads && !rows_apart(q_out, q_out_stride, (long)n_heads * head_dim, k_out, k_out_stride, (long)n_kv_heads * head_dim, n_rows, size))
-        TREE_FAIL(SJD_EINVAL, "q_out and k_out overlap");
-    // Rows a workgroup: their sines and cosines are shared by the heads of a row only, so more rows mean nothing but fewer workgroups;
-    // two for each of the 256 CUs, and few rows are split over their heads' units instead.
-    while (a.rows_per_wg < 8 && a.rows_per_wg * a.half * 2 <= 8 * kRotaryMaxHalf && n_rows / (2 * a.rows_per_wg) >= 512) a.rows_per_wg *= 2;
-    const unsigned gx = (unsigned)ceil_div(n_rows, a.rows_per_wg);
-    if (gx > kMaxWorkgroups) TREE_FAIL(SJD_EINVAL, "too many rows for one launch");
-    const long units = (long)a.rows_per_wg * (n_heads + n_kv_heads) * (w ? head_dim / 8 : head_dim);
-    long gy = gx >= 512 ? 1 : 512 / gx;
-    if (gy > (units + 255) / 256) gy = (units + 255) / 256;
-    const dim3 grid(gx, (unsigned)gy);
+    bool w;
+    const int rc = rotary_check(a, dtype, rotary_dim, w);
+    if (rc || !n_rows) return rc;
+    dim3 grid;
+    if (!rotary_grid(a, (long)(n_heads + n_kv_heads) * (w ? head_dim / 8 : head_dim), grid)) TREE_FAIL(SJD_EINVAL, "too many rows for one launch");
     hipStream_t st = (hipStream_t)hip_stream;
     if (dtype == SJD_F32) w ? rotary_kernel<float, true><<<grid, 256, 0, st>>>(a) : rotary_kernel<float, false><<<grid, 256, 0, st>>>(a);
     else w ? rotary_kernel<bf16_t, true><<<grid, 256, 0, st>>>(a) : rotary_kernel<bf16_t, false><<<grid, 256, 0, st>>>(a);
@@ -321,7 +270,7 @@ int sjd_op_tree_attention(void *hip_stream, const sjd_kv_cache *cache, int32_t d
     if (!n_rows) return SJD_OK;
     // in place: a workgroup has read its queries when it writes their results
     const long row = (long)n_heads * cache->head_dim;
-    if (!(q == out && (q_stride == out_stride || n_rows == 1)) && !rows_apart(q, q_stride, row, out, out_stride, row, n_rows, size))
+    if (!(q == out && (q_stride == out_stride || n_rows == 1)) && !rows_apart(q, q_stride, row, n_rows, out, out_stride, row, n_rows, size))
         TREE_FAIL(SJD_EINVAL, "the output overlaps the queries");
     const TreePlan p = tree_plan(cache, n_heads, max_rows, max_ctx);
     if (p.part_o + p.part_ml > workspace_bytes)

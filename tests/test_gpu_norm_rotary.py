@@ -1,0 +1,154 @@
+"""Norms of queries and keys with the rotary positions on the GPU, against 64 bits."""
+import numpy as np
+import pytest
+
+import prompt_oracle
+import tree_oracle
+
+pytestmark = pytest.mark.gpu
+
+
+def tensor(x, dtype):
+    import torch
+    t = torch.from_numpy(np.asarray(x, dtype=np.float32)).cuda()
+    return t if dtype == "f32" else t.bfloat16()
+
+
+def host(t):
+    return t.double().cpu().numpy()
+
+
+def check(got, x, gain, bias, layer, eps, positions, f, interleaved, magnitude, dtype):
+    """fp32: a sum of hd squares is hd 2^-24 off, relatively, its root half of that, and the division, the root, the product and the differences from the mean
+    round a handful of times: (hd + 16) 2^-24 of z, the normalised element.  The mean is, as far as it matters, hd 2^-24 of the mean magnitude of what is left, which is at most one
+    deviation: as much of 1.  Both times the gain; the bias rounds once more, then the turn takes 8 * 2^-24 of |a| + |b| of its pair, whose errors
+    it adds up; and half a step of the output's type."""
+    y, z = prompt_oracle.norm(host(x), host(gain), None if bias is None else host(bias), layer, eps)
+    want, size = tree_oracle.rotary(y, positions, f, interleaved, magnitude)
+    hd, r = x.shape[-1], 2 * len(f)
+    off = (hd + 16) * 2.0 ** -24 * (np.abs(z) + 1.0) * np.abs(host(gain)) + 2.0 ** -23 * np.abs(y)
+    a, b = (slice(0, r, 2), slice(1, r, 2)) if interleaved else (slice(0, r // 2), slice(r // 2, r))
+    both = magnitude * (off[..., a] + off[..., b])
+    off[..., a], off[..., b] = both, both
+    half = 2.0 ** -24 if dtype == "f32" else 2.0 ** -8
+    # (elements behind the turned part: their one rounding is in `half`)
+    tol = off + 8 * 2.0 ** -24 * size + half * np.abs(want) * (1 + 2.0 ** -7) + half * off + 1e-44
+    d = np.abs(host(got) - want) - tol
+    assert d.max() <= 0, (d.max(), np.unravel_index(d.argmax(), d.shape))
+
+
+SIZES = [(64, 64), (128, 128), (128, 64), (256, 256), (32, 32), (96, 96), (96, 80), (80, 30), (192, 192), (64, 2), (66, 66), (512, 512), (512, 16), (7, 4), (40, 40), (24, 8), (16, 16), (8, 8), (2, 2)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("hd,r", SIZES)
+def test_norm_rotary(dtype, interleaved, hd, r):
+    import paper_2512_07503_amd as sjd
+    import torch
+    rng = np.random.default_rng(hd + r)
+    f, table = tree_oracle.frequencies(r), sjd.rope_table(r)
+    for k, (n, H, Hk, norm, per_head, bias) in enumerate([(1, 1, 0, "rms", False, False), (5, 4, 2, "layer", True, True), (37, 6, 3, "rms", True, False), (700, 2, 1, "layer", False, True),
+                                                          (1100, 1, 1, "rms", False, True)]):
+        positions = rng.integers(-5, 1000000, n)
+        pos = torch.tensor(positions.astype(np.int32), device="cuda")
+        x = [tensor((rng.standard_normal((n, h, hd)) + 0.5) * np.exp(rng.standard_normal((1, h, 1))), dtype) for h in (H, Hk)]
+        shape = lambda h: (h, hd) if per_head else (hd,)
+        gain = [tensor(1 + 0.3 * rng.standard_normal(shape(h)), dtype) for h in (H, Hk)]
+        shift = [tensor(0.2 * rng.standard_normal(shape(h)), dtype) if bias else None for h in (H, Hk)]
+        kw = dict(norm=norm, eps=1e-5, interleaved=interleaved, magnitude=1.25)
+        if Hk:
+            out = sjd.op_norm_rotary(x[0], x[1], pos, table, gain[0], gain[1], q_bias=shift[0], k_bias=shift[1], **kw)
+        else:
+            out = sjd.op_norm_rotary(x[0], None, pos, table, gain[0], q_bias=shift[0], **kw)
+            assert out[1] is None
+        for i in range(2 if Hk else 1):
+            check(out[i], x[i], gain[i], shift[i], norm == "layer", 1e-5, positions, f, interleaved, 1.25, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+def test_in_place_within_a_fused_projection(dtype, norm):
+    """Queries and keys are parts of one buffer's rows; what lies beside them stays."""
+    import paper_2512_07503_amd as sjd
+    import torch
+    rng = np.random.default_rng(1)
+    for hd, pad in ((64, 0), (64, 3), (128, 8), (96, 0)):
+        buf = tensor(rng.standard_normal((9, 8 * hd + pad)), dtype)
+        old = buf.clone()
+        part = lambda b, lo, hi: b[:, lo * hd:hi * hd].unflatten(1, (hi - lo, hd))
+        q, k = part(buf, 0, 4), part(buf, 4, 6)
+        positions = np.arange(9) * 1000
+        gain, bias = tensor(rng.standard_normal(hd), dtype), tensor(rng.standard_normal(hd), dtype)
+        out = sjd.op_norm_rotary(q, k, torch.tensor(positions.astype(np.int32), device="cuda"), sjd.rope_table(hd), gain, gain, bias, bias, norm=norm, out=(q, k))
+        assert out[0].data_ptr() == q.data_ptr()
+        f = tree_oracle.frequencies(hd)
+        check(q, part(old, 0, 4), gain, bias, norm == "layer", 1e-5, positions, f, False, 1.0, dtype)
+        check(k, part(old, 4, 6), gain, bias, norm == "layer", 1e-5, positions, f, False, 1.0, dtype)
+        assert torch.equal(buf[:, 6 * hd:], old[:, 6 * hd:])
+
+
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+@pytest.mark.parametrize("hd,r", [(128, 128), (96, 50)])
+def test_far_from_the_middle(norm, hd, r):
+    """Elements whose squares are beyond fp32 or below it, a mean many times the deviation, heads of one value, heads of zeros."""
+    import paper_2512_07503_amd as sjd
+    import torch
+    rng = np.random.default_rng(3)
+    x = rng.standard_normal((8, 2, hd))
+    x[0] *= 1e38 / np.abs(x[0]).max()
+    x[1] *= 1e25
+    x[2] *= 1e-25
+    x[3] += 1000.0
+    x[4] = 12345.678
+    x[5] = 3e38
+    x[6] = 0.0
+    x[7, :, 1:] = 0.0
+    x[7, :, 0] = 2e38
+    t, gain = tensor(x, "f32"), tensor(np.ones(hd), "f32")
+    positions = np.zeros(8, dtype=np.int64)
+    got, _ = sjd.op_norm_rotary(t, None, torch.zeros(8, dtype=torch.int32, device="cuda"), sjd.rope_table(r), gain, norm=norm)
+    check(got, t, gain, None, norm == "layer", 1e-5, positions, tree_oracle.frequencies(r), False, 1.0, "f32")
+
+
+@pytest.mark.parametrize("hd", [64, 50])
+def test_infinities_and_nan_stay_in_their_head(hd):
+    import paper_2512_07503_amd as sjd
+    import torch
+    rng = np.random.default_rng(4)
+    x = rng.standard_normal((3, 8, hd))
+    clean = tensor(x, "bf16")
+    x[1, 2, 5], x[1, 6, 0], x[2, 7, hd - 1] = np.nan, np.inf, -np.inf
+    pos, table, gain = torch.arange(3, dtype=torch.int32, device="cuda"), sjd.rope_table(hd), tensor(np.ones(hd), "bf16")
+    for norm in ("rms", "layer"):
+        a, _ = sjd.op_norm_rotary(clean, None, pos, table, gain, norm=norm)
+        b, _ = sjd.op_norm_rotary(tensor(x, "bf16"), None, pos, table, gain, norm=norm)
+        hit = torch.zeros((3, 8), dtype=torch.bool, device="cuda")
+        hit[1, 2] = hit[1, 6] = hit[2, 7] = True
+        assert torch.equal(a[~hit], b[~hit]) and b[hit].isnan().any(dim=-1).all()
+
+
+def test_no_rows_and_many_rows():
+    import paper_2512_07503_amd as sjd
+    import torch
+    table, gain = sjd.rope_table(64), torch.ones(64, device="cuda")
+    q = torch.zeros((0, 2, 64), device="cuda")
+    assert sjd.op_norm_rotary(q, None, torch.zeros(0, dtype=torch.int32, device="cuda"), table, gain)[0].shape == (0, 2, 64)
+    n = 70001
+    q = torch.randn((n, 1, 64), device="cuda")
+    got, _ = sjd.op_norm_rotary(q, None, torch.arange(n, dtype=torch.int32, device="cuda"), table, gain)
+    pick = np.concatenate([np.arange(20), np.arange(n - 20, n), np.random.default_rng(0).integers(0, n, 200)])
+    check(got[pick], q[pick], gain, None, False, 1e-5, pick, tree_oracle.frequencies(64), False, 1.0, "f32")
+
+
+def test_is_the_norm_and_op_rotary():
+    """With a norm that changes nothing (elements of magnitude 1, a vanishing eps) it is op_rotary, to the norm's rounding."""
+    import paper_2512_07503_amd as sjd
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(5)
+    q = torch.where(torch.rand((40, 3, 128), generator=g, device="cuda") < 0.5, 1.0, -1.0)
+    pos = torch.arange(40, dtype=torch.int32, device="cuda") * 977
+    table = sjd.rope_table(64)
+    a, _ = sjd.op_rotary(q, None, pos, table)
+    b, _ = sjd.op_norm_rotary(q, None, pos, table, torch.ones(128, device="cuda"), eps=1e-30)
+    assert (a - b).abs().max().item() <= 8 * 2.0 ** -24      # a root and a quotient of 1, a step each, before the turn; sums of two

@@ -1,0 +1,86 @@
+"""The division of packed prompts' attention (csrc/prompt_layout.h, plain C++), compiled for the host: tiles, what they see, splits, places in LDS."""
+import os
+import subprocess
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2512_07503_amd", "csrc")
+_MAIN = r"""
+#include <cstdio>
+#include <cstdlib>
+#include <vector>
+#include "prompt_layout.h"
+#define CHECK(c) do { if (!(c)) { printf("line %d: %s\n", __LINE__, #c); exit(1); } } while (0)
+
+int main() {
+    srand(1);
+    // tiles: an upper bound over any cut of the rows; the keys that a tile's rows see
+    for (int it = 0; it < 20000; ++it) {
+        const int seqs = 1 + rand() % 9, G = 1 + rand() % 8, tile = 32 << rand() % 4;
+        long rows = 0, tiles = 0;
+        for (int b = 0; b < seqs; ++b) {
+            const int n = rand() % 3 ? rand() % 300 : 0, keys = rand() % 400;
+            rows += n;
+            const int t = prompt_tiles(n, G, tile);
+            CHECK((long)t * tile >= (long)n * G && (n == 0 ? t == 0 : (long)(t - 1) * tile < (long)n * G));
+            tiles += t;
+            for (int i = 0; i < t; ++i) {
+                int seen = 0;
+                for (int r = i * tile; r < (i + 1) * tile && r < n * G; ++r)
+                    for (int key = seen; key < keys; ++key)
+                        if (key <= r / G + prompt_offset(n, keys)) seen = key + 1;
+                CHECK(prompt_keys(i, n, keys, G, tile) == seen);
+            }
+        }
+        CHECK(tiles <= prompt_max_tiles(rows, seqs, G, tile));
+    }
+    CHECK(prompt_max_tiles(0, 5, 3, 128) == 0);
+    // splits go through every block once, whatever was expected of the number of keys
+    for (int it = 0; it < 200000; ++it) {
+        const int keys = rand() % 3000, block = 32 << rand() % 3, n_splits = 1 + rand() % 9, per = 1 + rand() % 20, blocks = (keys + block - 1) / block;
+        int at = 0, some = 0;
+        for (int s = 0; s < n_splits; ++s) {
+            const PromptBlocks r = prompt_blocks(keys, block, s, n_splits, per);
+            if (!r.any) continue;
+            CHECK(some == s && r.first == at && r.last >= r.first);
+            at = r.last;
+            ++some;
+        }
+        CHECK(at == blocks && some >= 1);
+        for (int s = 0; s < n_splits; ++s) CHECK(prompt_blocks(keys, block, s, n_splits, per).several == (some > 1));
+    }
+    // pieces of a row in LDS: each has a place in its row, and 8 tokens' pieces, and 64 bytes of 4 tokens, lie in different banks
+    for (int row : {64, 128, 192, 256, 384, 512, 768, 1024}) {
+        const int n = row / 16;
+        for (int t = 0; t < 64; ++t) {
+            std::vector<char> seen(n, 0);
+            for (int c = 0; c < n; ++c) {
+                const int p = prompt_swizzle(t, c, row);
+                CHECK(p >= 0 && p < n && !seen[p]);
+                seen[p] = 1;
+            }
+        }
+        auto bank = [&](int t, int c) { return (t * row / 16 + prompt_swizzle(t, c, row)) % 16; };      // of 16 bytes
+        for (int c = 0; c < n; ++c)
+            for (int t0 = 0; t0 < 64; t0 += 8) {
+                int used = 0;
+                for (int t = t0; t < t0 + 8; ++t) used |= 1 << bank(t, c);
+                CHECK(__builtin_popcount(used) == 8);
+            }
+        for (int c = 0; c < n; c += 4)
+            for (int t0 = 0; t0 < 64; t0 += 4) {
+                int used = 0;
+                for (int t = t0; t < t0 + 4; ++t)
+                    for (int i = 0; i < 4; ++i) used |= 1 << bank(t, c + i);
+                CHECK(used == 0xFFFF);
+            }
+    }
+    puts("ok");
+}
+"""
+
+
+def test_tiles_splits_and_places(tmp_path):
+    (tmp_path / "main.cpp").write_text(_MAIN)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-fsanitize=undefined,address", "-fno-sanitize-recover=all", "-I", CSRC, str(tmp_path / "main.cpp"), "-o",
+                    str(tmp_path / "main")], check=True)
+    r = subprocess.run([str(tmp_path / "main")], capture_output=True, text=True)
+    assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout + r.stderr
