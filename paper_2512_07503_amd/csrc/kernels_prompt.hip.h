@@ -25,6 +25,7 @@ struct PromptArgs {
 };
 
 constexpr int kPromptWaves = 4;
+constexpr int prompt_waves_per_simd(int size, int hd) { return size * hd <= 256 ? 2 : 1; }
 // tokens of a block
 template <typename T> constexpr int kPromptBlock = sizeof(T) == 2 ? 64 : 32;
 
@@ -122,17 +123,37 @@ typedef short prompt_s16x4 __attribute__((ext_vector_type(4)));
 // Keys or values of a block on their way to LDS.  WIDE: rows are 16-byte aligned and go there without passing through registers.  Tokens behind the last are
 // copies of the last one: nobody sees them.
 template <typename T, int HD, bool WIDE> struct PromptFetch {
-    static constexpr int BLOCK = kPromptBlock<T>, ROW = HD * sizeof(T), PIECES = BLOCK * ROW / 16, THREADS = kPromptWaves * 64;
-    static constexpr int PER = (PIECES + THREADS - 1) / THREADS;
-    SJD_D static void run(const T *base, long stride, int t0, int n_keys, unsigned char *lds, int wave, int lane) {
+    static constexpr int BLOCK = kPromptBlock<T>, ROW = HD * sizeof(T), PIECES = BLOCK * ROW / 16, THREADS = kPromptWaves * 64, PER = PIECES / THREADS;
+    static_assert(PIECES % THREADS == 0, "a block divides among the threads");
+    // Pieces of a lane whose tokens are a multiple of 16 apart have the same places in their rows
+    static constexpr int TOKENS = THREADS * 16 / ROW, DIFFERENT = THREADS * 16 % ROW == 0 && TOKENS % 16 == 0 ? 1 : PER;
+    uint32_t at[DIFFERENT];    // bytes from the block's first token
+    SJD_D static int token(int i, int wave, int lane) { return ((i * kPromptWaves + wave) * 64 + lane) / (ROW / 16); }
+    SJD_D static int piece(int i, int wave, int lane) {
+        const int n = (i * kPromptWaves + wave) * 64 + lane;
+        return prompt_swizzle(n / (ROW / 16), n % (ROW / 16), ROW);
+    }
+    SJD_D PromptFetch(long stride, int wave, int lane) {
+#pragma unroll
+        for (int i = 0; i < DIFFERENT; ++i) at[i] = (uint32_t)token(i, wave, lane) * (uint32_t)(stride * sizeof(T)) + piece(i, wave, lane) * 16;
+    }
+    SJD_D void run(const T *base, long stride, int t0, int n_keys, unsigned char *lds, int wave, int lane) const {
+        const char *block = (const char *)base + (size_t)t0 * stride * sizeof(T);
+        const bool whole = t0 + BLOCK <= n_keys;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int n0 = (i * kPromptWaves + wave) * 64, n = n0 + lane;
-            if (PIECES % THREADS != 0 && n0 >= PIECES) break;
-            const int t = n / (ROW / 16), c = prompt_swizzle(t, n % (ROW / 16), ROW);
-            const T *p = base + (size_t)min(t0 + t, n_keys - 1) * stride + c * (16 / sizeof(T));
-            if constexpr (WIDE) __builtin_amdgcn_global_load_lds((prompt_glb_t *)p, (prompt_lds_t *)(lds + n0 * 16), 16, 0, 0);
-            else {
+            unsigned char *to = lds + (i * kPromptWaves + wave) * 1024;
+            if constexpr (WIDE) {
+                const char *from = block + (DIFFERENT == 1 ? i * TOKENS * stride * (long)sizeof(T) : 0);
+                uint32_t off = at[DIFFERENT == 1 ? 0 : i];
+                if (!whole) {
+                    const int t = min(token(i, wave, lane), n_keys - 1 - t0);
+                    from = block;
+                    off = (uint32_t)t * (uint32_t)(stride * sizeof(T)) + piece(i, wave, lane) * 16;
+                }
+                __builtin_amdgcn_global_load_lds((prompt_glb_t *)(from + off), (prompt_lds_t *)to, 16, 0, 0);
+            } else {
+                const T *p = base + (size_t)min(t0 + token(i, wave, lane), n_keys - 1) * stride + piece(i, wave, lane) * (16 / sizeof(T));
                 u32x4 x;
                 if constexpr (sizeof(T) == 4) {
 #pragma unroll
@@ -141,7 +162,7 @@ template <typename T, int HD, bool WIDE> struct PromptFetch {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) x[e] = p[2 * e] | (uint32_t)p[2 * e + 1] << 16;
                 }
-                *reinterpret_cast<u32x4 *>(lds + n * 16) = x;
+                *reinterpret_cast<u32x4 *>(to + lane * 16) = x;
             }
         }
     }
@@ -220,6 +241,16 @@ template <int HD> SJD_D void prompt_rescale(PromptState<HD> &st, float mx) {
         for (int v = 0; v < 16; ++v) st.o[db][v] *= alpha;
 }
 
+// the larger of a lane's and its partner's in the other half
+SJD_D float prompt_both_halves(float x) {
+    const auto y = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(int, x), __builtin_bit_cast(int, x), false, false);
+    return fmaxf(__builtin_bit_cast(float, (int)y[0]), __builtin_bit_cast(float, (int)y[1]));
+}
+// sum + the two bf16 numbers of a pair
+SJD_D float prompt_add_pair(float sum, uint32_t pair) {
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(cache_bf16x2, pair), __builtin_bit_cast(cache_bf16x2, 0x3F803F80u), sum, false);
+}
+
 // is a value infinite or NaN
 SJD_D bool prompt_wild(float x) { return !finite_f(x); }
 // two bf16 numbers: infinite ones and NaN become 0, and are noted
@@ -237,10 +268,16 @@ template <typename T, int HD> SJD_D void prompt_add_wild(PromptState<HD> &st, co
 #pragma unroll
         for (int db = 0; db < HD / 32; ++db)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int j = 32 * db + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3), c = j * sizeof(T) / 16;
-                const float x = to_float<T>(*reinterpret_cast<const T *>(v + t * ROW + prompt_swizzle(t, c, ROW) * 16 + (j * sizeof(T)) % 16));
-                if (t <= last && prompt_wild(x)) st.o[db][e] += x;
+            for (int u = 0; u < 4; ++u) {
+                int at = t;
+                asm volatile("" : "+v"(at));      // (an address at a time: kept ahead of the loop they would take the registers of the caller's)
+                const int j = 32 * db + 8 * u + 4 * (lane >> 5);
+                const T *p = reinterpret_cast<const T *>(v + at * ROW + prompt_swizzle(at, j * (int)sizeof(T) / 16, ROW) * 16 + (j * sizeof(T)) % 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float x = to_float<T>(p[e]);
+                    if (t <= last && prompt_wild(x)) st.o[db][4 * u + e] += x;
+                }
             }
 }
 
@@ -307,11 +344,132 @@ SJD_D void prompt_block(PromptState<HD> &st, const unsigned char *k, const unsig
     if (MASKED && __ballot(wild)) prompt_add_wild<T, HD>(st, v, last, lane);
 }
 
+// N matrix products with M other pieces of work spread between them, in this order
+template <int N, int M, typename A, typename B> SJD_D void prompt_spread(A product, B other) {
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        product(i);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = i * M / N; j < (i + 1) * M / N; ++j) other(j);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// One block of 64 keys, of one or two tiles of 32 rows, bf16.  With two tiles the exponentials of one are spread between the matrix products of the other.  last[r]: of the
+// block's tokens, the last one that the lane's row sees; masked: some row may not see all of them.
+template <int HD, int RT>
+SJD_D void prompt_block16(PromptState<HD> (&st)[RT], const unsigned char *k, const unsigned char *v, const u32x4 (&q)[RT][HD / 16], const int (&sees)[RT], int t0, bool masked, float scale_log2e,
+                          int lane) {
+    constexpr int NQ = HD / 16, DB = HD / 32;
+    f32x16 s[RT][2];
+    u32x4 kf[2][NQ], vf[2][2 * DB], p[RT][4];
+    float m_use[RT], mx[RT];
+    bool wild[2] = {false, false};
+    const int t = lane & 31;
+    auto load_k = [&](int u, int n) { kf[u][n] = *reinterpret_cast<const u32x4 *>(k + (32 * u + t) * HD * 2 + prompt_swizzle(t, 2 * n + (lane >> 5), HD * 2) * 16); };
+    auto load_v = [&](int u, int n) { vf[u][n] = prompt_values16<HD>(v, 2 * u + n / DB, n % DB, lane); };
+    auto score = [&](int r, int u, int n) {
+        if (n == 0)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[r][u][e] = 0.0f;
+        s[r][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[u][n]), __builtin_bit_cast(bf16x8, q[r][n]), s[r][u], 0, 0, 0);
+    };
+    auto mask = [&](int r) {
+        const int mine = sees[r] - t0 - 4 * (lane >> 5);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[r][u][e] = 32 * u + 8 * (e >> 2) + (e & 3) <= mine ? s[r][u][e] : -INFINITY;
+    };
+    auto largest = [&](int r, int n) {       // n-th of 8
+        if (n == 0) mx[r] = s[r][0][0];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mx[r] = fmaxf(mx[r], s[r][n >> 2][4 * (n & 3) + e]);
+    };
+    auto settle = [&](int r) {
+        prompt_rescale<HD>(st[r], prompt_both_halves(mx[r]) * scale_log2e);
+        m_use[r] = st[r].m == -INFINITY ? 0.0f : st[r].m;
+    };
+    // probabilities 2 n and 2 n + 1 of 32 keys; those of n - 1 as operands
+    auto weigh = [&](int r, int u, int n) {
+        if (n < 8) {
+            s[r][u][2 * n] = __builtin_amdgcn_exp2f(fmaf(s[r][u][2 * n], scale_log2e, -m_use[r]));
+            s[r][u][2 * n + 1] = __builtin_amdgcn_exp2f(fmaf(s[r][u][2 * n + 1], scale_log2e, -m_use[r]));
+        }
+        if (n > 0) {
+            const uint32_t both = pack_bf16(s[r][u][2 * n - 2], s[r][u][2 * n - 1]);
+            p[r][2 * u + (n - 1) / 4][(n - 1) % 4] = both;
+            st[r].l = prompt_add_pair(st[r].l, both);
+        }
+    };
+    auto product = [&](int r, int u, int n) {      // n-th of 2 DB
+        st[r].o[n % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[u][n]), __builtin_bit_cast(bf16x8, p[r][2 * u + n / DB]), st[r].o[n % DB], 0, 0, 0);
+    };
+    // values that are infinite or NaN: 0 times them is NaN
+    auto look = [&](int u) {
+        float x = 0.0f;
+#pragma unroll
+        for (int n = 0; n < 2 * DB; ++n)
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                const uint32_t w = vf[u][n][d];
+                x = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(cache_bf16x2, w), __builtin_bit_cast(cache_bf16x2, 0u), x, false);
+            }
+        wild[u] = __ballot(x != 0.0f);
+        if (wild[u]) {
+            bool any = false;
+#pragma unroll
+            for (int n = 0; n < 2 * DB; ++n)
+#pragma unroll
+                for (int d = 0; d < 4; ++d) vf[u][n][d] = prompt_tame2(vf[u][n][d], any);
+        }
+    };
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) load_k(0, n);
+    prompt_spread<NQ, NQ>([&](int n) { score(0, 0, n); }, [&](int n) { load_k(1, n); });
+    prompt_spread<NQ, 0>([&](int n) { score(0, 1, n); }, [&](int) {});
+    if (masked) mask(0);
+    if constexpr (RT == 2) {
+        prompt_spread<NQ, 8>([&](int n) { score(1, 0, n); }, [&](int n) { largest(0, n); });
+        settle(0);
+        prompt_spread<NQ, 9 + 2 * DB>([&](int n) { score(1, 1, n); }, [&](int n) { n < 9 ? weigh(0, 0, n) : load_v(0, n - 9); });
+        if (masked) {
+            mask(1);
+            look(0);
+        }
+        prompt_spread<2 * DB, 17 + 2 * DB>([&](int n) { product(0, 0, n); }, [&](int n) { n < 9 ? weigh(0, 1, n) : n < 17 ? largest(1, n - 9) : load_v(1, n - 17); });
+        settle(1);
+        if (masked) look(1);
+        prompt_spread<2 * DB, 9>([&](int n) { product(0, 1, n); }, [&](int n) { weigh(1, 0, n); });
+        prompt_spread<2 * DB, 9>([&](int n) { product(1, 0, n); }, [&](int n) { weigh(1, 1, n); });
+        prompt_spread<2 * DB, 0>([&](int n) { product(1, 1, n); }, [&](int) {});
+    } else {
+#pragma unroll
+        for (int n = 0; n < 8; ++n) largest(0, n);
+        settle(0);
+#pragma unroll
+        for (int n = 0; n < 2 * DB; ++n) load_v(0, n);
+#pragma unroll
+        for (int n = 0; n < 9; ++n) weigh(0, 0, n);
+        if (masked) look(0);
+        prompt_spread<2 * DB, 9 + 2 * DB>([&](int n) { product(0, 0, n); }, [&](int n) { n < 2 * DB ? load_v(1, n) : weigh(0, 1, n - 2 * DB); });
+        if (masked) look(1);
+        prompt_spread<2 * DB, 0>([&](int n) { product(0, 1, n); }, [&](int) {});
+    }
+    if (wild[0] || wild[1])
+#pragma unroll
+        for (int r = 0; r < RT; ++r) prompt_add_wild<bf16_t, HD>(st[r], v, sees[r] - t0, lane);
+}
+
 // Workgroup = four wavefronts of RT tiles of 32 rows each, of a split.
 template <typename T, int HD, int RT, bool WIDE>
-__global__ __launch_bounds__(kPromptWaves * 64) void prompt_attention_kernel(PromptArgs a) {
+__global__ __launch_bounds__(kPromptWaves * 64, prompt_waves_per_simd(sizeof(T), HD)) void prompt_attention_kernel(PromptArgs a) {
     constexpr int BLOCK = kPromptBlock<T>, BYTES = BLOCK * HD * sizeof(T), ROWS = kPromptWaves * 32 * RT;
-    __shared__ __attribute__((aligned(16))) unsigned char lds[2][2][BYTES];
+    // (arrays of their own, so that the compiler knows that what is on its way to one is not read from the other)
+    __shared__ __attribute__((aligned(16))) unsigned char k_even[BYTES], v_even[BYTES], k_odd[BYTES], v_odd[BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int kvh = blockIdx.x % a.n_kv, tile = blockIdx.x / a.n_kv % a.tiles, split = blockIdx.x / a.n_kv / a.tiles;
     const PromptTile s = prompt_find_tile(a, ROWS, tile);
@@ -319,13 +477,9 @@ __global__ __launch_bounds__(kPromptWaves * 64) void prompt_attention_kernel(Pro
     const PromptBlocks range = prompt_blocks(prompt_keys(s.t, s.n, s.n_keys, a.G, ROWS), BLOCK, split, a.n_splits, a.per_split);
     if (!range.any) return;
     const T *k = (const T *)a.k + (size_t)s.k0 * a.k_stride + (size_t)kvh * HD, *v = (const T *)a.v + (size_t)s.k0 * a.v_stride + (size_t)kvh * HD;
-    auto fetch = [&](int blk, int buf) {
-        PromptFetch<T, HD, WIDE>::run(k, a.k_stride, blk * BLOCK, s.n_keys, lds[buf][0], wave, lane);
-        PromptFetch<T, HD, WIDE>::run(v, a.v_stride, blk * BLOCK, s.n_keys, lds[buf][1], wave, lane);
-    };
     PromptState<HD> st[RT];
     u32x4 q[RT][HD * sizeof(T) / 32];
-    int sees[RT], low[RT], high[RT];    // last key that the lane's row sees; the least and the largest such key of the tile's rows
+    int sees[RT], low = 0, high = -1;    // last key that the lane's row sees; the least and the largest such key of the wavefront's rows
     const int row0 = s.t * ROWS + wave * 32 * RT, offset = prompt_offset(s.n, s.n_keys);
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
@@ -333,20 +487,32 @@ __global__ __launch_bounds__(kPromptWaves * 64) void prompt_attention_kernel(Pro
         st[r].clear();
         prompt_load_q<T, HD>(a, s, kvh, first, lane, q[r]);
         sees[r] = node < s.n ? node + offset : -1;
-        low[r] = __builtin_amdgcn_readfirstlane(first / a.G + offset);
-        high[r] = __builtin_amdgcn_readfirstlane(first / a.G < s.n ? min((first + 31) / a.G, s.n - 1) + offset : -1);
     }
-    if (range.first < range.last) fetch(range.first, 0);
-    for (int blk = range.first; blk < range.last; ++blk) {
-        const int buf = (blk - range.first) & 1, t0 = blk * BLOCK;
-        __syncthreads();     // this block is there, and everybody is done with the last one
-        if (blk + 1 < range.last) fetch(blk + 1, buf ^ 1);
+    low = __builtin_amdgcn_readfirstlane(row0 / a.G + offset);
+    if (row0 / a.G < s.n) high = __builtin_amdgcn_readfirstlane(min((row0 + 32 * RT - 1) / a.G, s.n - 1) + offset);
+    const PromptFetch<T, HD, WIDE> fetch_k(a.k_stride, wave, lane), fetch_v(a.v_stride, wave, lane);
+    auto fetch = [&](int blk, unsigned char *lk, unsigned char *lv) {
+        fetch_k.run(k, a.k_stride, blk * BLOCK, s.n_keys, lk, wave, lane);
+        fetch_v.run(v, a.v_stride, blk * BLOCK, s.n_keys, lv, wave, lane);
+    };
+    auto block = [&](int blk, const unsigned char *lk, const unsigned char *lv) {
+        const int t0 = blk * BLOCK;
+        if (t0 > high) return;
+        if constexpr (sizeof(T) == 2) prompt_block16<HD, RT>(st, lk, lv, q, sees, t0, t0 + BLOCK - 1 > low, a.scale_log2e, lane);
+        else {
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            if (t0 > high[r]) continue;
-            if (t0 + BLOCK - 1 > low[r]) prompt_block<T, HD, true>(st[r], lds[buf][0], lds[buf][1], q[r], sees[r] - t0, a.scale_log2e, lane);
-            else prompt_block<T, HD, false>(st[r], lds[buf][0], lds[buf][1], q[r], sees[r] - t0, a.scale_log2e, lane);
+            for (int r = 0; r < RT; ++r) prompt_block<T, HD, true>(st[r], lk, lv, q[r], sees[r] - t0, a.scale_log2e, lane);
         }
+    };
+    if (range.first < range.last) fetch(range.first, k_even, v_even);
+    for (int blk = range.first; blk < range.last; blk += 2) {
+        __syncthreads();     // this block is there, and everybody is done with the last one
+        if (blk + 1 < range.last) fetch(blk + 1, k_odd, v_odd);
+        block(blk, k_even, v_even);
+        if (blk + 1 >= range.last) break;
+        __syncthreads();
+        if (blk + 2 < range.last) fetch(blk + 2, k_even, v_even);
+        block(blk + 1, k_odd, v_odd);
     }
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
