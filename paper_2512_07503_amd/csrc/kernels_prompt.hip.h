@@ -168,6 +168,12 @@ template <typename T, int HD, bool WIDE> struct PromptFetch {
     }
 };
 
+// What every thread has asked for is in LDS, and read from there.  (A barrier by itself waits for neither: loads to LDS are not stores to it in the compiler's eyes.)
+SJD_D void prompt_barrier() {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+}
+
 // S^T of 32 keys (from token `sub` * 32 of the block) and 32 rows
 template <typename T, int HD> SJD_D f32x16 prompt_scores(const unsigned char *k, int sub, const u32x4 (&q)[HD * sizeof(T) / 32], int lane) {
     f32x16 s;
@@ -429,8 +435,10 @@ SJD_D void prompt_block16(PromptState<HD> (&st)[RT], const unsigned char *k, con
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int n = 0; n < NQ; ++n) load_k(0, n);
+    __builtin_amdgcn_s_setprio(1);
     prompt_spread<NQ, NQ>([&](int n) { score(0, 0, n); }, [&](int n) { load_k(1, n); });
     prompt_spread<NQ, 0>([&](int n) { score(0, 1, n); }, [&](int) {});
+    __builtin_amdgcn_s_setprio(0);
     if (masked) mask(0);
     if constexpr (RT == 2) {
         prompt_spread<NQ, 8>([&](int n) { score(1, 0, n); }, [&](int n) { largest(0, n); });
@@ -455,9 +463,11 @@ SJD_D void prompt_block16(PromptState<HD> (&st)[RT], const unsigned char *k, con
 #pragma unroll
         for (int n = 0; n < 9; ++n) weigh(0, 0, n);
         if (masked) look(0);
+    __builtin_amdgcn_s_setprio(1);
         prompt_spread<2 * DB, 9 + 2 * DB>([&](int n) { product(0, 0, n); }, [&](int n) { n < 2 * DB ? load_v(1, n) : weigh(0, 1, n - 2 * DB); });
         if (masked) look(1);
         prompt_spread<2 * DB, 0>([&](int n) { product(0, 1, n); }, [&](int) {});
+    __builtin_amdgcn_s_setprio(0);
     }
     if (wild[0] || wild[1])
 #pragma unroll
@@ -506,11 +516,11 @@ __global__ __launch_bounds__(kPromptWaves * 64, prompt_waves_per_simd(sizeof(T),
     };
     if (range.first < range.last) fetch(range.first, k_even, v_even);
     for (int blk = range.first; blk < range.last; blk += 2) {
-        __syncthreads();     // this block is there, and everybody is done with the last one
+        prompt_barrier();     // this block is there, and everybody is done with the last one
         if (blk + 1 < range.last) fetch(blk + 1, k_odd, v_odd);
         block(blk, k_even, v_even);
         if (blk + 1 >= range.last) break;
-        __syncthreads();
+        prompt_barrier();
         if (blk + 2 < range.last) fetch(blk + 2, k_even, v_even);
         block(blk + 1, k_odd, v_odd);
     }

@@ -250,6 +250,15 @@ def test_same_bits_every_time():
         assert (c.run() == first).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_same_bits_with_the_card_full(dtype):
+    """Every block of keys is in LDS before anybody reads it, however long it took to get there."""
+    c = Case(dtype, 32, 8, 128, [2900, 1000], seed=21)
+    first = c.run().clone()
+    for _ in range(10):
+        assert (c.run() == first).all()
+
+
 def test_workspace():
     import paper_2512_07503_amd as sjd
     import torch
