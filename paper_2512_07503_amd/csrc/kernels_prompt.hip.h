@@ -6,6 +6,8 @@
 // and P^T needs no data movement: the accumulator registers of S^T are the B operand of the second product, if the keys of V^T are taken in their order.
 // Keys and values go through LDS, straight from memory, for all wavefronts of a workgroup.
 #pragma once
+#include <type_traits>
+
 #include "common.hip.h"
 #include "kernels_cache.hip.h"
 #include "prompt_layout.h"
@@ -120,6 +122,13 @@ typedef __attribute__((address_space(3))) void prompt_lds_t;
 typedef const __attribute__((address_space(1))) void prompt_glb_t;
 typedef short prompt_s16x4 __attribute__((ext_vector_type(4)));
 
+// 16 bytes of each lane, `off` from base, to LDS, the lanes' one behind the other.  In the compiler's own form every read of what it cannot tell from the target would wait for the load, the reads
+// of another buffer of the same array among them; here prompt_barrier is what waits.  (M0 holds the target for these loads alone.)
+SJD_D void prompt_to_lds(const char *base, uint32_t off, unsigned char *lds) {
+    const uint32_t to = (uint32_t)(uintptr_t)(prompt_lds_t *)lds;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off), "s"(base) : "memory");
+}
+
 // Keys or values of a block on their way to LDS.  WIDE: rows are 16-byte aligned and go there without passing through registers.  Tokens behind the last are
 // copies of the last one: nobody sees them.
 template <typename T, int HD, bool WIDE> struct PromptFetch {
@@ -139,78 +148,100 @@ template <typename T, int HD, bool WIDE> struct PromptFetch {
     }
     SJD_D void run(const T *base, long stride, int t0, int n_keys, unsigned char *lds, int wave, int lane) const {
         const char *block = (const char *)base + (size_t)t0 * stride * sizeof(T);
-        const bool whole = t0 + BLOCK <= n_keys;
+        unsigned char *to = lds + wave * 1024;
+        if (WIDE && t0 + BLOCK <= n_keys) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                prompt_to_lds(block + (DIFFERENT == 1 ? i * TOKENS * stride * (long)sizeof(T) : 0), at[DIFFERENT == 1 ? 0 : i], to + i * THREADS * 16);
+            return;
+        }
+        asm volatile("" : "+v"(lane));       // (rare: nothing of it is kept in registers from block to block)
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            unsigned char *to = lds + (i * kPromptWaves + wave) * 1024;
-            if constexpr (WIDE) {
-                const char *from = block + (DIFFERENT == 1 ? i * TOKENS * stride * (long)sizeof(T) : 0);
-                uint32_t off = at[DIFFERENT == 1 ? 0 : i];
-                if (!whole) {
-                    const int t = min(token(i, wave, lane), n_keys - 1 - t0);
-                    from = block;
-                    off = (uint32_t)t * (uint32_t)(stride * sizeof(T)) + piece(i, wave, lane) * 16;
-                }
-                __builtin_amdgcn_global_load_lds((prompt_glb_t *)(from + off), (prompt_lds_t *)to, 16, 0, 0);
-            } else {
-                const T *p = base + (size_t)min(t0 + token(i, wave, lane), n_keys - 1) * stride + piece(i, wave, lane) * (16 / sizeof(T));
+            const uint32_t t = (uint32_t)min(token(i, wave, lane), n_keys - 1 - t0);
+            if constexpr (WIDE) prompt_to_lds(block, t * (uint32_t)(stride * sizeof(T)) + piece(i, wave, lane) * 16, to + i * THREADS * 16);
+            else {
+                const T *e = (const T *)(block + t * (size_t)(stride * sizeof(T)) + piece(i, wave, lane) * 16);
                 u32x4 x;
-                if constexpr (sizeof(T) == 4) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = __builtin_bit_cast(uint32_t, p[e]);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = p[2 * e] | (uint32_t)p[2 * e + 1] << 16;
+                for (int d = 0; d < 4; ++d) {
+                    if constexpr (sizeof(T) == 4) x[d] = __builtin_bit_cast(uint32_t, e[d]);
+                    else x[d] = e[2 * d] | (uint32_t)e[2 * d + 1] << 16;
                 }
-                *reinterpret_cast<u32x4 *>(to + lane * 16) = x;
+                *reinterpret_cast<u32x4 *>(to + i * THREADS * 16 + lane * 16) = x;
             }
         }
     }
 };
 
-// What every thread has asked for is in LDS, and read from there.  (A barrier by itself waits for neither: loads to LDS are not stores to it in the compiler's eyes.)
+// What every thread has asked for is in LDS, and what was there has been read.  (A barrier by itself does not wait for loads to LDS.)
 SJD_D void prompt_barrier() {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
 }
 
-// S^T of 32 keys (from token `sub` * 32 of the block) and 32 rows
-template <typename T, int HD> SJD_D f32x16 prompt_scores(const unsigned char *k, int sub, const u32x4 (&q)[HD * sizeof(T) / 32], int lane) {
+// S^T of 32 keys and 32 rows, fp32
+template <int HD> SJD_D f32x16 prompt_scores32(const unsigned char *k, const u32x4 (&q)[HD / 8], int lane) {
     f32x16 s;
 #pragma unroll
     for (int v = 0; v < 16; ++v) s[v] = 0.0f;
-    constexpr int ROW = HD * sizeof(T);
-    const int t = sub * 32 + (lane & 31);
+    const int t = lane & 31;
 #pragma unroll
-    for (int n = 0; n < ROW / 32; ++n) {
-        const u32x4 x = *reinterpret_cast<const u32x4 *>(k + t * ROW + prompt_swizzle(t, 2 * n + (lane >> 5), ROW) * 16);
-        if constexpr (sizeof(T) == 2) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, q[n]), s, 0, 0, 0);
-        else {
+    for (int n = 0; n < HD / 8; ++n) {
+        const u32x4 x = *reinterpret_cast<const u32x4 *>(k + t * HD * 4 + prompt_swizzle(t, 2 * n + (lane >> 5), HD * 4) * 16);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t xe = x[e], qe = q[n][e];
-                s = __builtin_amdgcn_mfma_f32_32x32x2f32(__builtin_bit_cast(float, xe), __builtin_bit_cast(float, qe), s, 0, 0, 0);
-            }
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t xe = x[e], qe = q[n][e];
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__builtin_bit_cast(float, xe), __builtin_bit_cast(float, qe), s, 0, 0, 0);
         }
     }
     return s;
 }
 
-// A operand of the second product, dimensions 32 db + lane % 32.  bf16: 16 tokens, 16 i + 8 (e / 4) + 4 (lane / 32) + e % 4 for its element e, read from
-// their rows by the transposing loads (16 lanes fetch 16 dimensions of 4 tokens, and each gets the 4 tokens of one).
-template <int HD> SJD_D u32x4 prompt_values16(const unsigned char *v, int i, int db, int lane) {
-    constexpr int ROW = HD * 2;
-    u32x4 x;
+// Operands of the bf16 products in a block in LDS: places of a lane's 16 bytes of keys (rows of the operand = 32 keys, 16 dimensions at a time), and of the 8 bytes that it fetches for
+// values (rows = dimensions 32 db + lane % 32; of 16 keys 16 i, the element e is key 16 i + 8 (e / 4) + 4 (lane / 32) + e % 4, as the scores have them).  Those come from the rows by the
+// transposing loads: 16 lanes fetch 16 dimensions of 4 keys, and each gets the 4 keys of one.
+template <int HD> struct PromptPlaces {
+    static constexpr int ROW = HD * 2, AGAIN = ROW % 128 == 64 ? 64 : ROW % 256 == 128 ? 128 : 256, NK = AGAIN / 32, NV = AGAIN / 64;    // (places repeat after so many bytes)
+    int k[NK], v[2][NV];
+    SJD_D explicit PromptPlaces(int lane) {
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        const int t = 16 * i + 8 * r + 4 * (lane >> 5) + ((lane >> 2) & 3), j = 32 * db + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-        typedef __attribute__((address_space(3))) prompt_s16x4 lds4;
-        const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(v + t * ROW + prompt_swizzle(t, j >> 3, ROW) * 16 + (j & 4) * 2)));
-        x[2 * r] = y.x;
-        x[2 * r + 1] = y.y;
+        for (int n = 0; n < NK; ++n) {
+            k[n] = (lane & 31) * ROW + prompt_swizzle(lane & 31, 2 * n + (lane >> 5), ROW) * 16;
+            asm volatile("" : "+v"(k[n]));       // (once: the compiler would keep them for each buffer)
+        }
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int db = 0; db < NV; ++db) {
+                const int t = 8 * r + 4 * (lane >> 5) + ((lane >> 2) & 3), j = 32 * db + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+                v[r][db] = t * ROW + prompt_swizzle(t, j >> 3, ROW) * 16 + (j & 4) * 2;
+                asm volatile("" : "+v"(v[r][db]));
+            }
     }
-    return x;
-}
+    SJD_D void move(int bytes) {
+#pragma unroll
+        for (int n = 0; n < NK; ++n) k[n] += bytes;
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int db = 0; db < NV; ++db) v[r][db] += bytes;
+    }
+    SJD_D u32x4 keys(const unsigned char *block, int half, int n) const {
+        return *reinterpret_cast<const u32x4 *>(block + k[n % NK] + n / NK * AGAIN + half * 32 * ROW);
+    }
+    SJD_D u32x4 values(const unsigned char *block, int i, int db) const {
+        typedef __attribute__((address_space(3))) prompt_s16x4 lds4;
+        u32x4 x;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(block + v[r][db % NV] + db / NV * AGAIN + 16 * i * ROW)));
+            x[2 * r] = y.x;
+            x[2 * r + 1] = y.y;
+        }
+        return x;
+    }
+};
 // fp32: a token, 8 (v / 4) + 4 (lane / 32) + v % 4
 template <int HD> SJD_D float prompt_value32(const unsigned char *l, int v, int db, int lane) {
     constexpr int ROW = HD * 4;
@@ -236,15 +267,16 @@ template <int HD> struct PromptState {
 // the formula.
 constexpr float kPromptAhead = 8.0f;
 template <int HD> SJD_D void prompt_rescale(PromptState<HD> &st, float mx) {
-    if (!__ballot(mx > st.m)) return;
-    const float m = fmaxf(st.m, __builtin_ceilf(mx) + kPromptAhead);
+    const float m = mx > st.m ? __builtin_ceilf(mx) + kPromptAhead : st.m;
     const float alpha = __builtin_amdgcn_exp2f(st.m - (m == -INFINITY ? 0.0f : m));     // (not (-inf) - (-inf))
     st.m = m;
     st.l *= alpha;
 #pragma unroll
-    for (int db = 0; db < HD / 32; ++db)
+    for (int db = 0; db < HD / 32; ++db) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) st.o[db][v] *= alpha;
+        __builtin_amdgcn_sched_barrier(0);
+    }
 }
 
 // the larger of a lane's and its partner's in the other half
@@ -265,89 +297,77 @@ SJD_D uint32_t prompt_tame2(uint32_t u, bool &wild) {
     wild |= lo | hi;
     return u & ((lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u));
 }
-// Values that are infinite or NaN, of a block that not every row sees as a whole: in O += V P their 0 * inf would reach rows that do not see them, so there they are
-// taken as 0, and added here to the rows that do: p * inf is inf.  (Rare: token by token.)  `last`: the last token of the block that the lane's row sees.
-template <typename T, int HD> SJD_D void prompt_add_wild(PromptState<HD> &st, const unsigned char *v, int last, int lane) {
-    constexpr int ROW = HD * sizeof(T);
+// Values that are infinite or NaN, of units that not every row sees: in O += V P their 0 * inf would reach rows that do not see them, so there they are
+// taken as 0, and added here, behind the last block, to the rows that do: p * inf is inf.  (Rare: token by token, from memory.)  Tokens [from, to); `sees`: the last one that the lane's row sees.
+template <typename T, int HD> SJD_D void prompt_add_wild(PromptState<HD> &st, const T *v, long stride, int from, int to, int sees, int lane) {
 #pragma unroll 1
-    for (int t = 0; t < kPromptBlock<T>; ++t)
+    for (int t = from; t < to; ++t)
 #pragma unroll
         for (int db = 0; db < HD / 32; ++db)
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                int at = t;
-                asm volatile("" : "+v"(at));      // (an address at a time: kept ahead of the loop they would take the registers of the caller's)
-                const int j = 32 * db + 8 * u + 4 * (lane >> 5);
-                const T *p = reinterpret_cast<const T *>(v + at * ROW + prompt_swizzle(at, j * (int)sizeof(T) / 16, ROW) * 16 + (j * sizeof(T)) % 16);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x = to_float<T>(p[e]);
-                    if (t <= last && prompt_wild(x)) st.o[db][4 * u + e] += x;
-                }
+            for (int e = 0; e < 16; ++e) {
+                const float x = to_float<T>(v[t * stride + 32 * db + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3)]);
+                if (t <= sees && prompt_wild(x)) st.o[db][e] += x;
             }
 }
 
-// One block of 32 rows.  `last`: of the block's tokens, the last one that the lane's row sees.  MASKED: some row may not see all of them.
-template <typename T, int HD, bool MASKED>
-SJD_D void prompt_block(PromptState<HD> &st, const unsigned char *k, const unsigned char *v, const u32x4 (&q)[HD * sizeof(T) / 32], int last, float scale_log2e, int lane) {
-    constexpr int SUB = kPromptBlock<T> / 32;
-    f32x16 s[SUB];
-    const int mine = last - 4 * (lane >> 5);
-    float mx = -INFINITY;
+// One block of 32 keys and 32 rows, fp32.  `last`: of the block's keys, the last one that the lane's row sees; masked: some row may not see all of them.  -> whether
+// there were values then that are infinite or NaN, and taken as 0.
+template <int HD>
+SJD_D bool prompt_block32(PromptState<HD> &st, const unsigned char *k, const unsigned char *v, const u32x4 (&q)[HD / 8], int last, bool masked, float scale_log2e, int lane) {
+    f32x16 s = prompt_scores32<HD>(k, q, lane);
+    if (masked) {
+        const int mine = last - 4 * (lane >> 5);
 #pragma unroll
-    for (int u = 0; u < SUB; ++u) {
-        s[u] = prompt_scores<T, HD>(k, u, q, lane);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            if (MASKED) s[u][e] = 32 * u + 8 * (e >> 2) + (e & 3) <= mine ? s[u][e] : -INFINITY;
-            mx = fmaxf(mx, s[u][e]);
-        }
+        for (int e = 0; e < 16; ++e) s[e] = 8 * (e >> 2) + (e & 3) <= mine ? s[e] : -INFINITY;
     }
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * scale_log2e;
-    prompt_rescale<HD>(st, mx);
-    const float m_use = st.m == -INFINITY ? 0.0f : st.m;    // a row that has seen nothing so far: not (-inf) - (-inf)
-    float sum = 0.0f;
+    float mx = s[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
+    mx = prompt_both_halves(mx) * scale_log2e;
+    if (__ballot(mx > st.m)) prompt_rescale<HD>(st, mx);
+    const float m = st.m == -INFINITY ? 0.0f : st.m;        // a row that has seen nothing so far: not (-inf) - (-inf)
     bool wild = false;
 #pragma unroll
-    for (int u = 0; u < SUB; ++u) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[u][e] = __builtin_amdgcn_exp2f(fmaf(s[u][e], scale_log2e, -m_use));
-        if constexpr (sizeof(T) == 4) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                sum += s[u][e];
-#pragma unroll
-                for (int db = 0; db < HD / 32; ++db) {
-                    float x = prompt_value32<HD>(v, e, db, lane);
-                    if (MASKED && prompt_wild(x)) { wild = true; x = 0.0f; }
-                    st.o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, s[u][e], st.o[db], 0, 0, 0);
-                }
-            }
-        } else {
-            // What the products take is what the sum adds, so that a row's weights add up to 1 whatever their rounding to bf16 (a row that sees one token
-            // gives its value, exactly); one instruction for two of them.
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                u32x4 p;
-#pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    p[d] = pack_bf16(s[u][8 * i + 2 * d], s[u][8 * i + 2 * d + 1]);
-                    const uint32_t pd = p[d];
-                    sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(cache_bf16x2, pd), __builtin_bit_cast(cache_bf16x2, 0x3F803F80u), sum, false);
-                }
-#pragma unroll
-                for (int db = 0; db < HD / 32; ++db) {
-                    u32x4 x = prompt_values16<HD>(v, 2 * u + i, db, lane);
-                    if (MASKED)
-#pragma unroll
-                        for (int d = 0; d < 4; ++d) x[d] = prompt_tame2(x[d], wild);
-                    st.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, p), st.o[db], 0, 0, 0);
-                }
-            }
-        }
+    for (int e = 0; e < 16; ++e) {
+        s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], scale_log2e, -m));
+        st.l += s[e];
     }
-    st.l += sum;
-    if (MASKED && __ballot(wild)) prompt_add_wild<T, HD>(st, v, last, lane);
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+#pragma unroll
+        for (int db = 0; db < HD / 32; ++db) {
+            float x = prompt_value32<HD>(v, e, db, lane);
+            if (masked && prompt_wild(x)) { wild = true; x = 0.0f; }
+            st.o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, s[e], st.o[db], 0, 0, 0);
+        }
+    return __ballot(wild);
+}
+
+// What becomes of 32 rows (first: the first of them): results, or parts of them
+template <typename T, int HD>
+SJD_D void prompt_finish(const PromptArgs &a, const PromptTile &s, const PromptState<HD> &st, int kvh, bool several, size_t slot, int first, int lane) {
+    const int rho = first + (lane & 31), node = rho / a.G;
+    if (first >= (long)s.n * a.G) return;
+    const float sum = st.l + __shfl_xor(st.l, 32, 64);
+    // (it is NaN, and so is the row, where a score is; it is 0 where the row saw nothing)
+    const float norm = several ? 1.0f : sum == 0.0f ? 0.0f : 1.0f / sum;
+    if (several && lane < 32) {
+        a.part_ml[slot * 64 + lane] = st.m;
+        a.part_ml[slot * 64 + 32 + lane] = sum;
+    }
+    if (node >= s.n) return;
+#pragma unroll
+    for (int db = 0; db < HD / 32; ++db)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int j = db * 32 + 8 * u + 4 * (lane >> 5);
+            f32x4 t;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t[e] = norm == 0.0f ? 0.0f : st.o[db][4 * u + e] * norm;
+            if (several) *reinterpret_cast<f32x4 *>(a.part_o + slot * 32 * HD + prompt_part_index(lane & 31, j)) = t;
+            else prompt_store<T>(a, (size_t)s.r0 + node, kvh * a.G + rho - node * a.G, HD, j, t);
+        }
 }
 
 // N matrix products with M other pieces of work spread between them, in this order
@@ -363,198 +383,202 @@ template <int N, int M, typename A, typename B> SJD_D void prompt_spread(A produ
     }
 }
 
-// One block of 64 keys, of one or two tiles of 32 rows, bf16.  With two tiles the exponentials of one are spread between the matrix products of the other.  last[r]: of the
-// block's tokens, the last one that the lane's row sees; masked: some row may not see all of them.
-template <int HD, int RT>
-SJD_D void prompt_block16(PromptState<HD> (&st)[RT], const unsigned char *k, const unsigned char *v, const u32x4 (&q)[RT][HD / 16], const int (&sees)[RT], int t0, bool masked, float scale_log2e,
-                          int lane) {
-    constexpr int NQ = HD / 16, DB = HD / 32;
-    f32x16 s[RT][2];
-    u32x4 kf[2][NQ], vf[2][2 * DB], p[RT][4];
-    float m_use[RT], mx[RT];
-    bool wild[2] = {false, false};
-    const int t = lane & 31;
-    auto load_k = [&](int u, int n) { kf[u][n] = *reinterpret_cast<const u32x4 *>(k + (32 * u + t) * HD * 2 + prompt_swizzle(t, 2 * n + (lane >> 5), HD * 2) * 16); };
-    auto load_v = [&](int u, int n) { vf[u][n] = prompt_values16<HD>(v, 2 * u + n / DB, n % DB, lane); };
-    auto score = [&](int r, int u, int n) {
+// A wavefront of the bf16 kernel: 32 rows, a block of 64 keys at a time, in halves.
+template <int HD> struct PromptWave16 {
+    static constexpr int NQ = HD / 16, DB = HD / 32, BLOCK = kPromptBlock<bf16_t>;
+    PromptState<HD> st;
+    u32x4 q[NQ], k[2][NQ], v[2][2 * DB], p[2][2];     // operands: queries, keys, values, probabilities
+    f32x16 s[2];
+    float m, sum, e0, e1;
+    bool wild = false;                                // values of blocks that were masked were infinite or NaN
+    PromptPlaces<HD> at;
+    SJD_D explicit PromptWave16(int lane) : at(lane) { st.clear(); m = 0.0f; }
+    SJD_D void load_k(const unsigned char *block, int half, int n) { k[half][n] = at.keys(block, half, n); }
+    SJD_D void load_v(const unsigned char *block, int half, int n) { v[half][n] = at.values(block, 2 * half + n / DB, n % DB); }
+    template <int I> SJD_D void score(int n) {
         if (n == 0)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[r][u][e] = 0.0f;
-        s[r][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[u][n]), __builtin_bit_cast(bf16x8, q[r][n]), s[r][u], 0, 0, 0);
-    };
-    auto mask = [&](int r) {
-        const int mine = sees[r] - t0 - 4 * (lane >> 5);
+            for (int e = 0; e < 16; ++e) s[I][e] = 0.0f;
+        s[I] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k[I][n]), __builtin_bit_cast(bf16x8, q[n]), s[I], 0, 0, 0);
+    }
+    // last: of the unit's keys, the last one that the lane's row sees
+    template <int I> SJD_D void mask(int last) {
+        const int mine = last - 4 * (int)((threadIdx.x >> 5) & 1);
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int e = 0; e < 16; ++e) s[I][e] = 8 * (e >> 2) + (e & 3) <= mine ? s[I][e] : -INFINITY;
+    }
+    // Probabilities are 2^(score - m).  As long as a lane's of a unit add up to at most 1 none is above 1, and m stays; else, and at first, it is put ahead of the largest score.
+    SJD_D void settle(float scale_log2e) {
+        float mx = s[0][0];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[r][u][e] = 32 * u + 8 * (e >> 2) + (e & 3) <= mine ? s[r][u][e] : -INFINITY;
-    };
-    auto largest = [&](int r, int n) {       // n-th of 8
-        if (n == 0) mx[r] = s[r][0][0];
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) mx[r] = fmaxf(mx[r], s[r][n >> 2][4 * (n & 3) + e]);
-    };
-    auto settle = [&](int r) {
-        prompt_rescale<HD>(st[r], prompt_both_halves(mx[r]) * scale_log2e);
-        m_use[r] = st[r].m == -INFINITY ? 0.0f : st[r].m;
-    };
-    // probabilities 2 n and 2 n + 1 of 32 keys; those of n - 1 as operands
-    auto weigh = [&](int r, int u, int n) {
-        if (n < 8) {
-            s[r][u][2 * n] = __builtin_amdgcn_exp2f(fmaf(s[r][u][2 * n], scale_log2e, -m_use[r]));
-            s[r][u][2 * n + 1] = __builtin_amdgcn_exp2f(fmaf(s[r][u][2 * n + 1], scale_log2e, -m_use[r]));
-        }
+            for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[i][e]);
+        prompt_rescale<HD>(st, prompt_both_halves(mx) * scale_log2e);
+        m = st.m == -INFINITY ? 0.0f : st.m;           // a row that has seen nothing: not (-inf) - (-inf)
+    }
+    // probabilities 2 n and 2 n + 1; those of n - 1 as operands.  What the products take is what the sum adds, so that a row's weights add up to 1 whatever their rounding to bf16 (a row
+    // that sees one key gives its value, exactly).
+    template <int I> SJD_D void weigh(int n, float scale_log2e) {
         if (n > 0) {
-            const uint32_t both = pack_bf16(s[r][u][2 * n - 2], s[r][u][2 * n - 1]);
-            p[r][2 * u + (n - 1) / 4][(n - 1) % 4] = both;
-            st[r].l = prompt_add_pair(st[r].l, both);
+            const uint32_t both = pack_bf16(e0, e1);
+            p[I][(n - 1) / 4][(n - 1) % 4] = both;
+            sum = prompt_add_pair(sum, both);
         }
-    };
-    auto product = [&](int r, int u, int n) {      // n-th of 2 DB
-        st[r].o[n % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[u][n]), __builtin_bit_cast(bf16x8, p[r][2 * u + n / DB]), st[r].o[n % DB], 0, 0, 0);
-    };
-    // values that are infinite or NaN: 0 times them is NaN
-    auto look = [&](int u) {
+        if (n < 8) {
+            e0 = __builtin_amdgcn_exp2f(fmaf(s[I][2 * n], scale_log2e, -m));
+            e1 = __builtin_amdgcn_exp2f(fmaf(s[I][2 * n + 1], scale_log2e, -m));
+        }
+    }
+    template <int I> SJD_D void product(int n) {       // n-th of 2 DB
+        st.o[n % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[I][n]), __builtin_bit_cast(bf16x8, p[I][n / DB]), st.o[n % DB], 0, 0, 0);
+    }
+    // Are there values that are infinite or NaN (0 times them is NaN)?  They become 0.
+    template <int I> SJD_D bool tame() {
         float x = 0.0f;
 #pragma unroll
         for (int n = 0; n < 2 * DB; ++n)
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
-                const uint32_t w = vf[u][n][d];
+                const uint32_t w = v[I][n][d];
                 x = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(cache_bf16x2, w), __builtin_bit_cast(cache_bf16x2, 0u), x, false);
             }
-        wild[u] = __ballot(x != 0.0f);
-        if (wild[u]) {
+        const bool found = __ballot(x != 0.0f);
+        if (found) {
             bool any = false;
 #pragma unroll
             for (int n = 0; n < 2 * DB; ++n)
 #pragma unroll
-                for (int d = 0; d < 4; ++d) vf[u][n][d] = prompt_tame2(vf[u][n][d], any);
+                for (int d = 0; d < 4; ++d) v[I][n][d] = prompt_tame2(v[I][n][d], any);
         }
-    };
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) load_k(0, n);
-    __builtin_amdgcn_s_setprio(1);
-    prompt_spread<NQ, NQ>([&](int n) { score(0, 0, n); }, [&](int n) { load_k(1, n); });
-    prompt_spread<NQ, 0>([&](int n) { score(0, 1, n); }, [&](int) {});
-    __builtin_amdgcn_s_setprio(0);
-    if (masked) mask(0);
-    if constexpr (RT == 2) {
-        prompt_spread<NQ, 8>([&](int n) { score(1, 0, n); }, [&](int n) { largest(0, n); });
-        settle(0);
-        prompt_spread<NQ, 9 + 2 * DB>([&](int n) { score(1, 1, n); }, [&](int n) { n < 9 ? weigh(0, 0, n) : load_v(0, n - 9); });
-        if (masked) {
-            mask(1);
-            look(0);
-        }
-        prompt_spread<2 * DB, 17 + 2 * DB>([&](int n) { product(0, 0, n); }, [&](int n) { n < 9 ? weigh(0, 1, n) : n < 17 ? largest(1, n - 9) : load_v(1, n - 17); });
-        settle(1);
-        if (masked) look(1);
-        prompt_spread<2 * DB, 9>([&](int n) { product(0, 1, n); }, [&](int n) { weigh(1, 0, n); });
-        prompt_spread<2 * DB, 9>([&](int n) { product(1, 0, n); }, [&](int n) { weigh(1, 1, n); });
-        prompt_spread<2 * DB, 0>([&](int n) { product(1, 1, n); }, [&](int) {});
-    } else {
-#pragma unroll
-        for (int n = 0; n < 8; ++n) largest(0, n);
-        settle(0);
-#pragma unroll
-        for (int n = 0; n < 2 * DB; ++n) load_v(0, n);
-#pragma unroll
-        for (int n = 0; n < 9; ++n) weigh(0, 0, n);
-        if (masked) look(0);
-    __builtin_amdgcn_s_setprio(1);
-        prompt_spread<2 * DB, 9 + 2 * DB>([&](int n) { product(0, 0, n); }, [&](int n) { n < 2 * DB ? load_v(1, n) : weigh(0, 1, n - 2 * DB); });
-        if (masked) look(1);
-        prompt_spread<2 * DB, 0>([&](int n) { product(0, 1, n); }, [&](int) {});
-    __builtin_amdgcn_s_setprio(0);
+        return found;
     }
-    if (wild[0] || wild[1])
+    // A block.  last: of its keys, the last one that the lane's row sees; masked: some row may not see all of it; first: nothing came before it.
+    SJD_D void block(const unsigned char *keys, const unsigned char *values, int last, bool masked, bool first, float scale_log2e) {
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int r = 0; r < RT; ++r) prompt_add_wild<bf16_t, HD>(st[r], v, sees[r] - t0, lane);
-}
+        for (int n = 0; n < NQ; ++n) load_k(keys, 0, n);
+        __builtin_amdgcn_s_setprio(1);
+        prompt_spread<NQ, NQ>([&](int n) { score<0>(n); }, [&](int n) { load_k(keys, 1, n); });
+        prompt_spread<NQ, 0>([&](int n) { score<1>(n); }, [&](int) {});
+        __builtin_amdgcn_s_setprio(0);
+        if (masked) {
+            mask<0>(last);
+            mask<1>(last - 32);
+        }
+        sum = 0.0f;
+#pragma unroll
+        for (int n = 0; n < 9; ++n) weigh<0>(n, scale_log2e);
+#pragma unroll
+        for (int n = 0; n < 9; ++n) weigh<1>(n, scale_log2e);
+        if (__ballot(first || !(sum <= 1.0f))) {
+            settle(scale_log2e);
+            sum = 0.0f;
+#pragma unroll
+            for (int n = 0; n < 9; ++n) weigh<0>(n, scale_log2e);
+#pragma unroll
+            for (int n = 0; n < 9; ++n) weigh<1>(n, scale_log2e);
+        }
+        st.l += sum;
+#pragma unroll
+        for (int n = 0; n < 2 * DB; ++n) load_v(values, 0, n);
+        if (masked) wild |= tame<0>();
+        __builtin_amdgcn_s_setprio(1);
+        prompt_spread<2 * DB, 2 * DB>([&](int n) { product<0>(n); }, [&](int n) { load_v(values, 1, n); });
+        if (masked) wild |= tame<1>();
+        prompt_spread<2 * DB, 0>([&](int n) { product<1>(n); }, [&](int) {});
+        __builtin_amdgcn_s_setprio(0);
+    }
+};
 
-// Workgroup = four wavefronts of RT tiles of 32 rows each, of a split.
-template <typename T, int HD, int RT, bool WIDE>
-__global__ __launch_bounds__(kPromptWaves * 64, prompt_waves_per_simd(sizeof(T), HD)) void prompt_attention_kernel(PromptArgs a) {
-    constexpr int BLOCK = kPromptBlock<T>, BYTES = BLOCK * HD * sizeof(T), ROWS = kPromptWaves * 32 * RT;
-    // (arrays of their own, so that the compiler knows that what is on its way to one is not read from the other)
-    __shared__ __attribute__((aligned(16))) unsigned char k_even[BYTES], v_even[BYTES], k_odd[BYTES], v_odd[BYTES];
+// Workgroup = four wavefronts of 32 rows each, of a split.
+template <int HD, bool WIDE>
+__global__ __launch_bounds__(kPromptWaves * 64, prompt_waves_per_simd(2, HD)) void prompt_attention16_kernel(PromptArgs a) {
+    constexpr int BLOCK = kPromptBlock<bf16_t>, BYTES = BLOCK * HD * 2, ROWS = kPromptWaves * 32;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[4 * BYTES];      // keys and values of a block, and of the next one
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int kvh = blockIdx.x % a.n_kv, tile = blockIdx.x / a.n_kv % a.tiles, split = blockIdx.x / a.n_kv / a.tiles;
+    const int kvh = blockIdx.x % a.n_kv, tile = a.tiles - 1 - blockIdx.x / a.n_kv % a.tiles, split = blockIdx.x / a.n_kv / a.tiles;
     const PromptTile s = prompt_find_tile(a, ROWS, tile);
     if (s.b < 0) return;
     const PromptBlocks range = prompt_blocks(prompt_keys(s.t, s.n, s.n_keys, a.G, ROWS), BLOCK, split, a.n_splits, a.per_split);
     if (!range.any) return;
-    const T *k = (const T *)a.k + (size_t)s.k0 * a.k_stride + (size_t)kvh * HD, *v = (const T *)a.v + (size_t)s.k0 * a.v_stride + (size_t)kvh * HD;
-    PromptState<HD> st[RT];
-    u32x4 q[RT][HD * sizeof(T) / 32];
-    int sees[RT], low = 0, high = -1;    // last key that the lane's row sees; the least and the largest such key of the wavefront's rows
-    const int row0 = s.t * ROWS + wave * 32 * RT, offset = prompt_offset(s.n, s.n_keys);
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        const int first = row0 + 32 * r, node = (first + (lane & 31)) / a.G;
-        st[r].clear();
-        prompt_load_q<T, HD>(a, s, kvh, first, lane, q[r]);
-        sees[r] = node < s.n ? node + offset : -1;
-    }
-    low = __builtin_amdgcn_readfirstlane(row0 / a.G + offset);
-    if (row0 / a.G < s.n) high = __builtin_amdgcn_readfirstlane(min((row0 + 32 * RT - 1) / a.G, s.n - 1) + offset);
-    const PromptFetch<T, HD, WIDE> fetch_k(a.k_stride, wave, lane), fetch_v(a.v_stride, wave, lane);
-    auto fetch = [&](int blk, unsigned char *lk, unsigned char *lv) {
-        fetch_k.run(k, a.k_stride, blk * BLOCK, s.n_keys, lk, wave, lane);
-        fetch_v.run(v, a.v_stride, blk * BLOCK, s.n_keys, lv, wave, lane);
+    const bf16_t *k = (const bf16_t *)a.k + (size_t)s.k0 * a.k_stride + (size_t)kvh * HD, *v = (const bf16_t *)a.v + (size_t)s.k0 * a.v_stride + (size_t)kvh * HD;
+    PromptWave16<HD> w(lane);
+    const int row0 = s.t * ROWS + wave * 32, offset = prompt_offset(s.n, s.n_keys), node = (row0 + (lane & 31)) / a.G;
+    prompt_load_q<bf16_t, HD>(a, s, kvh, row0, lane, w.q);
+    // last key that the lane's row sees; the least such key of the wavefront's rows, and the blocks that one of them sees something of
+    const int sees = node < s.n ? node + offset : -1, low = __builtin_amdgcn_readfirstlane(row0 / a.G + offset);
+    const int mine = row0 / a.G < s.n ? __builtin_amdgcn_readfirstlane(min(range.last, (min((row0 + 31) / a.G, s.n - 1) + offset + BLOCK) / BLOCK)) : 0;
+    const PromptFetch<bf16_t, HD, WIDE> fetch_k(a.k_stride, wave, lane), fetch_v(a.v_stride, wave, lane);
+    auto get_k = [&](int blk, unsigned char *to) {
+        if (blk < range.last) fetch_k.run(k, a.k_stride, blk * BLOCK, s.n_keys, to, wave, lane);
     };
-    auto block = [&](int blk, const unsigned char *lk, const unsigned char *lv) {
-        const int t0 = blk * BLOCK;
-        if (t0 > high) return;
-        if constexpr (sizeof(T) == 2) prompt_block16<HD, RT>(st, lk, lv, q, sees, t0, t0 + BLOCK - 1 > low, a.scale_log2e, lane);
-        else {
-#pragma unroll
-            for (int r = 0; r < RT; ++r) prompt_block<T, HD, true>(st[r], lk, lv, q[r], sees[r] - t0, a.scale_log2e, lane);
-        }
+    auto get_v = [&](int blk, unsigned char *to) {
+        if (blk < range.last) fetch_v.run(v, a.v_stride, blk * BLOCK, s.n_keys, to, wave, lane);
     };
-    if (range.first < range.last) fetch(range.first, k_even, v_even);
-    for (int blk = range.first; blk < range.last; blk += 2) {
+    int blk = range.first, buf = 0;
+    get_k(blk, lds);
+    get_v(blk, lds + BYTES);
+    auto turn = [&]() {
         prompt_barrier();     // this block is there, and everybody is done with the last one
-        if (blk + 1 < range.last) fetch(blk + 1, k_odd, v_odd);
-        block(blk, k_even, v_even);
-        if (blk + 1 >= range.last) break;
-        prompt_barrier();
-        if (blk + 2 < range.last) fetch(blk + 2, k_even, v_even);
-        block(blk + 1, k_odd, v_odd);
+        buf = 2 * BYTES - buf;
+        get_k(blk + 1, lds + buf);
+        get_v(blk + 1, lds + buf + BYTES);
+    };
+    // (queries: waited for here; at their first use, in the loop, it would be a wait for everything, every time)
+#pragma unroll
+    for (int n = 0; n < HD / 16; ++n) asm volatile("" : "+v"(w.q[n]));
+    for (; blk < mine; ++blk) {
+        turn();
+        w.block(lds, lds + BYTES, sees - blk * BLOCK, blk * BLOCK + BLOCK - 1 > low, blk == range.first, a.scale_log2e);
+        w.at.move(buf ? 2 * BYTES : -2 * BYTES);
     }
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        const int rho = row0 + 32 * r + (lane & 31), node = rho / a.G;
-        if (row0 + 32 * r >= (long)s.n * a.G) continue;
-        const float sum = st[r].l + __shfl_xor(st[r].l, 32, 64);
-        // (it is NaN, and so is the row, where a score is; it is 0 where the row saw nothing)
-        const float norm = range.several ? 1.0f : sum == 0.0f ? 0.0f : 1.0f / sum;
-        const size_t slot = prompt_slot(a, tile, kvh, split) * (ROWS / 32) + wave * RT + r;
-        if (range.several && lane < 32) {
-            a.part_ml[slot * 64 + lane] = st[r].m;
-            a.part_ml[slot * 64 + 32 + lane] = sum;
-        }
-        if (node >= s.n) continue;
-#pragma unroll
-        for (int db = 0; db < HD / 32; ++db)
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int j = db * 32 + 8 * u + 4 * (lane >> 5);
-                f32x4 t;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) t[e] = norm == 0.0f ? 0.0f : st[r].o[db][4 * u + e] * norm;
-                if (range.several) *reinterpret_cast<f32x4 *>(a.part_o + slot * 32 * HD + prompt_part_index(lane & 31, j)) = t;
-                else prompt_store<T>(a, (size_t)s.r0 + node, kvh * a.G + rho - node * a.G, HD, j, t);
-            }
+    // what is left the other wavefronts see: this one helps to fetch (in a loop of its own: with a branch around the block above the output would be copied every time)
+    for (; blk < range.last; ++blk) turn();
+    if (w.wild) prompt_add_wild<bf16_t, HD>(w.st, v, a.v_stride, max(range.first, (low + 1) / BLOCK) * BLOCK, min(mine * BLOCK, s.n_keys), sees, lane);
+    prompt_finish<bf16_t, HD>(a, s, w.st, kvh, range.several, prompt_slot(a, tile, kvh, split) * (ROWS / 32) + wave, row0, lane);
+}
+
+// fp32, the same without an order of its own.
+template <int HD, bool WIDE>
+__global__ __launch_bounds__(kPromptWaves * 64, prompt_waves_per_simd(4, HD)) void prompt_attention32_kernel(PromptArgs a) {
+    constexpr int BLOCK = kPromptBlock<float>, BYTES = BLOCK * HD * 4, ROWS = kPromptWaves * 32;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[2][2][BYTES];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int kvh = blockIdx.x % a.n_kv, tile = a.tiles - 1 - blockIdx.x / a.n_kv % a.tiles, split = blockIdx.x / a.n_kv / a.tiles;
+    const PromptTile s = prompt_find_tile(a, ROWS, tile);
+    if (s.b < 0) return;
+    const PromptBlocks range = prompt_blocks(prompt_keys(s.t, s.n, s.n_keys, a.G, ROWS), BLOCK, split, a.n_splits, a.per_split);
+    if (!range.any) return;
+    const float *k = (const float *)a.k + (size_t)s.k0 * a.k_stride + (size_t)kvh * HD, *v = (const float *)a.v + (size_t)s.k0 * a.v_stride + (size_t)kvh * HD;
+    const int row0 = s.t * ROWS + wave * 32, offset = prompt_offset(s.n, s.n_keys), node = (row0 + (lane & 31)) / a.G;
+    PromptState<HD> st;
+    u32x4 q[HD / 8];
+    st.clear();
+    prompt_load_q<float, HD>(a, s, kvh, row0, lane, q);
+    const int sees = node < s.n ? node + offset : -1, low = __builtin_amdgcn_readfirstlane(row0 / a.G + offset);
+    const int mine = row0 / a.G < s.n ? __builtin_amdgcn_readfirstlane(min(range.last, (min((row0 + 31) / a.G, s.n - 1) + offset + BLOCK) / BLOCK)) : 0;
+    const PromptFetch<float, HD, WIDE> fetch_k(a.k_stride, wave, lane), fetch_v(a.v_stride, wave, lane);
+    auto fetch = [&](int blk, int buf) {
+        fetch_k.run(k, a.k_stride, blk * BLOCK, s.n_keys, lds[buf][0], wave, lane);
+        fetch_v.run(v, a.v_stride, blk * BLOCK, s.n_keys, lds[buf][1], wave, lane);
+    };
+    bool wild = false;
+    if (range.first < range.last) fetch(range.first, 0);
+    for (int blk = range.first; blk < range.last; ++blk) {
+        const int buf = (blk - range.first) & 1, t0 = blk * BLOCK;
+        prompt_barrier();     // this block is there, and everybody is done with the last one
+        if (blk + 1 < range.last) fetch(blk + 1, buf ^ 1);
+        if (blk < mine) wild |= prompt_block32<HD>(st, lds[buf][0], lds[buf][1], q, sees - t0, t0 + BLOCK - 1 > low, a.scale_log2e, lane);
     }
+    if (wild) prompt_add_wild<float, HD>(st, v, a.v_stride, max(range.first, (low + 1) / BLOCK) * BLOCK, min(mine * BLOCK, s.n_keys), sees, lane);
+    prompt_finish<float, HD>(a, s, st, kvh, range.several, prompt_slot(a, tile, kvh, split) * (ROWS / 32) + wave, row0, lane);
 }
 
 // Joins the splits of every row that has several: out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  A thread owns four dimensions of a row.
-template <typename T, int HD, int RT>
+template <typename T, int HD>
 __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
-    constexpr int ROWS = kPromptWaves * 32 * RT, QUADS = ROWS * (HD / 4), WGS = QUADS / 256;
+    constexpr int ROWS = kPromptWaves * 32, QUADS = ROWS * (HD / 4), WGS = QUADS / 256;
     const int part = blockIdx.x % WGS, kvh = blockIdx.x / WGS % a.n_kv, tile = blockIdx.x / WGS / a.n_kv;
     const PromptTile s = prompt_find_tile(a, ROWS, tile);
     if (s.b < 0) return;

@@ -59,9 +59,14 @@ int check_prompt(int32_t dtype, int32_t n_rows, int32_t n_seqs, int32_t n_heads,
 
 template <typename T, int HD> void run_prompt(hipStream_t st, const PromptArgs &a, bool wide_kv) {
     const unsigned grid = (unsigned)((size_t)a.tiles * a.n_kv * a.n_splits);
-    if (wide_kv) prompt_attention_kernel<T, HD, 1, true><<<grid, kPromptWaves * 64, 0, st>>>(a);
-    else prompt_attention_kernel<T, HD, 1, false><<<grid, kPromptWaves * 64, 0, st>>>(a);
-    if (a.n_splits > 1) prompt_join_kernel<T, HD, 1><<<(unsigned)((size_t)a.tiles * a.n_kv * (kPromptWaves * 32 * HD / 1024)), 256, 0, st>>>(a);
+    if constexpr (sizeof(T) == 2) {
+        if (wide_kv) prompt_attention16_kernel<HD, true><<<grid, kPromptWaves * 64, 0, st>>>(a);
+        else prompt_attention16_kernel<HD, false><<<grid, kPromptWaves * 64, 0, st>>>(a);
+    } else {
+        if (wide_kv) prompt_attention32_kernel<HD, true><<<grid, kPromptWaves * 64, 0, st>>>(a);
+        else prompt_attention32_kernel<HD, false><<<grid, kPromptWaves * 64, 0, st>>>(a);
+    }
+    if (a.n_splits > 1) prompt_join_kernel<T, HD><<<(unsigned)((size_t)a.tiles * a.n_kv * (kPromptWaves * 32 * HD / 1024)), 256, 0, st>>>(a);
 }
 template <typename T> void run_prompt_type(hipStream_t st, int hd, const PromptArgs &a, bool wide_kv) {
     switch (hd) {

@@ -58,6 +58,9 @@ int main() {
                 seen[p] = 1;
             }
         }
+        const int again = row % 128 == 64 ? 4 : row % 256 == 128 ? 8 : 16;      // pieces after which places repeat
+        for (int t = 0; t < 64; ++t)
+            for (int c = 0; c + again < n; ++c) CHECK(prompt_swizzle(t, c + again, row) == prompt_swizzle(t, c, row) + again && prompt_swizzle(t + 16, c, row) == prompt_swizzle(t, c, row));
         auto bank = [&](int t, int c) { return (t * row / 16 + prompt_swizzle(t, c, row)) % 16; };      // of 16 bytes
         for (int c = 0; c < n; ++c)
             for (int t0 = 0; t0 < 64; t0 += 8) {
