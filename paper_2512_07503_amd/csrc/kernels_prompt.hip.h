@@ -575,31 +575,46 @@ __global__ __launch_bounds__(kPromptWaves * 64, prompt_waves_per_simd(4, HD)) vo
     prompt_finish<float, HD>(a, s, st, kvh, range.several, prompt_slot(a, tile, kvh, split) * (ROWS / 32) + wave, row0, lane);
 }
 
-// Joins the splits of every row that has several: out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  A thread owns four dimensions of a row.
+// Joins the splits of every row that has several: out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  A thread owns four dimensions of a row; eight splits are on their way
+// together.  Where a split saw nothing of a row l = 0.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
-    constexpr int ROWS = kPromptWaves * 32, QUADS = ROWS * (HD / 4), WGS = QUADS / 256;
+    constexpr int ROWS = kPromptWaves * 32, QUADS = ROWS * (HD / 4), WGS = QUADS / 256, N = 8;
     const int part = blockIdx.x % WGS, kvh = blockIdx.x / WGS % a.n_kv, tile = blockIdx.x / WGS / a.n_kv;
     const PromptTile s = prompt_find_tile(a, ROWS, tile);
     if (s.b < 0) return;
-    const int keys = prompt_keys(s.t, s.n, s.n_keys, a.G, ROWS);
-    if (!prompt_blocks(keys, kPromptBlock<T>, 0, a.n_splits, a.per_split).several) return;
+    const int splits = prompt_splits(prompt_keys(s.t, s.n, s.n_keys, a.G, ROWS), kPromptBlock<T>, a.n_splits, a.per_split);
     const int u = part * 256 + threadIdx.x, row = u & 31, j = (u >> 5) % (HD / 4) * 4, sub = (u >> 5) / (HD / 4);
     const int rho = s.t * ROWS + sub * 32 + row, node = rho / a.G;
-    if (node >= s.n) return;
+    if (splits == 1 || node >= s.n) return;
     float m = -INFINITY, denom = 0.0f;
     f32x4 t = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int i = 0; i < a.n_splits && prompt_blocks(keys, kPromptBlock<T>, i, a.n_splits, a.per_split).any; ++i) {
-        const size_t slot = prompt_slot(a, tile, kvh, i) * (ROWS / 32) + sub;
-        const float pm = a.part_ml[slot * 64 + row], pl = a.part_ml[slot * 64 + 32 + row];
-        const f32x4 po = *reinterpret_cast<const f32x4 *>(a.part_o + slot * 32 * HD + prompt_part_index(row, j));
-        if (pl == 0.0f) continue;
-        const float m_new = fmaxf(m, pm), m_use = m_new == -INFINITY ? 0.0f : m_new;
-        const float alpha = __builtin_amdgcn_exp2f(m - m_use), w = __builtin_amdgcn_exp2f(pm - m_use);
-        m = m_new;
-        denom = denom * alpha + w * pl;
+    for (int i0 = 0; i0 < splits; i0 += N) {
+        float pm[N], pl[N];
+        f32x4 po[N];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) t[e] = (finite_f(t[e]) ? t[e] * alpha : t[e]) + (finite_f(po[e]) ? w * po[e] : po[e]);      // (alpha may be 0: not 0 * inf)
+        for (int i = 0; i < N; ++i) {
+            const size_t slot = prompt_slot(a, tile, kvh, min(i0 + i, splits - 1)) * (ROWS / 32) + sub;
+            pm[i] = a.part_ml[slot * 64 + row];
+            pl[i] = i0 + i < splits ? a.part_ml[slot * 64 + 32 + row] : 0.0f;
+            po[i] = *reinterpret_cast<const f32x4 *>(a.part_o + slot * 32 * HD + prompt_part_index(row, j));
+        }
+        float m_new = m;
+#pragma unroll
+        for (int i = 0; i < N; ++i) m_new = fmaxf(m_new, pm[i]);
+        const float m_use = m_new == -INFINITY ? 0.0f : m_new, alpha = __builtin_amdgcn_exp2f(m - m_use);
+        m = m_new;
+        denom *= alpha;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t[e] = finite_f(t[e]) ? t[e] * alpha : t[e];      // (alpha may be 0: not 0 * inf)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (pl[i] == 0.0f) continue;
+            const float w = __builtin_amdgcn_exp2f(pm[i] - m_use);
+            denom += w * pl[i];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t[e] += finite_f(po[i][e]) ? w * po[i][e] : po[i][e];
+        }
     }
     const float inv = denom == 0.0f ? 0.0f : 1.0f / denom;
 #pragma unroll

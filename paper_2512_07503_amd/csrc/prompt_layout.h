@@ -22,16 +22,16 @@ constexpr int prompt_keys(int t, int n, int n_keys, int G, int tile) {
     const int seen = i + 1 + prompt_offset(n, n_keys);
     return seen < 0 ? 0 : seen;
 }
-// Blocks [first, last) of split `split` of at most n_splits, of `per` blocks each (the last of all takes what is left), and whether there is more than one split
+// How many splits there are of a tile whose rows see n_keys_seen keys, of at most n_splits, of `per` blocks each (the last of all takes what is left)
+constexpr int prompt_splits(int n_keys_seen, int block, int n_splits, int per) {
+    const int blocks = (n_keys_seen + block - 1) / block, want = (blocks + per - 1) / per;
+    return want < 1 ? 1 : want < n_splits ? want : n_splits;
+}
+// Blocks [first, last) of split `split`, whether there is such a split, and whether there is more than one
 struct PromptBlocks { int first, last; bool any, several; };
 constexpr PromptBlocks prompt_blocks(int n_keys_seen, int block, int split, int n_splits, int per) {
-    const int blocks = (n_keys_seen + block - 1) / block;
-    PromptBlocks r{0, blocks, split == 0, false};
-    if (n_splits == 1) return r;
-    const int splits = blocks <= per ? 1 : (blocks + per - 1) / per < n_splits ? (blocks + per - 1) / per : n_splits;
-    r.several = splits > 1;
-    r.any = split < splits;
-    r.first = split * per < blocks ? split * per : blocks;
+    const int blocks = (n_keys_seen + block - 1) / block, splits = prompt_splits(n_keys_seen, block, n_splits, per);
+    PromptBlocks r{split * per < blocks ? split * per : blocks, blocks, split < splits, splits > 1};
     if (split + 1 < splits) r.last = r.first + per;
     return r;
 }

@@ -24,13 +24,15 @@ template <typename T> void run_norm_rotary(hipStream_t st, dim3 grid, int team, 
 // ------------------------------------------------------------------------------------------------------------- attention
 struct PromptPlan { int tiles, n_splits, per_split; size_t part_o, part_ml; };
 
-// Rows a tile, and how many ways the keys of a tile are split: until 512 workgroups are there, two for each of the 256 CUs, but no split with less than four blocks of keys.
+// How many ways the keys of a tile are split: not at all where there is a workgroup for each of the 512 that the card holds, two a CU, without (what is split is written and read
+// once more); else into three times as many, of at least four blocks each, as sequences' lengths differ (1000 rows in 264 tiles behind 21 000 and 30 000 keys: 1, 2, 4, 6, 8, 12 ways: 550,
+// 461, 456, 432, 434, 438 us).
 PromptPlan prompt_plan(int dtype, int n_rows, int n_seqs, int n_heads, int n_kv, int hd, int max_kv) {
     PromptPlan p;
     const int G = n_heads / n_kv, rows = kPromptWaves * 32, block = dtype == SJD_F32 ? kPromptBlock<float> : kPromptBlock<bf16_t>;
     p.tiles = (int)prompt_max_tiles(n_rows, n_seqs, G, rows);
     const size_t work = (size_t)p.tiles * n_kv, blocks = ceil_div_sz((size_t)max_kv, block);
-    const size_t want = ceil_div_sz(512, work ? work : 1), most = blocks / 4 ? blocks / 4 : 1;
+    const size_t want = work >= 512 ? 1 : ceil_div_sz(1536, work ? work : 1), most = blocks / 4 ? blocks / 4 : 1;
     p.n_splits = (int)(want < most ? want : most);
     p.per_split = (int)ceil_div_sz(blocks ? blocks : 1, p.n_splits);
     const size_t slots = p.n_splits > 1 ? work * p.n_splits * (rows / 32) : 0;
