@@ -8,47 +8,68 @@ struct NormRotaryArgs {
     RotaryArgs r;
     const void *gain[2], *bias[2];   // of queries, keys; a bias may be NULL
     int per_head;                    // gains and biases are [heads][hd], else [hd]
-    int layer;                       // subtract the mean
     float eps;
 };
 
+// Sum over a team of lanes (1, 2, .. 64, aligned), in every one of them.  Within 16 lanes by moves that are part of an addition: neighbours, pairs, then mirror images of 8 and of
+// 16 lanes, whose halves hold one number each by then.
+template <int CTRL> SJD_D float norm_moved(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xF, 0xF, true)); }
+template <int TEAM> SJD_D float norm_sum(float x) {
+    if constexpr (TEAM > 1) x += norm_moved<0xB1>(x);        // lanes 1 0 3 2
+    if constexpr (TEAM > 2) x += norm_moved<0x4E>(x);        // 2 3 0 1
+    if constexpr (TEAM > 4) x += norm_moved<0x141>(x);       // 7 6 .. 0
+    if constexpr (TEAM > 8) x += norm_moved<0x140>(x);       // 15 14 .. 0
+    if constexpr (TEAM > 16) {
+        const auto y = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(int, x), __builtin_bit_cast(int, x), false, false);
+        x = __builtin_bit_cast(float, (int)y[0]) + __builtin_bit_cast(float, (int)y[1]);
+    }
+    if constexpr (TEAM > 32) {
+        const auto y = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(int, x), __builtin_bit_cast(int, x), false, false);
+        x = __builtin_bit_cast(float, (int)y[0]) + __builtin_bit_cast(float, (int)y[1]);
+    }
+    return x;
+}
+
 // y = ((x * pre - shift) - off) * scale
 struct NormStats { float pre, shift, off, scale; };
-// From a lane's elements (0 where it has none, has[e] false) and a sum over the lanes of the head.  Squares of elements beyond 2^60 do not fit: then the
+// From a lane's elements (0 where it has none, has(e) false).  Squares of elements beyond 2^60 do not fit: then the
 // elements are taken 2^-72 times as large (the norm does not change, but for eps, which is far below).  What the mean's rounding leaves, the mean of the
 // differences from it, is taken off as well: it would be 2^-24 of the mean, which may be many times the deviation.
-template <int N, typename Sum, typename Has> SJD_D NormStats norm_stats(const float (&x)[N], Has has, int hd, bool layer, float eps, Sum sum) {
+template <int N, int TEAM, bool LAYER> SJD_D void norm_moments(const float (&x)[N], uint32_t has, float inv, float pre, NormStats &s, float &var) {
+    s.pre = pre;
+    s.shift = s.off = 0.0f;
+    if constexpr (LAYER) {
+        float t = 0.0f;
+#pragma unroll
+        for (int e = 0; e < N; ++e) t = fmaf(x[e], pre, t);
+        s.shift = norm_sum<TEAM>(t) * inv;
+        asm volatile("" : "+v"(s.shift));      // (the rounded one, also in the differences: fused with them the product would not be)
+    }
+    float first = 0.0f, second = 0.0f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        float d = x[e] * pre;
+        if constexpr (LAYER) {
+            d = has >> e & 1u ? d - s.shift : 0.0f;
+            first += d;
+        }
+        second = fmaf(d, d, second);
+    }
+    var = norm_sum<TEAM>(second) * inv;
+    if constexpr (LAYER) {
+        s.off = norm_sum<TEAM>(first) * inv;
+        const float less = var - s.off * s.off;
+        var = less < 0.0f ? 0.0f : less;
+    }
+}
+template <int N, int TEAM, bool LAYER> SJD_D NormStats norm_stats(const float (&x)[N], uint32_t has, int hd, float eps) {
     NormStats s;
     const float inv = 1.0f / (float)hd;
-    auto moments = [&](float pre, float &shift, float &off, float &var) {
-        shift = off = 0.0f;
-        if (layer) {
-            float t = 0.0f;
-#pragma unroll
-            for (int e = 0; e < N; ++e) t += x[e] * pre;
-            shift = sum(t) * inv;
-        }
-        float first = 0.0f, second = 0.0f;
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const float d = has(e) ? x[e] * pre - shift : 0.0f;
-            first += d;
-            second = fmaf(d, d, second);
-        }
-        var = sum(second) * inv;
-        if (layer) {
-            off = sum(first) * inv;
-            const float less = var - off * off;
-            var = less < 0.0f ? 0.0f : less;
-        }
-    };
     float var;
-    s.pre = 1.0f;
-    moments(1.0f, s.shift, s.off, var);
+    norm_moments<N, TEAM, LAYER>(x, has, inv, 1.0f, s, var);
     if (!(var < INFINITY)) {
-        s.pre = 0x1p-72f;
+        norm_moments<N, TEAM, LAYER>(x, has, inv, 0x1p-72f, s, var);
         eps = 0x1p-126f;
-        moments(s.pre, s.shift, s.off, var);
     }
     s.scale = 1.0f / sqrtf(var + eps);
     return s;
@@ -56,47 +77,65 @@ template <int N, typename Sum, typename Has> SJD_D NormStats norm_stats(const fl
 
 // WIDE rows (16-byte aligned, in pieces of 8 elements).  A lane of the team has two pieces: the two halves of 8 turned pairs, or what lies behind the turned part;
 // interleaved: 16 elements in a row.
-template <typename T, int TEAM>
+template <typename T, int TEAM, bool LAYER>
 __global__ __launch_bounds__(256) void norm_rotary_kernel(NormRotaryArgs p) {
     const RotaryArgs &a = p.r;
     __shared__ float2 cs[8 * kRotaryMaxHalf];   // (cos, sin) * magnitude of [row][pair]; rows_per_wg * half <= 8 * 256
     const int row0 = blockIdx.x * a.rows_per_wg, rows = min(a.rows_per_wg, a.n_rows - row0), tid = threadIdx.x;
     const int half = a.half, heads = a.heads[0] + a.heads[1], hd = a.hd;
-    for (int u = tid; u < rows * half; u += 256) {
-        const int r = u / half, i = u - r * half;
-        float s, c;
-        sincos_turns((uint64_t)(int64_t)a.positions[row0 + r] * a.table[i], s, c);
-        cs[u] = float2{c * a.magnitude, s * a.magnitude};
-    }
-    __syncthreads();
     const int unit = tid & (TEAM - 1), turned = a.interleaved ? (hd + 15) >> 4 : half >> 3;
     const bool turn = unit < turned;
     const int j0 = a.interleaved ? 16 * unit : turn ? 8 * unit : 2 * half + 16 * (unit - turned);
     const int j1 = !a.interleaved && turn ? j0 + half : j0 + 8;
     const bool has0 = j0 < hd, has1 = j1 < hd;
-    const int total = rows * heads, step = gridDim.y * (256 / TEAM);
-    for (int u = blockIdx.y * (256 / TEAM) + tid / TEAM; u < total; u += step) {
-        const int r = u / heads, hh = u - r * heads, side = hh >= a.heads[0], h = side ? hh - a.heads[0] : hh;
-        const T *x = (const T *)a.x[side] + (size_t)(row0 + r) * a.x_stride[side] + (size_t)h * hd;
-        T *y = (T *)a.y[side] + (size_t)(row0 + r) * a.y_stride[side] + (size_t)h * hd;
+    // heads of the workgroup's rows, a team's one behind the other: head hh of row r
+    const int step = gridDim.y * (256 / TEAM), dr = step / heads, dh = step - dr * heads;
+    int r = (blockIdx.y * (256 / TEAM) + tid / TEAM) / heads, hh = blockIdx.y * (256 / TEAM) + tid / TEAM - r * heads;
+    Raw8<T> x[2], g[2], b[2];
+    auto load = [&]() {
+        const int side = hh >= a.heads[0], h = side ? hh - a.heads[0] : hh;
+        const T *px = (const T *)a.x[side] + (size_t)(row0 + r) * a.x_stride[side] + (size_t)h * hd;
         const size_t g0 = p.per_head ? (size_t)h * hd : 0;
-        const T *gain = (const T *)p.gain[side] + g0, *bias = p.bias[side] ? (const T *)p.bias[side] + g0 : nullptr;
-        float v[16] = {}, g[16] = {}, b[16] = {};
-        float (&v0)[8] = reinterpret_cast<float (&)[8]>(v[0]), (&v1)[8] = reinterpret_cast<float (&)[8]>(v[8]);
-        if (has0) load8(x + j0, true, v0);
-        if (has1) load8(x + j1, true, v1);
-        if (has0) load8(gain + j0, true, reinterpret_cast<float (&)[8]>(g[0]));
-        if (has1) load8(gain + j1, true, reinterpret_cast<float (&)[8]>(g[8]));
-        if (bias && has0) load8(bias + j0, true, reinterpret_cast<float (&)[8]>(b[0]));
-        if (bias && has1) load8(bias + j1, true, reinterpret_cast<float (&)[8]>(b[8]));
-        const NormStats s = norm_stats<16>(v, [&](int e) { return e < 8 ? has0 : has1; }, hd, p.layer, p.eps, [](float t) {
+        const T *pg = (const T *)p.gain[side] + g0, *pb = (const T *)p.bias[side] + g0;
+        if (has0) { x[0] = load_raw8(px + j0); g[0] = load_raw8(pg + j0); }
+        if (has1) { x[1] = load_raw8(px + j1); g[1] = load_raw8(pg + j1); }
+        if (p.bias[side]) {
+            if (has0) b[0] = load_raw8(pb + j0);
+            if (has1) b[1] = load_raw8(pb + j1);
+        } else {
 #pragma unroll
-            for (int d = 1; d < TEAM; d <<= 1) t += __shfl_xor(t, d, 64);
-            return t;
-        });
+            for (int i = 0; i < 2; ++i) b[i] = Raw8<T>{};
+        }
+    };
 #pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] = fmaf((v[e] * s.pre - s.shift - s.off) * s.scale, g[e], b[e]);
+    for (int i = 0; i < 2; ++i) x[i] = g[i] = b[i] = Raw8<T>{};
+    if (r < rows) load();
+    for (int u = tid; u < rows * half; u += 256) {
+        const int rr = u / half, i = u - rr * half;
+        float s, c;
+        sincos_turns((uint64_t)(int64_t)a.positions[row0 + rr] * a.table[i], s, c);
+        cs[u] = float2{c * a.magnitude, s * a.magnitude};
+    }
+    __syncthreads();
+    while (r < rows) {
+        float v0[8], v1[8], g0[8], g1[8], b0[8], b1[8], v[16];
+        unpack8(x[0], v0); unpack8(x[1], v1); unpack8(g[0], g0); unpack8(g[1], g1); unpack8(b[0], b0); unpack8(b[1], b1);
         const float2 *w = cs + r * half;
+        const int side = hh >= a.heads[0];
+        T *y = (T *)a.y[side] + (size_t)(row0 + r) * a.y_stride[side] + (size_t)(side ? hh - a.heads[0] : hh) * hd;
+        r += dr;
+        hh += dh;
+        if (hh >= heads) { hh -= heads; ++r; }
+        if (r < rows) load();          // the next head, while this one is worked on
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] = e < 8 ? v0[e & 7] : v1[e & 7];
+        const NormStats s = norm_stats<16, TEAM, LAYER>(v, (has0 ? 0xFFu : 0u) | (has1 ? 0xFF00u : 0u), hd, p.eps);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            float d = v[e] * s.pre;
+            if constexpr (LAYER) d = d - s.shift - s.off;
+            v[e] = fmaf(d * s.scale, e < 8 ? g0[e & 7] : g1[e & 7], e < 8 ? b0[e & 7] : b1[e & 7]);
+        }
         if (a.interleaved) {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -110,18 +149,20 @@ __global__ __launch_bounds__(256) void norm_rotary_kernel(NormRotaryArgs p) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float2 t = w[j0 + e];
-                const float a0 = v0[e], a1 = v1[e];
-                v0[e] = fmaf(a0, t.x, -(a1 * t.y));
-                v1[e] = fmaf(a1, t.x, a0 * t.y);
+                const float a0 = v[e], a1 = v[8 + e];
+                v[e] = fmaf(a0, t.x, -(a1 * t.y));
+                v[8 + e] = fmaf(a1, t.x, a0 * t.y);
             }
         }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { v0[e] = v[e]; v1[e] = v[8 + e]; }
         if (has0) store8(y + j0, true, v0);
         if (has1) store8(y + j1, true, v1);
     }
 }
 
 // Any alignment and sizes: a wavefront a head, a lane has pairs lane + 64 n and elements behind the turned part 2 half + lane + 64 n.
-template <typename T>
+template <typename T, bool LAYER>
 __global__ __launch_bounds__(256) void norm_rotary_any_kernel(NormRotaryArgs p) {
     const RotaryArgs &a = p.r;
     const int row = blockIdx.x, lane = threadIdx.x & 63, half = a.half, hd = a.hd, rest = hd - 2 * half, heads = a.heads[0] + a.heads[1];
@@ -143,13 +184,13 @@ __global__ __launch_bounds__(256) void norm_rotary_any_kernel(NormRotaryArgs p) 
         auto at = [&](int e) { return e < 8 ? (a.interleaved ? 2 * (lane + 64 * (e >> 1)) + (e & 1) : lane + 64 * (e >> 1) + (e & 1) * half) : 2 * half + lane + 64 * (e - 8); };
         auto has = [&](int e) { return e < 8 ? lane + 64 * (e >> 1) < half : lane + 64 * (e - 8) < rest; };
         float v[16];
+        uint32_t there = 0u;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] = has(e) ? to_float<T>(x[at(e)]) : 0.0f;
-        const NormStats s = norm_stats<16>(v, has, hd, p.layer, p.eps, [](float t) {
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) t += __shfl_xor(t, d, 64);
-            return t;
-        });
+        for (int e = 0; e < 16; ++e) {
+            v[e] = has(e) ? to_float<T>(x[at(e)]) : 0.0f;
+            there |= has(e) ? 1u << e : 0u;
+        }
+        const NormStats s = norm_stats<16, 64, LAYER>(v, there, hd, p.eps);
 #pragma unroll
         for (int e = 0; e < 16; ++e)
             if (has(e)) v[e] = fmaf((v[e] * s.pre - s.shift - s.off) * s.scale, to_float<T>(gain[at(e)]), bias ? to_float<T>(bias[at(e)]) : 0.0f);

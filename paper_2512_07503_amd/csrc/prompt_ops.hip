@@ -10,15 +10,19 @@
 
 namespace {
 
-template <typename T> void run_norm_rotary(hipStream_t st, dim3 grid, int team, const NormRotaryArgs &a) {
+template <typename T, bool LAYER> void run_norm_rotary(hipStream_t st, dim3 grid, int team, const NormRotaryArgs &a) {
     switch (team) {
-    case 1: norm_rotary_kernel<T, 1><<<grid, 256, 0, st>>>(a); break;
-    case 2: norm_rotary_kernel<T, 2><<<grid, 256, 0, st>>>(a); break;
-    case 4: norm_rotary_kernel<T, 4><<<grid, 256, 0, st>>>(a); break;
-    case 8: norm_rotary_kernel<T, 8><<<grid, 256, 0, st>>>(a); break;
-    case 16: norm_rotary_kernel<T, 16><<<grid, 256, 0, st>>>(a); break;
-    default: norm_rotary_kernel<T, 32><<<grid, 256, 0, st>>>(a); break;
+    case 0: norm_rotary_any_kernel<T, LAYER><<<grid, 256, 0, st>>>(a); break;
+    case 1: norm_rotary_kernel<T, 1, LAYER><<<grid, 256, 0, st>>>(a); break;
+    case 2: norm_rotary_kernel<T, 2, LAYER><<<grid, 256, 0, st>>>(a); break;
+    case 4: norm_rotary_kernel<T, 4, LAYER><<<grid, 256, 0, st>>>(a); break;
+    case 8: norm_rotary_kernel<T, 8, LAYER><<<grid, 256, 0, st>>>(a); break;
+    case 16: norm_rotary_kernel<T, 16, LAYER><<<grid, 256, 0, st>>>(a); break;
+    default: norm_rotary_kernel<T, 32, LAYER><<<grid, 256, 0, st>>>(a); break;
     }
+}
+template <typename T> void run_norm_rotary_type(hipStream_t st, dim3 grid, int team, bool layer, const NormRotaryArgs &a) {
+    layer ? run_norm_rotary<T, true>(st, grid, team, a) : run_norm_rotary<T, false>(st, grid, team, a);
 }
 
 // ------------------------------------------------------------------------------------------------------------- attention
@@ -108,7 +112,7 @@ int sjd_op_norm_rotary(void *hip_stream, int32_t dtype, int32_t norm, float eps,
                        const void *k_gain, const void *k_bias, void *k_out, int64_t k_out_stride, int32_t n_kv_heads) {
     NormRotaryArgs a = {{table, positions, {q, k}, {q_out, k_out}, {(long)q_stride, (long)k_stride}, {(long)q_out_stride, (long)k_out_stride},
                          {n_heads, n_kv_heads}, n_rows, head_dim, rotary_dim / 2, interleaved ? 1 : 0, 1, magnitude},
-                        {q_gain, k_gain}, {q_bias, k_bias}, per_head ? 1 : 0, norm == SJD_NORM_LAYER ? 1 : 0, eps};
+                        {q_gain, k_gain}, {q_bias, k_bias}, per_head ? 1 : 0, eps};
     bool w;
     const int rc = rotary_check(a.r, dtype, rotary_dim, w);
     if (rc) return rc;
@@ -131,20 +135,18 @@ int sjd_op_norm_rotary(void *hip_stream, int32_t dtype, int32_t norm, float eps,
     if (!n_rows) return SJD_OK;
     hipStream_t st = (hipStream_t)hip_stream;
     const int heads = n_heads + n_kv_heads;
+    int team = 0;            // lanes a head: one for 16 elements, 0: any rows
+    dim3 grid;
     if (w) {
-        // lanes a head: one for 16 elements
         const int need = a.r.interleaved ? (head_dim + 15) / 16 : a.r.half / 8 + (head_dim - rotary_dim + 15) / 16;
-        int team = 1;
-        while (team < need) team *= 2;
-        dim3 grid;
+        for (team = 1; team < need;) team *= 2;
         if (!rotary_grid(a.r, (long)heads * team, grid)) TREE_FAIL(SJD_EINVAL, "too many rows for one launch");
-        dtype == SJD_F32 ? run_norm_rotary<float>(st, grid, team, a) : run_norm_rotary<bf16_t>(st, grid, team, a);
     } else {
         if ((size_t)n_rows > kMaxWorkgroups) TREE_FAIL(SJD_EINVAL, "too many rows for one launch");
-        const dim3 grid(n_rows, n_rows >= 512 ? 1 : ceil_div(heads, 4) < 512 / n_rows + 1 ? ceil_div(heads, 4) : 512 / n_rows + 1);
-        if (dtype == SJD_F32) norm_rotary_any_kernel<float><<<grid, 256, 0, st>>>(a);
-        else norm_rotary_any_kernel<bf16_t><<<grid, 256, 0, st>>>(a);
+        grid = dim3(n_rows, n_rows >= 512 ? 1 : ceil_div(heads, 4) < 512 / n_rows + 1 ? ceil_div(heads, 4) : 512 / n_rows + 1);
     }
+    const bool layer = norm == SJD_NORM_LAYER;
+    dtype == SJD_F32 ? run_norm_rotary_type<float>(st, grid, team, layer, a) : run_norm_rotary_type<bf16_t>(st, grid, team, layer, a);
     TREE_TRY(hipGetLastError());
     return SJD_OK;
 }
