@@ -30,54 +30,53 @@ template <int TEAM> SJD_D float norm_sum(float x) {
     return x;
 }
 
-// y = ((x * pre - shift) - off) * scale
-struct NormStats { float pre, shift, off, scale; };
-// From a lane's elements (0 where it has none, has(e) false).  Squares of elements beyond 2^60 do not fit: then the
-// elements are taken 2^-72 times as large (the norm does not change, but for eps, which is far below).  What the mean's rounding leaves, the mean of the
-// differences from it, is taken off as well: it would be 2^-24 of the mean, which may be many times the deviation.
-template <int N, int TEAM, bool LAYER> SJD_D void norm_moments(const float (&x)[N], uint32_t has, float inv, float pre, NormStats &s, float &var) {
-    s.pre = pre;
-    s.shift = s.off = 0.0f;
+// The normalised x in its place: z = (x - c) / sqrt(mean((x - c)^2) + eps), of a lane's elements (0 where it has none: bit e of `has`; FULL: it has all).
+// With means: c rounded is 2^-24 of it off, which may be many times the deviation, so what it leaves, the mean of the differences from it, is taken off as well.
+// Squares of elements beyond 2^60 do not fit: then they are taken 2^-72 times as large (the norm does not change, but for eps, which is far below).
+template <int N, int TEAM, bool LAYER, bool FULL> SJD_D float norm_moments(float (&x)[N], uint32_t has, float inv, float &off) {
+    off = 0.0f;
+    float first = 0.0f, second = 0.0f;
     if constexpr (LAYER) {
         float t = 0.0f;
 #pragma unroll
-        for (int e = 0; e < N; ++e) t = fmaf(x[e], pre, t);
-        s.shift = norm_sum<TEAM>(t) * inv;
-        asm volatile("" : "+v"(s.shift));      // (the rounded one, also in the differences: fused with them the product would not be)
-    }
-    float first = 0.0f, second = 0.0f;
+        for (int e = 0; e < N; ++e) t += x[e];
+        float c = norm_sum<TEAM>(t) * inv;
+        asm volatile("" : "+v"(c));      // (the rounded one in all differences: fused with one of them the product would not be)
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-        float d = x[e] * pre;
-        if constexpr (LAYER) {
-            d = has >> e & 1u ? d - s.shift : 0.0f;
-            first += d;
+        for (int e = 0; e < N; ++e) {
+            x[e] = FULL || (has >> e & 1u) ? x[e] - c : 0.0f;
+            first += x[e];
         }
-        second = fmaf(d, d, second);
     }
-    var = norm_sum<TEAM>(second) * inv;
-    if constexpr (LAYER) {
-        s.off = norm_sum<TEAM>(first) * inv;
-        const float less = var - s.off * s.off;
-        var = less < 0.0f ? 0.0f : less;
-    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) second = fmaf(x[e], x[e], second);
+    const float var = norm_sum<TEAM>(second) * inv;
+    if constexpr (!LAYER) return var;
+    off = norm_sum<TEAM>(first) * inv;
+    const float less = var - off * off;
+    return less < 0.0f ? 0.0f : less;
 }
-template <int N, int TEAM, bool LAYER> SJD_D NormStats norm_stats(const float (&x)[N], uint32_t has, int hd, float eps) {
-    NormStats s;
+template <int N, int TEAM, bool LAYER, bool FULL> SJD_D void normalise(float (&x)[N], uint32_t has, int hd, float eps) {
     const float inv = 1.0f / (float)hd;
-    float var;
-    norm_moments<N, TEAM, LAYER>(x, has, inv, 1.0f, s, var);
+    float y[N], off;
+    if constexpr (LAYER)
+#pragma unroll
+        for (int e = 0; e < N; ++e) y[e] = x[e];
+    float var = norm_moments<N, TEAM, LAYER, FULL>(x, has, inv, off);
     if (!(var < INFINITY)) {
-        norm_moments<N, TEAM, LAYER>(x, has, inv, 0x1p-72f, s, var);
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = (LAYER ? y[e] : x[e]) * 0x1p-72f;
+        var = norm_moments<N, TEAM, LAYER, FULL>(x, has, inv, off);
         eps = 0x1p-126f;
     }
-    s.scale = 1.0f / sqrtf(var + eps);
-    return s;
+    const float scale = 1.0f / sqrtf(var + eps), less = -off * scale;
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = LAYER ? fmaf(x[e], scale, less) : x[e] * scale;
 }
 
 // WIDE rows (16-byte aligned, in pieces of 8 elements).  A lane of the team has two pieces: the two halves of 8 turned pairs, or what lies behind the turned part;
 // interleaved: 16 elements in a row.
-template <typename T, int TEAM, bool LAYER>
+template <typename T, int TEAM, bool LAYER, bool FULL>
 __global__ __launch_bounds__(256) void norm_rotary_kernel(NormRotaryArgs p) {
     const RotaryArgs &a = p.r;
     __shared__ float2 cs[8 * kRotaryMaxHalf];   // (cos, sin) * magnitude of [row][pair]; rows_per_wg * half <= 8 * 256
@@ -87,7 +86,7 @@ __global__ __launch_bounds__(256) void norm_rotary_kernel(NormRotaryArgs p) {
     const bool turn = unit < turned;
     const int j0 = a.interleaved ? 16 * unit : turn ? 8 * unit : 2 * half + 16 * (unit - turned);
     const int j1 = !a.interleaved && turn ? j0 + half : j0 + 8;
-    const bool has0 = j0 < hd, has1 = j1 < hd;
+    const bool has0 = FULL || j0 < hd, has1 = FULL || j1 < hd;
     // heads of the workgroup's rows, a team's one behind the other: head hh of row r
     const int step = gridDim.y * (256 / TEAM), dr = step / heads, dh = step - dr * heads;
     int r = (blockIdx.y * (256 / TEAM) + tid / TEAM) / heads, hh = blockIdx.y * (256 / TEAM) + tid / TEAM - r * heads;
@@ -129,13 +128,9 @@ __global__ __launch_bounds__(256) void norm_rotary_kernel(NormRotaryArgs p) {
         if (r < rows) load();          // the next head, while this one is worked on
 #pragma unroll
         for (int e = 0; e < 16; ++e) v[e] = e < 8 ? v0[e & 7] : v1[e & 7];
-        const NormStats s = norm_stats<16, TEAM, LAYER>(v, (has0 ? 0xFFu : 0u) | (has1 ? 0xFF00u : 0u), hd, p.eps);
+        normalise<16, TEAM, LAYER, FULL>(v, (has0 ? 0xFFu : 0u) | (has1 ? 0xFF00u : 0u), hd, p.eps);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            float d = v[e] * s.pre;
-            if constexpr (LAYER) d = d - s.shift - s.off;
-            v[e] = fmaf(d * s.scale, e < 8 ? g0[e & 7] : g1[e & 7], e < 8 ? b0[e & 7] : b1[e & 7]);
-        }
+        for (int e = 0; e < 16; ++e) v[e] = fmaf(v[e], e < 8 ? g0[e & 7] : g1[e & 7], e < 8 ? b0[e & 7] : b1[e & 7]);
         if (a.interleaved) {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -190,10 +185,10 @@ __global__ __launch_bounds__(256) void norm_rotary_any_kernel(NormRotaryArgs p) 
             v[e] = has(e) ? to_float<T>(x[at(e)]) : 0.0f;
             there |= has(e) ? 1u << e : 0u;
         }
-        const NormStats s = norm_stats<16, 64, LAYER>(v, there, hd, p.eps);
+        normalise<16, 64, LAYER, false>(v, there, hd, p.eps);
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-            if (has(e)) v[e] = fmaf((v[e] * s.pre - s.shift - s.off) * s.scale, to_float<T>(gain[at(e)]), bias ? to_float<T>(bias[at(e)]) : 0.0f);
+            if (has(e)) v[e] = fmaf(v[e], to_float<T>(gain[at(e)]), bias ? to_float<T>(bias[at(e)]) : 0.0f);
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
             const float a0 = v[2 * n], a1 = v[2 * n + 1];

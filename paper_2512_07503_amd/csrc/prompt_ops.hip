@@ -10,15 +10,19 @@
 
 namespace {
 
+template <typename T, int TEAM, bool LAYER> void run_norm_rotary_team(hipStream_t st, dim3 grid, const NormRotaryArgs &a) {
+    if (a.r.hd == 16 * TEAM) norm_rotary_kernel<T, TEAM, LAYER, true><<<grid, 256, 0, st>>>(a);
+    else norm_rotary_kernel<T, TEAM, LAYER, false><<<grid, 256, 0, st>>>(a);
+}
 template <typename T, bool LAYER> void run_norm_rotary(hipStream_t st, dim3 grid, int team, const NormRotaryArgs &a) {
     switch (team) {
     case 0: norm_rotary_any_kernel<T, LAYER><<<grid, 256, 0, st>>>(a); break;
-    case 1: norm_rotary_kernel<T, 1, LAYER><<<grid, 256, 0, st>>>(a); break;
-    case 2: norm_rotary_kernel<T, 2, LAYER><<<grid, 256, 0, st>>>(a); break;
-    case 4: norm_rotary_kernel<T, 4, LAYER><<<grid, 256, 0, st>>>(a); break;
-    case 8: norm_rotary_kernel<T, 8, LAYER><<<grid, 256, 0, st>>>(a); break;
-    case 16: norm_rotary_kernel<T, 16, LAYER><<<grid, 256, 0, st>>>(a); break;
-    default: norm_rotary_kernel<T, 32, LAYER><<<grid, 256, 0, st>>>(a); break;
+    case 1: run_norm_rotary_team<T, 1, LAYER>(st, grid, a); break;
+    case 2: run_norm_rotary_team<T, 2, LAYER>(st, grid, a); break;
+    case 4: run_norm_rotary_team<T, 4, LAYER>(st, grid, a); break;
+    case 8: run_norm_rotary_team<T, 8, LAYER>(st, grid, a); break;
+    case 16: run_norm_rotary_team<T, 16, LAYER>(st, grid, a); break;
+    default: run_norm_rotary_team<T, 32, LAYER>(st, grid, a); break;
     }
 }
 template <typename T> void run_norm_rotary_type(hipStream_t st, dim3 grid, int team, bool layer, const NormRotaryArgs &a) {
