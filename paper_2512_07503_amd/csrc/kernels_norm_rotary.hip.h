@@ -35,24 +35,24 @@ template <int TEAM> SJD_D float norm_sum(float x) {
 // Squares of elements beyond 2^60 do not fit: then they are taken 2^-72 times as large (the norm does not change, but for eps, which is far below).
 template <int N, int TEAM, bool LAYER, bool FULL> SJD_D float norm_moments(float (&x)[N], uint32_t has, float inv, float &off) {
     off = 0.0f;
-    float first = 0.0f, second = 0.0f;
+    float first[2] = {0.0f, 0.0f}, second[2] = {0.0f, 0.0f};      // (two chains of additions each)
     if constexpr (LAYER) {
-        float t = 0.0f;
+        float t[2] = {0.0f, 0.0f};
 #pragma unroll
-        for (int e = 0; e < N; ++e) t += x[e];
-        float c = norm_sum<TEAM>(t) * inv;
+        for (int e = 0; e < N; ++e) t[e & 1] += x[e];
+        float c = norm_sum<TEAM>(t[0] + t[1]) * inv;
         asm volatile("" : "+v"(c));      // (the rounded one in all differences: fused with one of them the product would not be)
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             x[e] = FULL || (has >> e & 1u) ? x[e] - c : 0.0f;
-            first += x[e];
+            first[e & 1] += x[e];
         }
     }
 #pragma unroll
-    for (int e = 0; e < N; ++e) second = fmaf(x[e], x[e], second);
-    const float var = norm_sum<TEAM>(second) * inv;
+    for (int e = 0; e < N; ++e) second[e & 1] = fmaf(x[e], x[e], second[e & 1]);
+    const float var = norm_sum<TEAM>(second[0] + second[1]) * inv;
     if constexpr (!LAYER) return var;
-    off = norm_sum<TEAM>(first) * inv;
+    off = norm_sum<TEAM>(first[0] + first[1]) * inv;
     const float less = var - off * off;
     return less < 0.0f ? 0.0f : less;
 }
@@ -69,7 +69,7 @@ template <int N, int TEAM, bool LAYER, bool FULL> SJD_D void normalise(float (&x
         var = norm_moments<N, TEAM, LAYER, FULL>(x, has, inv, off);
         eps = 0x1p-126f;
     }
-    const float scale = 1.0f / sqrtf(var + eps), less = -off * scale;
+    const float scale = __builtin_amdgcn_rsqf(var + eps), less = -off * scale;     // (within 2^-23; the argument is at least 1e-30)
 #pragma unroll
     for (int e = 0; e < N; ++e) x[e] = LAYER ? fmaf(x[e], scale, less) : x[e] * scale;
 }

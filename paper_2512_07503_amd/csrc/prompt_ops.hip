@@ -144,7 +144,8 @@ int sjd_op_norm_rotary(void *hip_stream, int32_t dtype, int32_t norm, float eps,
     if (w) {
         const int need = a.r.interleaved ? (head_dim + 15) / 16 : a.r.half / 8 + (head_dim - rotary_dim + 15) / 16;
         for (team = 1; team < need;) team *= 2;
-        if (!rotary_grid(a.r, (long)heads * team, grid)) TREE_FAIL(SJD_EINVAL, "too many rows for one launch");
+        // (2 rows a workgroup at most, 4, 8: 9 408 rows of 64 heads of 128 with means, gains and biases 61.9, 65.3, 68.7 us, 12 000 rows of 40 heads 40.4, 40.0, 43.0)
+        if (!rotary_grid(a.r, 2, (long)heads * team, grid)) TREE_FAIL(SJD_EINVAL, "too many rows for one launch");
     } else {
         if ((size_t)n_rows > kMaxWorkgroups) TREE_FAIL(SJD_EINVAL, "too many rows for one launch");
         grid = dim3(n_rows, n_rows >= 512 ? 1 : ceil_div(heads, 4) < 512 / n_rows + 1 ? ceil_div(heads, 4) : 512 / n_rows + 1);

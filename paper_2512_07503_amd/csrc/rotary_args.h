@@ -34,9 +34,9 @@ inline int rotary_check(const RotaryArgs &a, int32_t dtype, int32_t rotary_dim, 
 }
 
 // Rows a workgroup: their sines and cosines are shared by the heads of a row only, so more rows mean nothing but fewer workgroups;
-// two for each of the 256 CUs, and few rows are split over their heads' units (of which a row has `units`) instead.
-inline bool rotary_grid(RotaryArgs &a, long units, dim3 &grid) {
-    while (a.rows_per_wg < 8 && a.rows_per_wg * a.half * 2 <= 8 * kRotaryMaxHalf && a.n_rows / (2 * a.rows_per_wg) >= 512) a.rows_per_wg *= 2;
+// two for each of the 256 CUs, and few rows are split over their heads' units (of which a row has `units`) instead.  most_rows <= 8.
+inline bool rotary_grid(RotaryArgs &a, int most_rows, long units, dim3 &grid) {
+    while (a.rows_per_wg < most_rows && a.rows_per_wg * a.half * 2 <= 8 * kRotaryMaxHalf && a.n_rows / (2 * a.rows_per_wg) >= 512) a.rows_per_wg *= 2;
     const unsigned gx = (unsigned)ceil_div(a.n_rows, a.rows_per_wg);
     if (gx > kMaxWorkgroups) return false;
     long gy = gx >= 512 ? 1 : 512 / gx;

@@ -220,7 +220,7 @@ int sjd_op_rotary(void *hip_stream, int32_t dtype, int32_t interleaved, const ui
     const int rc = rotary_check(a, dtype, rotary_dim, w);
     if (rc || !n_rows) return rc;
     dim3 grid;
-    if (!rotary_grid(a, (long)(n_heads + n_kv_heads) * (w ? head_dim / 8 : head_dim), grid)) TREE_FAIL(SJD_EINVAL, "too many rows for one launch");
+    if (!rotary_grid(a, 8, (long)(n_heads + n_kv_heads) * (w ? head_dim / 8 : head_dim), grid)) TREE_FAIL(SJD_EINVAL, "too many rows for one launch");
     hipStream_t st = (hipStream_t)hip_stream;
     if (dtype == SJD_F32) w ? rotary_kernel<float, true><<<grid, 256, 0, st>>>(a) : rotary_kernel<float, false><<<grid, 256, 0, st>>>(a);
     else w ? rotary_kernel<bf16_t, true><<<grid, 256, 0, st>>>(a) : rotary_kernel<bf16_t, false><<<grid, 256, 0, st>>>(a);
