@@ -16,6 +16,7 @@ constexpr int kTopMax = 64;                        // likeliest ids at most: a l
 constexpr int kLogprobStep = 1024;                 // elements a wavefront takes at a time
 constexpr int kLogprobBuffer = kLogprobStep + kTopMax;
 constexpr int kLogprobWaves = 4;
+constexpr int kLogprobSift = 256;                  // so many are collected before they are sifted, which makes what follows rarer
 
 struct LogprobArgs {
     const void *z;             // [n_rows][vocab], rows a stride apart
@@ -75,28 +76,66 @@ SJD_D float logprob_lane_threshold(float x, int n) {
     return fmaxf(logprob_unorder(t), kLowest);
 }
 
-// Keeps the n largest of `count` keys, in the order in which they are.  A wavefront's own buffer.
-SJD_D int logprob_select(uint64_t *keys, int count, int n, int lane) {
-    if (count <= n) return count;
-    uint64_t t = 0;
+// Keeps the n largest of `count` keys, in the order in which they are, and says the least of them.  A wavefront's own buffer; the keys are distinct.  get(i): key i, 0 behind the last;
+// GROUPS of 64 of them are looked at (0: as many as there are).
+template <int GROUPS, typename Get> SJD_D int logprob_sift(uint64_t *keys, int count, int n, int lane, Get get, uint64_t &least) {
+    const int groups = GROUPS ? GROUPS : (count + 63) >> 6;
+    auto reach = [&](auto good) {       // how many keys are good
+        int c = 0;
+        if constexpr (GROUPS > 0) {
+#pragma unroll
+            for (int i = 0; i < GROUPS; ++i) c += __popcll(__ballot(good(get(i))));
+        } else {
 #pragma unroll 1
-    for (int bit = 63; bit >= 0; --bit) {
-        const uint64_t u = t | 1ull << bit;
-        int reach = 0;
+            for (int i = 0; i < groups; ++i) c += __popcll(__ballot(good(get(i))));
+        }
+        return c;
+    };
+    uint32_t hi = 0u, lo = 0u;
+    bool exact = false;
 #pragma unroll 1
-        for (int i = 0; i < count; i += 64) reach += __popcll(__ballot(i + lane < count && keys[i + lane] >= u));
-        if (reach >= n) t = u;
-        if (reach == n) break;
+    for (int bit = 31; bit >= 0 && !exact; --bit) {
+        const uint32_t u = hi | 1u << bit;
+        const int c = reach([&](uint64_t k) { return (uint32_t)(k >> 32) >= u; });
+        if (c >= n) hi = u;
+        exact = c == n;
     }
-    int kept = 0;
+    if (!exact) {                       // equal logits at the border: the lower ids, whose low halves are larger
+        const int need = n - reach([&](uint64_t k) { return (uint32_t)(k >> 32) > hi; });
 #pragma unroll 1
-    for (int i = 0; i < count; i += 64) {
-        const uint64_t key = i + lane < count ? keys[i + lane] : 0;
-        const uint64_t takes = __ballot(key >= t && key != 0);
-        if (key >= t && key != 0) keys[kept + __popcll(takes & ((1ull << lane) - 1))] = key;     // (at or before its place)
-        kept += __popcll(takes);
+        for (int bit = 31; bit >= 0 && !exact; --bit) {
+            const uint32_t u = lo | 1u << bit;
+            const int c = reach([&](uint64_t k) { return (uint32_t)(k >> 32) == hi && (uint32_t)k >= u; });
+            if (c >= need) lo = u;
+            exact = c == need;
+        }
+    }
+    least = (uint64_t)hi << 32 | lo;
+    int kept = 0;
+    auto keep = [&](uint64_t k) {
+        const bool takes = k >= least;
+        const uint64_t all = __ballot(takes);
+        if (takes) keys[kept + __popcll(all & ((1ull << lane) - 1))] = k;     // (at or before its place)
+        kept += __popcll(all);
+    };
+    if constexpr (GROUPS > 0) {
+#pragma unroll
+        for (int i = 0; i < GROUPS; ++i) keep(get(i));
+    } else {
+#pragma unroll 1
+        for (int i = 0; i < groups; ++i) keep(get(i));
     }
     return kept;
+}
+SJD_D int logprob_select(uint64_t *keys, int count, int n, int lane, uint64_t &least) {
+    constexpr int G = kLogprobSift / 64;
+    if (count <= kLogprobSift) {        // in registers
+        uint64_t k[G];
+#pragma unroll
+        for (int i = 0; i < G; ++i) k[i] = 64 * i + lane < count ? keys[64 * i + lane] : 0;
+        return logprob_sift<G>(keys, count, n, lane, [&](int i) { return k[i]; }, least);
+    }
+    return logprob_sift<0>(keys, count, n, lane, [&](int i) { return 64 * i + lane < count ? keys[64 * i + lane] : 0; }, least);
 }
 
 // A row's results from its sum and its `n` best keys; key(i): the i-th, 0 where there are fewer
@@ -117,6 +156,18 @@ template <typename Key> SJD_D void logprob_finish(const LogprobArgs &a, size_t r
     }
 }
 
+// The larger of two or three; one that is NaN is left out, or (a signaling one) makes it NaN.  (fmaxf would first make sure, element by element, that none is a signaling NaN.)
+SJD_D float logprob_max(float a, float b) {
+    float r;
+    asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+SJD_D float logprob_max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
 // One step: 16 elements of every lane.  id(e): of a lane's element e; `live`: bit e is set where there is one.  TOP: candidates are collected.
 // WHERE: all ids are before the token (-1), behind it (1), or anything (0).
 // The state of a lane: exponents are L (z - o) - c; of a wavefront: rank, keys collected, threshold, whether any o is not 0.
@@ -132,9 +183,9 @@ struct LogprobState {
 };
 template <bool TOP, int WHERE, typename Id>
 SJD_D void logprob_step(LogprobState &st, const float (&z)[16], Id id, uint32_t live, float z_token, int token, int n_top, uint64_t *keys, int lane) {
-    float top = z[0];
+    float top = logprob_max(z[0], z[1]);
 #pragma unroll
-    for (int e = 1; e < 16; ++e) top = fmaxf(top, z[e]);
+    for (int e = 2; e < 16; e += 2) top = logprob_max3(top, z[e], z[e + 1]);
     if (__ballot(top > st.m)) {
         const float m = fmaxf(st.m, top);
         const bool far = fabsf(m) >= kLogprobFar && m > -INFINITY;
@@ -158,7 +209,7 @@ SJD_D void logprob_step(LogprobState &st, const float (&z)[16], Id id, uint32_t 
     for (int e = 0; e < 16; ++e) {
         const float p = __builtin_amdgcn_exp2f(x[e]);
         st.s += p;
-        st.t = fmaf(p, fmaxf(x[e], -300.0f), st.t);       // (p of -inf is 0)
+        st.t = fmaf(p, logprob_max(x[e], -300.0f), st.t);       // (p of -inf is 0)
         if (WHERE < 0) st.rank += __popcll(__ballot(z[e] >= z_token));
         else if (WHERE > 0) st.rank += __popcll(__ballot(z[e] > z_token));
         else st.rank += __popcll(__ballot((live >> e & 1u) && (z[e] > z_token || (z[e] == z_token && id(e) < token))));
@@ -179,7 +230,16 @@ SJD_D void logprob_step(LogprobState &st, const float (&z)[16], Id id, uint32_t 
                 n = number();
             }
         }
-        if (st.count + n > kLogprobBuffer) st.count = logprob_select(keys, st.count, n_top, lane);
+        if (st.count + n > kLogprobSift && st.count > n_top) {
+            uint64_t worst;
+            st.count = logprob_select(keys, st.count, n_top, lane, worst);
+            // (n_top keys with lower ids reach it: what comes has to be larger.  This step's own threshold, if that is higher, takes equal ones)
+            const float above = logprob_above(logprob_key_z(worst));
+            if (above > st.least) {
+                st.least = above;
+                n = number();
+            }
+        }
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const uint64_t takes = __ballot(z[e] >= st.least);
@@ -201,13 +261,21 @@ __global__ __launch_bounds__(kLogprobWaves * 64) void logprob_kernel(LogprobArgs
     const size_t row = blockIdx.x / a.n_splits;
     const int split = blockIdx.x % a.n_splits, V = a.vocab;
     const T *z = (const T *)a.z + row * a.stride;
-    const int token = a.tokens[row];
-    const bool known = token >= 0 && token < V;
-    const float z_token = known ? to_float<T>(z[token]) : __builtin_nanf("");
     const int head = min((int)((16 - ((uintptr_t)z & 15)) & 15) / (int)sizeof(T), V), vecs = (V - head) / VE, tail = head + vecs * VE;
     const int parts = a.n_splits * kLogprobWaves, part = split * kLogprobWaves + wave;
     const int v0 = (int)((long)vecs * part / parts), v1 = (int)((long)vecs * (part + 1) / parts);
     uint64_t *keys = buffer[TOP ? wave : 0];
+    const u32x4 *p = reinterpret_cast<const u32x4 *>(z + head);
+    u32x4 next[VECS] = {};
+    auto fetch = [&](int v) {
+#pragma unroll
+        for (int i = 0; i < VECS; ++i)
+            if (v + 64 * i + lane < v1) next[i] = p[v + 64 * i + lane];
+    };
+    const int token = a.tokens[row];
+    fetch(v0);                          // (on its way beside the token's logit)
+    const bool known = token >= 0 && token < V;
+    const float z_token = known ? to_float<T>(z[token]) : __builtin_nanf("");
     LogprobState st = {-INFINITY, 0.0f, 0.0f, 0.0f, 0.0f, 0, 0, kLowest, false};
     auto single = [&](int first, int end) {                            // at most 15 elements
         float x[16];
@@ -218,14 +286,6 @@ __global__ __launch_bounds__(kLogprobWaves * 64) void logprob_kernel(LogprobArgs
         logprob_step<TOP, 0>(st, x, [&](int) { return first + lane; }, there ? 1u : 0u, z_token, token, a.n_top, keys, lane);
     };
     if (part == 0 && head) single(0, head);
-    const u32x4 *p = reinterpret_cast<const u32x4 *>(z + head);
-    u32x4 next[VECS] = {};
-    auto fetch = [&](int v) {
-#pragma unroll
-        for (int i = 0; i < VECS; ++i)
-            if (v + 64 * i + lane < v1) next[i] = p[v + 64 * i + lane];
-    };
-    fetch(v0);
     for (int v = v0; v < v1; v += 64 * VECS) {
         float x[16];
 #pragma unroll
@@ -261,7 +321,11 @@ __global__ __launch_bounds__(kLogprobWaves * 64) void logprob_kernel(LogprobArgs
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) r = logprob_join(r, LogprobSum{__shfl_xor(r.m, d, 64), __shfl_xor(r.s, d, 64), __shfl_xor(r.t, d, 64), 0});
     r.rank = st.rank;
-    if constexpr (TOP) st.count = logprob_select(keys, st.count, a.n_top, lane);
+    if constexpr (TOP)
+        if (st.count > 64) {            // a lane's key each
+            uint64_t worst;
+            st.count = logprob_select(keys, st.count, a.n_top, lane, worst);
+        }
     if (lane == 0) {
         sums[wave] = r;
         counts[wave] = st.count;
@@ -275,7 +339,9 @@ __global__ __launch_bounds__(kLogprobWaves * 64) void logprob_kernel(LogprobArgs
     int place = 0;
     if constexpr (TOP) {
         if (lane < st.count) mine = keys[lane];
+#pragma unroll
         for (int w = 0; w < kLogprobWaves; ++w)
+#pragma unroll 4
             for (int i = 0; i < counts[w]; ++i) place += buffer[w][i] > mine;
         __syncthreads();
         if (threadIdx.x < kTopMax) buffer[0][threadIdx.x] = 0;
@@ -297,25 +363,44 @@ constexpr int kLogprobJoin = 1024;
 template <typename T>
 __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a) {
     __shared__ uint64_t keys[kLogprobJoin], best[kTopMax];
+    __shared__ int some;
     const size_t row = blockIdx.x, bytes = logprob_part_bytes(a.n_top);
     const unsigned char *parts = a.parts + row * a.n_splits * bytes;
     const int tid = threadIdx.x, lane = tid & 63, n = a.n_splits * a.n_top;
+    uint64_t mine[kLogprobJoin / 256];
+#pragma unroll
+    for (int i = 0; i < kLogprobJoin / 256; ++i) {
+        const int u = tid + 256 * i;
+        mine[i] = u < n ? reinterpret_cast<const uint64_t *>(parts + u / a.n_top * bytes + 16)[u % a.n_top] : 0;
+    }
     const int token = a.tokens[row];
     const bool known = token >= 0 && token < a.vocab;
     const float z_token = known ? to_float<T>(((const T *)a.z)[row * a.stride + token]) : -INFINITY;
-    for (int i = tid; i < n; i += 256) keys[i] = reinterpret_cast<const uint64_t *>(parts + i / a.n_top * bytes + 16)[i % a.n_top];
-    if (tid < kTopMax) best[tid] = 0;
+    // A part's last key is reached by n_top of its own: only what reaches the largest of them can be among the best.
+    uint64_t least = 0;
+    if (a.n_top)
+        for (int i = lane; i < a.n_splits; i += 64) least = max(least, reinterpret_cast<const uint64_t *>(parts + i * bytes + 16)[a.n_top - 1]);
     LogprobSum r = {-INFINITY, 0.0f, 0.0f, 0};
     for (int i = lane; i < a.n_splits; i += 64) r = logprob_join(r, *reinterpret_cast<const LogprobSum *>(parts + i * bytes));
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) r = logprob_join(r, LogprobSum{__shfl_xor(r.m, d, 64), __shfl_xor(r.s, d, 64), __shfl_xor(r.t, d, 64), __shfl_xor(r.rank, d, 64)});
+    for (int d = 1; d < 64; d <<= 1) {
+        r = logprob_join(r, LogprobSum{__shfl_xor(r.m, d, 64), __shfl_xor(r.s, d, 64), __shfl_xor(r.t, d, 64), __shfl_xor(r.rank, d, 64)});
+        least = max(least, (uint64_t)__shfl_xor((unsigned long long)least, d, 64));
+    }
     if (!known) r.rank = -1;
+    if (tid < kTopMax) best[tid] = 0;
+    if (tid == 0) some = 0;
     __syncthreads();
-    for (int i = tid; i < n; i += 256) {
-        const uint64_t mine = keys[i];
+#pragma unroll
+    for (int i = 0; i < kLogprobJoin / 256; ++i)
+        if (mine[i] && mine[i] >= least) keys[atomicAdd(&some, 1)] = mine[i];       // (in any order: a key's place is the number of larger ones)
+    __syncthreads();
+    for (int i = tid; i < some; i += 256) {
+        const uint64_t key = keys[i];
         int place = 0;
-        for (int j = 0; j < n; ++j) place += keys[j] > mine;
-        if (mine && place < a.n_top) best[place] = mine;
+#pragma unroll 4
+        for (int j = 0; j < some; ++j) place += keys[j] > key;
+        if (place < a.n_top) best[place] = key;
     }
     __syncthreads();
     logprob_finish(a, row, r, z_token, [&](int i) { return best[i]; }, tid, 256);

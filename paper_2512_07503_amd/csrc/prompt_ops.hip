@@ -90,9 +90,9 @@ template <typename T> void run_prompt_type(hipStream_t st, int hd, const PromptA
 }
 
 // ------------------------------------------------------------------------------------------------------ log probabilities
-// How many workgroups a row is split over: four for each CU, but none with less than one step a wavefront, and no more than one joining workgroup holds.
+// How many workgroups a row is split over: as many as the card holds at once, four a CU, but none with less than one step a wavefront, and no more than one joining workgroup holds.
 int logprob_splits(int n_rows, int vocab, int n_top) {
-    const int want = ceil_div(1024, n_rows > 0 ? n_rows : 1), most = vocab / (kLogprobWaves * kLogprobStep), held = n_top ? kLogprobJoin / n_top : 64;
+    const int want = 1024 / (n_rows > 0 ? n_rows : 1), most = vocab / (kLogprobWaves * kLogprobStep), held = n_top ? kLogprobJoin / n_top : 64;
     int n = want < most ? want : most;
     if (n > held) n = held;
     if (n > 64) n = 64;
