@@ -1,8 +1,8 @@
 // Log probabilities of given tokens, with the token's rank, the row's entropy and its likeliest ids, in one pass over the logits.
 //
-// Of a row z with maximum m:  s = sum 2^(L (z - m)), t = sum 2^(L (z - m)) L (z - m), L = log2 e:
+// Of a row z with a reference m near its maximum:  s = sum 2^(L (z - m)), t = sum 2^(L (z - m)) L (z - m), L = log2 e:
 //   log p = z_token - m - ln s,   entropy = ln s - ln 2 t / s.
-// Lanes have a maximum of their own, and join at the end.  Until then exponents are L z - c, one instruction, with c = L m rounded once: the same factor 2^(L m - c) in
+// Lanes have a reference of their own, and join at the end.  Until then exponents are L z - c, one instruction, with c = L m rounded once: the same factor 2^(L m - c) in
 // every term of a lane, which its end takes off again.  From magnitudes of 2^22 on, where that factor is anything, they are L (z - m).
 //
 // The n likeliest ids: a wavefront goes through its part of the row in the order of the ids, 64 lanes x 16 elements at a time, and collects, in LDS, what may still be
@@ -11,6 +11,7 @@
 #pragma once
 #include "common.hip.h"
 #include "kernels_cache.hip.h"
+#include "lanes.hip.h"
 
 constexpr int kTopMax = 64;                        // likeliest ids at most: a lane's each
 constexpr int kLogprobStep = 1024;                 // elements a wavefront takes at a time
@@ -46,20 +47,28 @@ SJD_D float logprob_above(float x) { return logprob_unorder(logprob_order(x) + 1
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 constexpr float kLowest = -3.402823466e38f;
-constexpr float kLogprobFar = 0x1p22f;
+constexpr float kLogprobFar = 0x1p22f, kLogprobSlack = 8.0f;
 
-// a joined by b, either about its own maximum
-SJD_D LogprobSum logprob_join(const LogprobSum &a, const LogprobSum &b) {
-    LogprobSum r;
-    r.m = fmaxf(a.m, b.m);
-    r.rank = a.rank + b.rank;
-    const float da = (a.m - r.m) * kLog2e, db = (b.m - r.m) * kLog2e, fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
-    r.s = 0.0f;
-    r.t = 0.0f;
-    // (an empty part has s = 0 and a maximum of -inf; NaN is passed on)
-    if (a.s != 0.0f) { r.s = a.s * fa; r.t = fa == 0.0f ? 0.0f : fmaf(a.s, da, a.t) * fa; }
-    if (b.s != 0.0f) { r.s = fmaf(b.s, fb, r.s); r.t = fb == 0.0f ? r.t : fmaf(fmaf(b.s, db, b.t), fb, r.t); }
-    return r;
+// The same about another reference, that is not below
+SJD_D void logprob_move(LogprobSum &a, float m) {
+    const float d = (a.m - m) * kLog2e, f = __builtin_amdgcn_exp2f(d);
+    // (an empty part has s = 0 and a reference of -inf; NaN stays)
+    a.t = a.s == 0.0f || f == 0.0f ? 0.0f : fmaf(a.s, d, a.t) * f;
+    a.s = a.s == 0.0f ? 0.0f : a.s * f;
+    a.m = m;
+}
+SJD_D LogprobSum logprob_join(LogprobSum a, LogprobSum b) {
+    const float m = fmaxf(a.m, b.m);
+    logprob_move(a, m);
+    logprob_move(b, m);
+    return LogprobSum{m, a.s + b.s, a.t + b.t, a.rank + b.rank};
+}
+// of all lanes; the ranks are left as they are
+SJD_D LogprobSum logprob_join_lanes(LogprobSum a) {
+    logprob_move(a, lanes_max<64>(a.m));
+    a.s = lanes_sum<64>(a.s);
+    a.t = lanes_sum<64>(a.t);
+    return a;
 }
 
 // n-th largest of the lanes' x: the largest float that n lanes reach; kLowest if fewer than n are above -inf
@@ -186,8 +195,9 @@ SJD_D void logprob_step(LogprobState &st, const float (&z)[16], Id id, uint32_t 
     float top = logprob_max(z[0], z[1]);
 #pragma unroll
     for (int e = 2; e < 16; e += 2) top = logprob_max3(top, z[e], z[e + 1]);
-    if (__ballot(top > st.m)) {
-        const float m = fmaxf(st.m, top);
+    // The reference is the largest logit of a lane, but for 8: it moves where it is exceeded by more (exponentials of up to 2^11.6 cost the sums nothing).
+    if (__ballot(top > st.m + kLogprobSlack)) {
+        const float m = top > st.m + kLogprobSlack ? top : st.m;
         const bool far = fabsf(m) >= kLogprobFar && m > -INFINITY;
         const float o = far ? m : 0.0f, c = far || m == -INFINITY ? 0.0f : m * kLog2e;
         const float d = fmaf(st.o - o, kLog2e, st.c - c), f = __builtin_amdgcn_exp2f(d);
@@ -317,9 +327,7 @@ __global__ __launch_bounds__(kLogprobWaves * 64) void logprob_kernel(LogprobArgs
     if (part == parts - 1 && tail < V) single(tail, V);
 
     // the wavefront's, then the workgroup's
-    LogprobSum r = st.sum();
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) r = logprob_join(r, LogprobSum{__shfl_xor(r.m, d, 64), __shfl_xor(r.s, d, 64), __shfl_xor(r.t, d, 64), 0});
+    LogprobSum r = logprob_join_lanes(st.sum());
     r.rank = st.rank;
     if constexpr (TOP)
         if (st.count > 64) {            // a lane's key each
@@ -382,9 +390,10 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a) {
         for (int i = lane; i < a.n_splits; i += 64) least = max(least, reinterpret_cast<const uint64_t *>(parts + i * bytes + 16)[a.n_top - 1]);
     LogprobSum r = {-INFINITY, 0.0f, 0.0f, 0};
     for (int i = lane; i < a.n_splits; i += 64) r = logprob_join(r, *reinterpret_cast<const LogprobSum *>(parts + i * bytes));
+    r = logprob_join_lanes(r);
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-        r = logprob_join(r, LogprobSum{__shfl_xor(r.m, d, 64), __shfl_xor(r.s, d, 64), __shfl_xor(r.t, d, 64), __shfl_xor(r.rank, d, 64)});
+        r.rank += __shfl_xor(r.rank, d, 64);
         least = max(least, (uint64_t)__shfl_xor((unsigned long long)least, d, 64));
     }
     if (!known) r.rank = -1;

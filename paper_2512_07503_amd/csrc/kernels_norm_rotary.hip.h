@@ -3,6 +3,7 @@
 // A head is held in the registers of a team of lanes, 16 elements each, from the load to the store: read once, written once, rounded once.
 #pragma once
 #include "kernels_rotary.hip.h"
+#include "lanes.hip.h"
 
 struct NormRotaryArgs {
     RotaryArgs r;
@@ -10,25 +11,6 @@ struct NormRotaryArgs {
     int per_head;                    // gains and biases are [heads][hd], else [hd]
     float eps;
 };
-
-// Sum over a team of lanes (1, 2, .. 64, aligned), in every one of them.  Within 16 lanes by moves that are part of an addition: neighbours, pairs, then mirror images of 8 and of
-// 16 lanes, whose halves hold one number each by then.
-template <int CTRL> SJD_D float norm_moved(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xF, 0xF, true)); }
-template <int TEAM> SJD_D float norm_sum(float x) {
-    if constexpr (TEAM > 1) x += norm_moved<0xB1>(x);        // lanes 1 0 3 2
-    if constexpr (TEAM > 2) x += norm_moved<0x4E>(x);        // 2 3 0 1
-    if constexpr (TEAM > 4) x += norm_moved<0x141>(x);       // 7 6 .. 0
-    if constexpr (TEAM > 8) x += norm_moved<0x140>(x);       // 15 14 .. 0
-    if constexpr (TEAM > 16) {
-        const auto y = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(int, x), __builtin_bit_cast(int, x), false, false);
-        x = __builtin_bit_cast(float, (int)y[0]) + __builtin_bit_cast(float, (int)y[1]);
-    }
-    if constexpr (TEAM > 32) {
-        const auto y = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(int, x), __builtin_bit_cast(int, x), false, false);
-        x = __builtin_bit_cast(float, (int)y[0]) + __builtin_bit_cast(float, (int)y[1]);
-    }
-    return x;
-}
 
 // The normalised x in its place: z = (x - c) / sqrt(mean((x - c)^2) + eps), of a lane's elements (0 where it has none: bit e of `has`; FULL: it has all).
 // With means: c rounded is 2^-24 of it off, which may be many times the deviation, so what it leaves, the mean of the differences from it, is taken off as well.
@@ -40,7 +22,7 @@ template <int N, int TEAM, bool LAYER, bool FULL> SJD_D float norm_moments(float
         float t[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int e = 0; e < N; ++e) t[e & 1] += x[e];
-        float c = norm_sum<TEAM>(t[0] + t[1]) * inv;
+        float c = lanes_sum<TEAM>(t[0] + t[1]) * inv;
         asm volatile("" : "+v"(c));      // (the rounded one in all differences: fused with one of them the product would not be)
 #pragma unroll
         for (int e = 0; e < N; ++e) {
@@ -50,9 +32,9 @@ template <int N, int TEAM, bool LAYER, bool FULL> SJD_D float norm_moments(float
     }
 #pragma unroll
     for (int e = 0; e < N; ++e) second[e & 1] = fmaf(x[e], x[e], second[e & 1]);
-    const float var = norm_sum<TEAM>(second[0] + second[1]) * inv;
+    const float var = lanes_sum<TEAM>(second[0] + second[1]) * inv;
     if constexpr (!LAYER) return var;
-    off = norm_sum<TEAM>(first[0] + first[1]) * inv;
+    off = lanes_sum<TEAM>(first[0] + first[1]) * inv;
     const float less = var - off * off;
     return less < 0.0f ? 0.0f : less;
 }
