@@ -298,3 +298,16 @@ def test_refusals():
     whole = torch.zeros((31, 8, 64), dtype=torch.bfloat16, device="cuda")
     with pytest.raises(sjd.SjdError):
         sjd.op_prompt_attention(whole[:30, :4], k, v, s, out=whole[1:, :4])
+
+
+@pytest.mark.parametrize("dtype,stride", [("bf16", 40_000_000), ("f32", 36_000_000)])
+def test_rows_far_apart(dtype, stride):
+    """Rows of a block of keys more than 2^32 bytes from its first one."""
+    import torch
+
+    def far(c):
+        x = torch.empty((len(c.k) * stride,), dtype=c.k.dtype, device="cuda").view(len(c.k), stride)
+        x[:, :64], x[:, 64:128] = c.k[:, 0], c.v[:, 0]
+        c.k, c.v = x[:, :64].unflatten(1, (1, 64)), x[:, 64:128].unflatten(1, (1, 64))
+    c = Case(dtype, 2, 1, 64, [3, 20], [66, 4], seed=21, edit=far)
+    c.check(c.run())
