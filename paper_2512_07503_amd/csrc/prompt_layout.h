@@ -11,9 +11,11 @@ constexpr int prompt_offset(int n, int n_keys) { return n_keys - n; }
 
 // tiles of n rows
 constexpr int prompt_tiles(int n, int G, int tile) { return (int)(((long)n * G + tile - 1) / tile); }
-// and an upper bound over n_rows rows of n_seqs sequences
+// Where the tiles of sequence b begin whose rows begin at `first`, if every sequence has its place whatever those before it have: places ascend, and those behind a sequence's tiles are empty.
+constexpr int prompt_first_tile(int first, int b, int G, int tile) { return (int)((long)first * G / tile) + b; }
+// An upper bound of the tiles, and of these places, over n_rows rows of n_seqs sequences
 constexpr long prompt_max_tiles(long n_rows, long n_seqs, int G, int tile) {
-    return n_rows * G / tile + (n_seqs < n_rows ? n_seqs : n_rows);
+    return n_rows * G / tile + (n_seqs < n_rows || n_seqs > 64 ? n_seqs : n_rows);
 }
 // keys that some row of tile t of a sequence sees: 0 .. prompt_keys - 1
 constexpr int prompt_keys(int t, int n, int n_keys, int G, int tile) {

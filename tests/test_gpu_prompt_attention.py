@@ -311,3 +311,16 @@ def test_rows_far_apart(dtype, stride):
         c.k, c.v = x[:, :64].unflatten(1, (1, 64)), x[:, 64:128].unflatten(1, (1, 64))
     c = Case(dtype, 2, 1, 64, [3, 20], [66, 4], seed=21, edit=far)
     c.check(c.run())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n_seqs,most", [(63, 80), (64, 300), (65, 300), (150, 150), (4100, 9)])
+def test_many_sequences(dtype, n_seqs, most):
+    rng = np.random.default_rng(22 + n_seqs)
+    n = (rng.integers(0, most, n_seqs) * (rng.random(n_seqs) < 0.7)).tolist()
+    c = Case(dtype, 6, 2, 32, n, seed=22, lead=70, trail=9)
+    c.check(c.run())
+    t = (np.asarray(n) + rng.integers(-3, 200 if n_seqs < 1000 else 4, n_seqs)).clip(0).tolist()
+    c = Case(dtype, 3, 3, 32, n, t, seed=23, lead=3, trail=200)
+    c.check(c.run())
+    c.check(c.run(max_kv=1000))

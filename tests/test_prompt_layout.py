@@ -15,11 +15,13 @@ int main() {
     // tiles: an upper bound over any cut of the rows; the keys that a tile's rows see
     for (int it = 0; it < 20000; ++it) {
         const int seqs = 1 + rand() % 9, G = 1 + rand() % 8, tile = 32 << rand() % 4;
-        long rows = 0, tiles = 0;
+        long rows = rand() % 3 ? 0 : rand() % 200, tiles = 0, place = 0;
         for (int b = 0; b < seqs; ++b) {
             const int n = rand() % 3 ? rand() % 300 : 0, keys = rand() % 400;
+            const int t = prompt_tiles(n, G, tile), at = prompt_first_tile((int)rows, b, G, tile);
+            CHECK(at >= place);
+            place = at + (t ? t : 1);
             rows += n;
-            const int t = prompt_tiles(n, G, tile);
             CHECK((long)t * tile >= (long)n * G && (n == 0 ? t == 0 : (long)(t - 1) * tile < (long)n * G));
             tiles += t;
             for (int i = 0; i < t; ++i) {
@@ -30,9 +32,9 @@ int main() {
                 CHECK(prompt_keys(i, n, keys, G, tile) == seen);
             }
         }
-        CHECK(tiles <= prompt_max_tiles(rows, seqs, G, tile));
+        CHECK(tiles <= prompt_max_tiles(rows, seqs, G, tile) && place <= rows * G / tile + seqs);
     }
-    CHECK(prompt_max_tiles(0, 5, 3, 128) == 0);
+    CHECK(prompt_max_tiles(0, 5, 3, 128) == 0 && prompt_max_tiles(1280, 65, 3, 128) == 95);
     // splits go through every block once, whatever was expected of the number of keys
     for (int it = 0; it < 200000; ++it) {
         const int keys = rand() % 3000, block = 32 << rand() % 3, n_splits = 1 + rand() % 9, per = 1 + rand() % 20, blocks = (keys + block - 1) / block;
