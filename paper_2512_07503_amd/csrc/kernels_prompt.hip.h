@@ -27,9 +27,12 @@ struct PromptArgs {
 };
 
 constexpr int kPromptWaves = 4;
-constexpr int prompt_waves_per_simd(int size, int hd) { return size * hd <= 256 ? 2 : 1; }
-// tokens of a block
-template <typename T> constexpr int kPromptBlock = sizeof(T) == 2 ? 64 : 32;
+// Waves that the compiler leaves registers for, of a SIMD: two overlap one's products with the other's exponentials (fp32, 8 192 rows of 16 heads of 128 in 4 groups over themselves: 67 against 52 TFLOP/s);
+// with heads of 192 and 256 in fp32 the queries and the output alone fill what one may have.
+constexpr int prompt_waves_per_simd(int size, int hd) { return size == 2 || hd <= 128 ? 2 : 1; }
+// Tokens of a block.  Of wide heads 32, which halves the scores, and with operands that are loaded as others are used up leaves room for a second wave or a third (bf16, as above, heads of 256: 1 120
+// against 435 TFLOP/s, 192: 1 104 against 811, 128: 999 against 979; heads of 64: 772 against 784).
+constexpr int prompt_block(int size, int hd) { return size == 2 && hd < 128 ? 64 : 32; }
 
 // A workgroup's tile: sequence (-1: there is none), tile of it, first row and number of rows, first key and number of keys
 struct PromptTile { int b, t, r0, n, k0, n_keys; };
@@ -146,7 +149,7 @@ SJD_D void prompt_to_lds(const char *base, uint32_t off, unsigned char *lds) {
 // Keys or values of a block on their way to LDS.  WIDE: rows are 16-byte aligned and go there without passing through registers.  Tokens behind the last are
 // copies of the last one: nobody sees them.
 template <typename T, int HD, bool WIDE> struct PromptFetch {
-    static constexpr int BLOCK = kPromptBlock<T>, ROW = HD * sizeof(T), PIECES = BLOCK * ROW / 16, THREADS = kPromptWaves * 64, PER = PIECES / THREADS;
+    static constexpr int BLOCK = prompt_block(sizeof(T), HD), ROW = HD * sizeof(T), PIECES = BLOCK * ROW / 16, THREADS = kPromptWaves * 64, PER = PIECES / THREADS;
     static_assert(PIECES % THREADS == 0, "a block divides among the threads");
     // Pieces of a lane whose tokens are a multiple of 16 apart have the same places in their rows
     static constexpr int TOKENS = THREADS * 16 / ROW, DIFFERENT = THREADS * 16 % ROW == 0 && TOKENS % 16 == 0 ? 1 : PER;
@@ -217,17 +220,19 @@ template <int HD> SJD_D f32x16 prompt_scores32(const unsigned char *k, const u32
 // transposing loads: 16 lanes fetch 16 dimensions of 4 keys, and each gets the 4 keys of one.
 template <int HD> struct PromptPlaces {
     static constexpr int ROW = HD * 2, AGAIN = ROW % 128 == 64 ? 64 : ROW % 256 == 128 ? 128 : 256, NK = AGAIN / 32, NV = AGAIN / 64;    // (places repeat after so many bytes)
-    int k[NK], v[2][NV];
+    // Places within these differ from the first by an exclusive or of what their pieces differ in: where registers are short only the first is kept.
+    static constexpr int KK = prompt_block(2, HD) == 32 ? 1 : NK, KV = prompt_block(2, HD) == 32 ? 1 : NV;
+    int k[KK], v[2][KV];
     SJD_D explicit PromptPlaces(int lane) {
 #pragma unroll
-        for (int n = 0; n < NK; ++n) {
+        for (int n = 0; n < KK; ++n) {
             k[n] = (lane & 31) * ROW + prompt_swizzle(lane & 31, 2 * n + (lane >> 5), ROW) * 16;
             asm volatile("" : "+v"(k[n]));       // (once: the compiler would keep them for each buffer)
         }
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
-            for (int db = 0; db < NV; ++db) {
+            for (int db = 0; db < KV; ++db) {
                 const int t = 8 * r + 4 * (lane >> 5) + ((lane >> 2) & 3), j = 32 * db + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
                 v[r][db] = t * ROW + prompt_swizzle(t, j >> 3, ROW) * 16 + (j & 4) * 2;
                 asm volatile("" : "+v"(v[r][db]));
@@ -235,21 +240,23 @@ template <int HD> struct PromptPlaces {
     }
     SJD_D void move(int bytes) {
 #pragma unroll
-        for (int n = 0; n < NK; ++n) k[n] += bytes;
+        for (int n = 0; n < KK; ++n) k[n] += bytes;
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
-            for (int db = 0; db < NV; ++db) v[r][db] += bytes;
+            for (int db = 0; db < KV; ++db) v[r][db] += bytes;
     }
     SJD_D u32x4 keys(const unsigned char *block, int half, int n) const {
-        return *reinterpret_cast<const u32x4 *>(block + k[n % NK] + n / NK * AGAIN + half * 32 * ROW);
+        const int at = KK == 1 ? k[0] ^ n % NK * 32 : k[n % NK];
+        return *reinterpret_cast<const u32x4 *>(block + at + n / NK * AGAIN + half * 32 * ROW);
     }
     SJD_D u32x4 values(const unsigned char *block, int i, int db) const {
         typedef __attribute__((address_space(3))) prompt_s16x4 lds4;
         u32x4 x;
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(block + v[r][db % NV] + db / NV * AGAIN + 16 * i * ROW)));
+            const int at = KV == 1 ? v[r][0] ^ db % NV * 64 : v[r][db % NV];
+            const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(block + at + db / NV * AGAIN + 16 * i * ROW)));
             x[2 * r] = y.x;
             x[2 * r + 1] = y.y;
         }
@@ -397,35 +404,40 @@ template <int N, int M, typename A, typename B> SJD_D void prompt_spread(A produ
     }
 }
 
-// A wavefront of the bf16 kernel: 32 rows, a block of 64 keys at a time, in halves.
+// A wavefront of the bf16 kernel: 32 rows, a block of keys at a time, 32 (HALVES: 1) or 64 (2).
 template <int HD> struct PromptWave16 {
-    static constexpr int NQ = HD / 16, DB = HD / 32, BLOCK = kPromptBlock<bf16_t>;
+    static constexpr int NQ = HD / 16, DB = HD / 32, HALVES = prompt_block(2, HD) / 32, NK = HALVES * NQ, NV = HALVES * 2 * DB;
+    // Operands of keys and values that are loaded before their products begin, and those held: the others replace those that have been used
+    static constexpr int AHEAD = HALVES == 2 ? NQ : 4, HELD = 2 * AHEAD;
+    static_assert(NQ == 2 * DB && NK % AHEAD == 0, "as many for keys as for values");
     PromptState<HD> st;
-    u32x4 q[NQ], k[2][NQ], v[2][2 * DB], p[2][2];     // operands: queries, keys, values, probabilities
-    f32x16 s[2];
+    u32x4 q[NQ], k[HELD], v[HELD], p[HALVES][2];      // operands: queries, keys, values, probabilities
+    f32x16 s[HALVES];
     float m, sum, e0, e1;
     bool wild = false;                                // values of blocks that were masked were infinite or NaN
     PromptPlaces<HD> at;
     SJD_D explicit PromptWave16(int lane) : at(lane) { st.clear(); m = 0.0f; }
-    SJD_D void load_k(const unsigned char *block, int half, int n) { k[half][n] = at.keys(block, half, n); }
-    SJD_D void load_v(const unsigned char *block, int half, int n) { v[half][n] = at.values(block, 2 * half + n / DB, n % DB); }
-    template <int I> SJD_D void score(int n) {
-        if (n == 0)
+    SJD_D void load_k(const unsigned char *block, int n) { k[n % HELD] = at.keys(block, n / NQ, n % NQ); }
+    SJD_D void load_v(const unsigned char *block, int n) { v[n % HELD] = at.values(block, n / DB, n % DB); }
+    SJD_D void score(int n) {
+        if (n % NQ == 0)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[I][e] = 0.0f;
-        s[I] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k[I][n]), __builtin_bit_cast(bf16x8, q[n]), s[I], 0, 0, 0);
+            for (int e = 0; e < 16; ++e) s[n / NQ][e] = 0.0f;
+        s[n / NQ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k[n % HELD]), __builtin_bit_cast(bf16x8, q[n % NQ]), s[n / NQ], 0, 0, 0);
     }
-    // last: of the unit's keys, the last one that the lane's row sees
-    template <int I> SJD_D void mask(int last) {
+    // last: of the block's keys, the last one that the lane's row sees
+    SJD_D void mask(int last) {
         const int mine = last - 4 * (int)((threadIdx.x >> 5) & 1);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[I][e] = 8 * (e >> 2) + (e & 3) <= mine ? s[I][e] : -INFINITY;
+        for (int i = 0; i < HALVES; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[i][e] = 32 * i + 8 * (e >> 2) + (e & 3) <= mine ? s[i][e] : -INFINITY;
     }
-    // Probabilities are 2^(score - m).  As long as a lane's of a unit add up to at most 1 none is above 1, and m stays; else, and at first, it is put ahead of the largest score.
+    // Probabilities are 2^(score - m).  As long as a lane's of a block add up to at most 1 none is above 1, and m stays; else, and at first, it is put ahead of the largest score.
     SJD_D void settle(float scale_log2e) {
         float mx = s[0][0];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < HALVES; ++i)
 #pragma unroll
             for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[i][e]);
         prompt_rescale<HD>(st, prompt_both_halves(mx) * scale_log2e);
@@ -444,26 +456,34 @@ template <int HD> struct PromptWave16 {
             e1 = __builtin_amdgcn_exp2f(fmaf(s[I][2 * n + 1], scale_log2e, -m));
         }
     }
-    template <int I> SJD_D void product(int n) {       // n-th of 2 DB
-        st.o[n % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[I][n]), __builtin_bit_cast(bf16x8, p[I][n / DB]), st.o[n % DB], 0, 0, 0);
-    }
-    // Are there values that are infinite or NaN (0 times them is NaN)?  They become 0.
-    template <int I> SJD_D bool tame() {
-        float x = 0.0f;
+    SJD_D void weigh_all(float scale_log2e) {
+        sum = 0.0f;
 #pragma unroll
-        for (int n = 0; n < 2 * DB; ++n)
+        for (int n = 0; n < 9; ++n) weigh<0>(n, scale_log2e);
+        if constexpr (HALVES == 2)
+#pragma unroll
+            for (int n = 0; n < 9; ++n) weigh<1>(n, scale_log2e);
+    }
+    SJD_D void product(int n) {
+        st.o[n % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[n % HELD]), __builtin_bit_cast(bf16x8, p[n / (2 * DB)][n / DB % 2]), st.o[n % DB], 0, 0, 0);
+    }
+    // Are there values in N operands that are infinite or NaN (0 times them is NaN)?  They become 0.
+    template <int N> static SJD_D bool tame(u32x4 *x) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int n = 0; n < N; ++n)
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
-                const uint32_t w = v[I][n][d];
-                x = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(cache_bf16x2, w), __builtin_bit_cast(cache_bf16x2, 0u), x, false);
+                const uint32_t w = x[n][d];
+                sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(cache_bf16x2, w), __builtin_bit_cast(cache_bf16x2, 0u), sum, false);
             }
-        const bool found = __ballot(x != 0.0f);
+        const bool found = __ballot(sum != 0.0f);
         if (found) {
             bool any = false;
 #pragma unroll
-            for (int n = 0; n < 2 * DB; ++n)
+            for (int n = 0; n < N; ++n)
 #pragma unroll
-                for (int d = 0; d < 4; ++d) v[I][n][d] = prompt_tame2(v[I][n][d], any);
+                for (int d = 0; d < 4; ++d) x[n][d] = prompt_tame2(x[n][d], any);
         }
         return found;
     }
@@ -471,36 +491,27 @@ template <int HD> struct PromptWave16 {
     SJD_D void block(const unsigned char *keys, const unsigned char *values, int last, bool masked, bool first, float scale_log2e) {
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) load_k(keys, 0, n);
+        for (int n = 0; n < AHEAD; ++n) load_k(keys, n);
         __builtin_amdgcn_s_setprio(1);
-        prompt_spread<NQ, NQ>([&](int n) { score<0>(n); }, [&](int n) { load_k(keys, 1, n); });
-        prompt_spread<NQ, 0>([&](int n) { score<1>(n); }, [&](int) {});
+        prompt_spread<NK - AHEAD, NK - AHEAD>([&](int n) { score(n); }, [&](int n) { load_k(keys, n + AHEAD); });
+        prompt_spread<AHEAD, 0>([&](int n) { score(NK - AHEAD + n); }, [&](int) {});
         __builtin_amdgcn_s_setprio(0);
-        if (masked) {
-            mask<0>(last);
-            mask<1>(last - 32);
-        }
-        sum = 0.0f;
-#pragma unroll
-        for (int n = 0; n < 9; ++n) weigh<0>(n, scale_log2e);
-#pragma unroll
-        for (int n = 0; n < 9; ++n) weigh<1>(n, scale_log2e);
+        if (masked) mask(last);
+        weigh_all(scale_log2e);
         if (__ballot(first || !(sum <= 1.0f))) {
             settle(scale_log2e);
-            sum = 0.0f;
-#pragma unroll
-            for (int n = 0; n < 9; ++n) weigh<0>(n, scale_log2e);
-#pragma unroll
-            for (int n = 0; n < 9; ++n) weigh<1>(n, scale_log2e);
+            weigh_all(scale_log2e);
         }
         st.l += sum;
 #pragma unroll
-        for (int n = 0; n < 2 * DB; ++n) load_v(values, 0, n);
-        if (masked) wild |= tame<0>();
-        __builtin_amdgcn_s_setprio(1);
-        prompt_spread<2 * DB, 2 * DB>([&](int n) { product<0>(n); }, [&](int n) { load_v(values, 1, n); });
-        if (masked) wild |= tame<1>();
-        prompt_spread<2 * DB, 0>([&](int n) { product<1>(n); }, [&](int) {});
+        for (int n = 0; n < AHEAD; ++n) load_v(values, n);
+#pragma unroll
+        for (int n = 0; n < NV; n += AHEAD) {           // (those of a masked block are looked at while the next ones are not yet there)
+            if (masked) wild |= tame<AHEAD>(v + n % HELD);
+            __builtin_amdgcn_s_setprio(1);
+            if (n + AHEAD < NV) prompt_spread<AHEAD, AHEAD>([&](int i) { product(n + i); }, [&](int i) { load_v(values, n + i + AHEAD); });
+            else prompt_spread<AHEAD, 0>([&](int i) { product(n + i); }, [&](int) {});
+        }
         __builtin_amdgcn_s_setprio(0);
     }
 };
@@ -508,7 +519,7 @@ template <int HD> struct PromptWave16 {
 // Workgroup = four wavefronts of 32 rows each, of a split.
 template <int HD, bool WIDE>
 __global__ __launch_bounds__(kPromptWaves * 64, prompt_waves_per_simd(2, HD)) void prompt_attention16_kernel(PromptArgs a) {
-    constexpr int BLOCK = kPromptBlock<bf16_t>, BYTES = BLOCK * HD * 2, ROWS = kPromptWaves * 32;
+    constexpr int BLOCK = prompt_block(2, HD), BYTES = BLOCK * HD * 2, ROWS = kPromptWaves * 32;
     __shared__ __attribute__((aligned(16))) unsigned char lds[4 * BYTES];      // keys and values of a block, and of the next one
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int kvh = blockIdx.x % a.n_kv, tile = blockIdx.x / a.n_kv % a.tiles, split = blockIdx.x / a.n_kv / a.tiles;
@@ -556,7 +567,7 @@ __global__ __launch_bounds__(kPromptWaves * 64, prompt_waves_per_simd(2, HD)) vo
 // fp32, the same without an order of its own.
 template <int HD, bool WIDE>
 __global__ __launch_bounds__(kPromptWaves * 64, prompt_waves_per_simd(4, HD)) void prompt_attention32_kernel(PromptArgs a) {
-    constexpr int BLOCK = kPromptBlock<float>, BYTES = BLOCK * HD * 4, ROWS = kPromptWaves * 32;
+    constexpr int BLOCK = prompt_block(4, HD), BYTES = BLOCK * HD * 4, ROWS = kPromptWaves * 32;
     __shared__ __attribute__((aligned(16))) unsigned char lds[2][2][BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int kvh = blockIdx.x % a.n_kv, tile = blockIdx.x / a.n_kv % a.tiles, split = blockIdx.x / a.n_kv / a.tiles;
@@ -597,7 +608,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
     const int part = blockIdx.x % WGS, kvh = blockIdx.x / WGS % a.n_kv, tile = blockIdx.x / WGS / a.n_kv;
     const PromptTile s = prompt_find_tile(a, ROWS, tile);
     if (s.b < 0) return;
-    const int splits = prompt_splits(prompt_keys(s.t, s.n, s.n_keys, a.G, ROWS), kPromptBlock<T>, a.n_splits, a.per_split);
+    const int splits = prompt_splits(prompt_keys(s.t, s.n, s.n_keys, a.G, ROWS), prompt_block(sizeof(T), HD), a.n_splits, a.per_split);
     const int u = part * 256 + threadIdx.x, row = u & 31, j = (u >> 5) % (HD / 4) * 4, sub = (u >> 5) / (HD / 4);
     const int rho = s.t * ROWS + sub * 32 + row, node = rho / a.G;
     if (splits == 1 || node >= s.n) return;

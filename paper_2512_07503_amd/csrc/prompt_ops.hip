@@ -37,7 +37,7 @@ struct PromptPlan { int tiles, n_splits, per_split; size_t part_o, part_ml; };
 // 461, 456, 432, 434, 438 us).
 PromptPlan prompt_plan(int dtype, int n_rows, int n_seqs, int n_heads, int n_kv, int hd, int max_kv) {
     PromptPlan p;
-    const int G = n_heads / n_kv, rows = kPromptWaves * 32, block = dtype == SJD_F32 ? kPromptBlock<float> : kPromptBlock<bf16_t>;
+    const int G = n_heads / n_kv, rows = kPromptWaves * 32, block = prompt_block(dtype == SJD_F32 ? 4 : 2, hd);
     p.tiles = (int)prompt_max_tiles(n_rows, n_seqs, G, rows);
     const size_t work = (size_t)p.tiles * n_kv, blocks = ceil_div_sz((size_t)max_kv, block);
     const size_t want = work >= 512 ? 1 : ceil_div_sz(1536, work ? work : 1), most = blocks / 4 ? blocks / 4 : 1;
