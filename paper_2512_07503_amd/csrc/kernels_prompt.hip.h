@@ -23,7 +23,7 @@ struct PromptArgs {
     float scale_log2e;
     float *part_o;             // [tile][kv head][split][32-row tile][32 * hd]   unnormalised, order of prompt_part_index
     float *part_ml;            // [tile][kv head][split][32-row tile][2][32]     reference (base 2), sum
-    bool q_wide, out_wide;     // rows 16-byte (out: 4 elements) aligned
+    bool q_wide, out_wide;     // rows 16-byte aligned
 };
 
 constexpr int kPromptWaves = 4;
@@ -365,29 +365,54 @@ SJD_D bool prompt_block32(PromptState<HD> &st, const unsigned char *k, const uns
     return __ballot(wild);
 }
 
-// What becomes of 32 rows (first: the first of them): results, or parts of them
+// What becomes of 32 rows (first: the first of them; node: the lane's row of the sequence): results, or parts of them
 template <typename T, int HD>
-SJD_D void prompt_finish(const PromptArgs &a, const PromptTile &s, const PromptState<HD> &st, int kvh, bool several, size_t slot, int first, int lane) {
-    const int rho = first + (lane & 31), node = rho / a.G;
+SJD_D void prompt_finish(const PromptArgs &a, const PromptTile &s, const PromptState<HD> &st, int kvh, bool several, size_t slot, int first, int node, int lane) {
     if (first >= (long)s.n * a.G) return;
     const float sum = st.l + __shfl_xor(st.l, 32, 64);
-    // (it is NaN, and so is the row, where a score is; it is 0 where the row saw nothing)
-    const float norm = several ? 1.0f : sum == 0.0f ? 0.0f : 1.0f / sum;
-    if (several && lane < 32) {
-        a.part_ml[slot * 64 + lane] = st.m;
-        a.part_ml[slot * 64 + 32 + lane] = sum;
+    if (several) {
+        if (lane < 32) {
+            a.part_ml[slot * 64 + lane] = st.m;
+            a.part_ml[slot * 64 + 32 + lane] = sum;
+        }
+        if (node >= s.n) return;
+        float *part = a.part_o + slot * 32 * HD + prompt_part_index(lane & 31, 4 * (lane >> 5));
+#pragma unroll
+        for (int db = 0; db < HD / 32; ++db)
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                *reinterpret_cast<f32x4 *>(part + prompt_part_index(0, db * 32 + 8 * u)) = f32x4{st.o[db][4 * u], st.o[db][4 * u + 1], st.o[db][4 * u + 2], st.o[db][4 * u + 3]};
+        return;
     }
-    if (node >= s.n) return;
+    // (it is NaN, and so is the row, where a score is; it is 0 where the row saw nothing, and so is the output)
+    const float norm = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const size_t row = (size_t)s.r0 + node;
+    const int h = kvh * a.G + first + (lane & 31) - node * a.G;
+    if (sizeof(T) == 4 || !a.out_wide) {
+        if (node >= s.n) return;
+#pragma unroll
+        for (int db = 0; db < HD / 32; ++db)
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                prompt_store<T>(a, row, h, HD, db * 32 + 8 * u + 4 * (lane >> 5), f32x4{st.o[db][4 * u], st.o[db][4 * u + 1], st.o[db][4 * u + 2], st.o[db][4 * u + 3]} * norm);
+        return;
+    }
+    // a lane holds 4 of 8 dimensions, and stores all 8 of one half of them
+    const bool live = node < s.n;
+    bf16_t *out = (bf16_t *)a.out + (live ? row * a.out_stride + (size_t)h * HD : 0) + 8 * (lane >> 5);
 #pragma unroll
     for (int db = 0; db < HD / 32; ++db)
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int j = db * 32 + 8 * u + 4 * (lane >> 5);
-            f32x4 t;
+        for (int u = 0; u < 4; u += 2) {
+            u32x4 x;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) t[e] = norm == 0.0f ? 0.0f : st.o[db][4 * u + e] * norm;
-            if (several) *reinterpret_cast<f32x4 *>(a.part_o + slot * 32 * HD + prompt_part_index(lane & 31, j)) = t;
-            else prompt_store<T>(a, (size_t)s.r0 + node, kvh * a.G + rho - node * a.G, HD, j, t);
+            for (int e = 0; e < 2; ++e) {
+                const auto y = __builtin_amdgcn_permlane32_swap(pack_bf16(st.o[db][4 * u + 2 * e] * norm, st.o[db][4 * u + 2 * e + 1] * norm),
+                                                                pack_bf16(st.o[db][4 * u + 4 + 2 * e] * norm, st.o[db][4 * u + 4 + 2 * e + 1] * norm), false, false);
+                x[e] = y[0];
+                x[2 + e] = y[1];
+            }
+            if (live) *reinterpret_cast<u32x4 *>(out + db * 32 + 8 * u) = x;
         }
 }
 
@@ -561,7 +586,7 @@ __global__ __launch_bounds__(kPromptWaves * 64, prompt_waves_per_simd(2, HD)) vo
     // what is left the other wavefronts see: this one helps to fetch (in a loop of its own: with a branch around the block above the output would be copied every time)
     for (; blk < range.last; ++blk) turn();
     if (w.wild) prompt_add_wild<bf16_t, HD>(w.st, v, a.v_stride, max(range.first, (low + 1) / BLOCK) * BLOCK, min(mine * BLOCK, s.n_keys), sees, lane);
-    prompt_finish<bf16_t, HD>(a, s, w.st, kvh, range.several, prompt_slot(a, tile, kvh, split) * (ROWS / 32) + wave, row0, lane);
+    prompt_finish<bf16_t, HD>(a, s, w.st, kvh, range.several, prompt_slot(a, tile, kvh, split) * (ROWS / 32) + wave, row0, node, lane);
 }
 
 // fp32, the same without an order of its own.
@@ -597,7 +622,7 @@ __global__ __launch_bounds__(kPromptWaves * 64, prompt_waves_per_simd(4, HD)) vo
         if (blk < mine) wild |= prompt_block32<HD>(st, lds[buf][0], lds[buf][1], q, sees - t0, t0 + BLOCK - 1 > low, a.scale_log2e, lane);
     }
     if (wild) prompt_add_wild<float, HD>(st, v, a.v_stride, max(range.first, (low + 1) / BLOCK) * BLOCK, min(mine * BLOCK, s.n_keys), sees, lane);
-    prompt_finish<float, HD>(a, s, st, kvh, range.several, prompt_slot(a, tile, kvh, split) * (ROWS / 32) + wave, row0, lane);
+    prompt_finish<float, HD>(a, s, st, kvh, range.several, prompt_slot(a, tile, kvh, split) * (ROWS / 32) + wave, row0, node, lane);
 }
 
 // Joins the splits of every row that has several: out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  A thread owns four dimensions of a row; eight splits are on their way

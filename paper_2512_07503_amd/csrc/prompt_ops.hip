@@ -202,7 +202,7 @@ int sjd_op_prompt_attention(void *hip_stream, int32_t dtype, const void *q, int6
     a.part_o = (float *)workspace;
     a.part_ml = (float *)((char *)workspace + p.part_o);
     a.q_wide = wide(q, q_stride, size, 16);
-    a.out_wide = wide(out, out_stride, size, 4 * size);
+    a.out_wide = wide(out, out_stride, size, 16);
     // (their places within a block are 32-bit offsets)
     auto near = [&](long stride) { return n_kv_rows < 2 || stride < (1l << 31) / (64 * size); };
     const bool wide_kv = wide(k, k_stride, size, 16) && wide(v, v_stride, size, 16) && near(k_stride) && near(v_stride);
