@@ -197,24 +197,6 @@ SJD_D void prompt_barrier() {
     __syncthreads();
 }
 
-// S^T of 32 keys and 32 rows, fp32
-template <int HD> SJD_D f32x16 prompt_scores32(const unsigned char *k, const u32x4 (&q)[HD / 8], int lane) {
-    f32x16 s;
-#pragma unroll
-    for (int v = 0; v < 16; ++v) s[v] = 0.0f;
-    const int t = lane & 31;
-#pragma unroll
-    for (int n = 0; n < HD / 8; ++n) {
-        const u32x4 x = *reinterpret_cast<const u32x4 *>(k + t * HD * 4 + prompt_swizzle(t, 2 * n + (lane >> 5), HD * 4) * 16);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint32_t xe = x[e], qe = q[n][e];
-            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__builtin_bit_cast(float, xe), __builtin_bit_cast(float, qe), s, 0, 0, 0);
-        }
-    }
-    return s;
-}
-
 // Operands of the bf16 products in a block in LDS: places of a lane's 16 bytes of keys (rows of the operand = 32 keys, 16 dimensions at a time), and of the 8 bytes that it fetches for
 // values (rows = dimensions 32 db + lane % 32; of 16 keys 16 i, the element e is key 16 i + 8 (e / 4) + 4 (lane / 32) + e % 4, as the scores have them).  Those come from the rows by the
 // transposing loads: 16 lanes fetch 16 dimensions of 4 keys, and each gets the 4 keys of one.
@@ -263,12 +245,22 @@ template <int HD> struct PromptPlaces {
         return x;
     }
 };
-// fp32: a token, 8 (v / 4) + 4 (lane / 32) + v % 4
-template <int HD> SJD_D float prompt_value32(const unsigned char *l, int v, int db, int lane) {
-    constexpr int ROW = HD * 4;
-    const int t = 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3), j = 32 * db + (lane & 31);
-    return *reinterpret_cast<const float *>(l + t * ROW + prompt_swizzle(t, j >> 2, ROW) * 16 + (j & 3) * 4);
-}
+// The same for fp32: a lane's 16 bytes of keys, and its value of token 8 (e / 4) + 4 (lane / 32) + e % 4.  All places differ from the first by an exclusive or and an offset.
+template <int HD> struct PromptPlaces32 {
+    static constexpr int ROW = HD * 4, AGAIN = ROW % 256 == 128 ? 128 : 256;
+    int k, v;
+    SJD_D explicit PromptPlaces32(int lane) {
+        k = (lane & 31) * ROW + prompt_swizzle(lane & 31, lane >> 5, ROW) * 16;
+        v = 4 * (lane >> 5) * ROW + prompt_swizzle(4 * (lane >> 5), (lane >> 2) & 7, ROW) * 16 + (lane & 3) * 4;
+        asm volatile("" : "+v"(k), "+v"(v));
+    }
+    SJD_D void move(int bytes) { k += bytes; v += bytes; }
+    SJD_D u32x4 keys(const unsigned char *block, int n) const { return *reinterpret_cast<const u32x4 *>(block + (k ^ n * 32 % AGAIN) + n * 32 / AGAIN * AGAIN); }
+    SJD_D float value(const unsigned char *block, int e, int db) const {
+        const int t = 8 * (e >> 2) + (e & 3);        // (its swizzle and that of 4 (lane / 32) have no bit in common)
+        return *reinterpret_cast<const float *>(block + (v ^ prompt_swizzle(t, 0, ROW) * 16 ^ db * 128 % AGAIN) + t * ROW + db * 128 / AGAIN * AGAIN);
+    }
+};
 
 // The running state of 32 rows: O^T, reference of the exponentials (base 2), this lane's half of the sums
 template <int HD> struct PromptState {
@@ -332,38 +324,77 @@ template <typename T, int HD> SJD_D void prompt_add_wild(PromptState<HD> &st, co
             }
 }
 
-// One block of 32 keys and 32 rows, fp32.  `last`: of the block's keys, the last one that the lane's row sees; masked: some row may not see all of them.  -> whether
-// there were values then that are infinite or NaN, and taken as 0.
-template <int HD>
-SJD_D bool prompt_block32(PromptState<HD> &st, const unsigned char *k, const unsigned char *v, const u32x4 (&q)[HD / 8], int last, bool masked, float scale_log2e, int lane) {
-    f32x16 s = prompt_scores32<HD>(k, q, lane);
-    if (masked) {
-        const int mine = last - 4 * (lane >> 5);
+// N matrix products with M other pieces of work spread between them, in this order
+template <int N, int M, typename A, typename B> SJD_D void prompt_spread(A product, B other) {
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[e] = 8 * (e >> 2) + (e & 3) <= mine ? s[e] : -INFINITY;
+    for (int i = 0; i < N; ++i) {
+        product(i);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = i * M / N; j < (i + 1) * M / N; ++j) other(j);
+        __builtin_amdgcn_sched_barrier(0);
     }
-    float mx = s[0];
-#pragma unroll
-    for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
-    mx = prompt_both_halves(mx) * scale_log2e;
-    if (__ballot(mx > st.m)) prompt_rescale<HD>(st, mx);
-    const float m = st.m == -INFINITY ? 0.0f : st.m;        // a row that has seen nothing so far: not (-inf) - (-inf)
-    bool wild = false;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], scale_log2e, -m));
-        st.l += s[e];
-    }
-#pragma unroll
-    for (int e = 0; e < 16; ++e)
-#pragma unroll
-        for (int db = 0; db < HD / 32; ++db) {
-            float x = prompt_value32<HD>(v, e, db, lane);
-            if (masked && prompt_wild(x)) { wild = true; x = 0.0f; }
-            st.o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, s[e], st.o[db], 0, 0, 0);
-        }
-    return __ballot(wild);
 }
+
+// A wavefront of the fp32 kernel: 32 rows, a block of 32 keys at a time.
+template <int HD> struct PromptWave32 {
+    // keys: 4 products from 16 bytes; values: one from 4.  Those that are loaded before their products begin
+    static constexpr int NK = HD / 8, DB = HD / 32, NV = 16 * DB, AHEAD_K = 2, AHEAD_V = 8;
+    PromptState<HD> st;
+    u32x4 q[NK], k[2 * AHEAD_K];
+    float v[2 * AHEAD_V];
+    f32x16 s;
+    bool wild = false;                                // values of blocks that were masked were infinite or NaN
+    PromptPlaces32<HD> at;
+    SJD_D explicit PromptWave32(int lane) : at(lane) { st.clear(); }
+    // last: of the block's keys, the last one that the lane's row sees; masked: some row may not see all of them
+    SJD_D void block(const unsigned char *keys, const unsigned char *values, int last, bool masked, float scale_log2e, int lane) {
+        auto load_k = [&](int n) { k[n % (2 * AHEAD_K)] = at.keys(keys, n); };
+        auto score = [&](int n) {
+            const uint32_t ke = k[n / 4 % (2 * AHEAD_K)][n % 4], qe = q[n / 4][n % 4];
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__builtin_bit_cast(float, ke), __builtin_bit_cast(float, qe), s, 0, 0, 0);
+        };
+        auto load_v = [&](int n) { v[n % (2 * AHEAD_V)] = at.value(values, n / DB, n % DB); };
+        auto product = [&](int n) { st.o[n % DB] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[n % (2 * AHEAD_V)], s[n / DB], st.o[n % DB], 0, 0, 0); };
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int n = 0; n < AHEAD_K; ++n) load_k(n);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = 0.0f;
+        prompt_spread<4 * (NK - AHEAD_K), NK - AHEAD_K>([&](int n) { score(n); }, [&](int n) { load_k(n + AHEAD_K); });
+        prompt_spread<4 * AHEAD_K, 0>([&](int n) { score(4 * (NK - AHEAD_K) + n); }, [&](int) {});
+#pragma unroll
+        for (int n = 0; n < AHEAD_V; ++n) load_v(n);
+        if (masked) {
+            const int mine = last - 4 * (lane >> 5);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = 8 * (e >> 2) + (e & 3) <= mine ? s[e] : -INFINITY;
+        }
+        float mx = s[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
+        mx = prompt_both_halves(mx) * scale_log2e;
+        if (__ballot(mx > st.m)) prompt_rescale<HD>(st, mx);
+        const float m = st.m == -INFINITY ? 0.0f : st.m;        // a row that has seen nothing so far: not (-inf) - (-inf)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], scale_log2e, -m));
+            st.l += s[e];
+        }
+#pragma unroll
+        for (int n = 0; n < NV; n += AHEAD_V) {
+            if (masked)
+#pragma unroll
+                for (int i = 0; i < AHEAD_V; ++i) {
+                    float &x = v[(n + i) % (2 * AHEAD_V)];
+                    if (prompt_wild(x)) { wild = true; x = 0.0f; }
+                }
+            if (n + AHEAD_V < NV) prompt_spread<AHEAD_V, AHEAD_V>([&](int i) { product(n + i); }, [&](int i) { load_v(n + i + AHEAD_V); });
+            else prompt_spread<AHEAD_V, 0>([&](int i) { product(n + i); }, [&](int) {});
+        }
+    }
+};
 
 // What becomes of 32 rows (first: the first of them; node: the lane's row of the sequence): results, or parts of them
 template <typename T, int HD>
@@ -414,19 +445,6 @@ SJD_D void prompt_finish(const PromptArgs &a, const PromptTile &s, const PromptS
             }
             if (live) *reinterpret_cast<u32x4 *>(out + db * 32 + 8 * u) = x;
         }
-}
-
-// N matrix products with M other pieces of work spread between them, in this order
-template <int N, int M, typename A, typename B> SJD_D void prompt_spread(A product, B other) {
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        product(i);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int j = i * M / N; j < (i + 1) * M / N; ++j) other(j);
-        __builtin_amdgcn_sched_barrier(0);
-    }
 }
 
 // A wavefront of the bf16 kernel: 32 rows, a block of keys at a time, 32 (HALVES: 1) or 64 (2).
@@ -589,11 +607,11 @@ __global__ __launch_bounds__(kPromptWaves * 64, prompt_waves_per_simd(2, HD)) vo
     prompt_finish<bf16_t, HD>(a, s, w.st, kvh, range.several, prompt_slot(a, tile, kvh, split) * (ROWS / 32) + wave, row0, node, lane);
 }
 
-// fp32, the same without an order of its own.
+// fp32, the same.
 template <int HD, bool WIDE>
 __global__ __launch_bounds__(kPromptWaves * 64, prompt_waves_per_simd(4, HD)) void prompt_attention32_kernel(PromptArgs a) {
     constexpr int BLOCK = prompt_block(4, HD), BYTES = BLOCK * HD * 4, ROWS = kPromptWaves * 32;
-    __shared__ __attribute__((aligned(16))) unsigned char lds[2][2][BYTES];
+    __shared__ __attribute__((aligned(16))) unsigned char lds[4 * BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int kvh = blockIdx.x % a.n_kv, tile = blockIdx.x / a.n_kv % a.tiles, split = blockIdx.x / a.n_kv / a.tiles;
     const PromptTile s = prompt_find_tile(a, ROWS, tile);
@@ -602,27 +620,33 @@ __global__ __launch_bounds__(kPromptWaves * 64, prompt_waves_per_simd(4, HD)) vo
     if (!range.any) return;
     const float *k = (const float *)a.k + (size_t)s.k0 * a.k_stride + (size_t)kvh * HD, *v = (const float *)a.v + (size_t)s.k0 * a.v_stride + (size_t)kvh * HD;
     const int row0 = s.t * ROWS + wave * 32, offset = prompt_offset(s.n, s.n_keys), node = (row0 + (lane & 31)) / a.G;
-    PromptState<HD> st;
-    u32x4 q[HD / 8];
-    st.clear();
-    prompt_load_q<float, HD>(a, s, kvh, row0, lane, q);
+    PromptWave32<HD> w(lane);
+    prompt_load_q<float, HD>(a, s, kvh, row0, lane, w.q);
     const int sees = node < s.n ? node + offset : -1, low = __builtin_amdgcn_readfirstlane(row0 / a.G + offset);
     const int mine = row0 / a.G < s.n ? __builtin_amdgcn_readfirstlane(min(range.last, (min((row0 + 31) / a.G, s.n - 1) + offset + BLOCK) / BLOCK)) : 0;
     const PromptFetch<float, HD, WIDE> fetch_k(a.k_stride, wave, lane), fetch_v(a.v_stride, wave, lane);
-    auto fetch = [&](int blk, int buf) {
-        fetch_k.run(k, a.k_stride, blk * BLOCK, s.n_keys, lds[buf][0], wave, lane);
-        fetch_v.run(v, a.v_stride, blk * BLOCK, s.n_keys, lds[buf][1], wave, lane);
+    auto fetch = [&](int blk, unsigned char *to) {
+        if (blk >= range.last) return;
+        fetch_k.run(k, a.k_stride, blk * BLOCK, s.n_keys, to, wave, lane);
+        fetch_v.run(v, a.v_stride, blk * BLOCK, s.n_keys, to + BYTES, wave, lane);
     };
-    bool wild = false;
-    if (range.first < range.last) fetch(range.first, 0);
-    for (int blk = range.first; blk < range.last; ++blk) {
-        const int buf = (blk - range.first) & 1, t0 = blk * BLOCK;
+    int blk = range.first, buf = 0;
+    fetch(blk, lds);
+    auto turn = [&]() {
         prompt_barrier();     // this block is there, and everybody is done with the last one
-        if (blk + 1 < range.last) fetch(blk + 1, buf ^ 1);
-        if (blk < mine) wild |= prompt_block32<HD>(st, lds[buf][0], lds[buf][1], q, sees - t0, t0 + BLOCK - 1 > low, a.scale_log2e, lane);
+        buf = 2 * BYTES - buf;
+        fetch(blk + 1, lds + buf);
+    };
+#pragma unroll
+    for (int n = 0; n < HD / 8; ++n) asm volatile("" : "+v"(w.q[n]));        // (as above)
+    for (; blk < mine; ++blk) {
+        turn();
+        w.block(lds, lds + BYTES, sees - blk * BLOCK, blk * BLOCK + BLOCK - 1 > low, a.scale_log2e, lane);
+        w.at.move(buf ? 2 * BYTES : -2 * BYTES);
     }
-    if (wild) prompt_add_wild<float, HD>(st, v, a.v_stride, max(range.first, (low + 1) / BLOCK) * BLOCK, min(mine * BLOCK, s.n_keys), sees, lane);
-    prompt_finish<float, HD>(a, s, st, kvh, range.several, prompt_slot(a, tile, kvh, split) * (ROWS / 32) + wave, row0, node, lane);
+    for (; blk < range.last; ++blk) turn();
+    if (__ballot(w.wild)) prompt_add_wild<float, HD>(w.st, v, a.v_stride, max(range.first, (low + 1) / BLOCK) * BLOCK, min(mine * BLOCK, s.n_keys), sees, lane);
+    prompt_finish<float, HD>(a, s, w.st, kvh, range.several, prompt_slot(a, tile, kvh, split) * (ROWS / 32) + wave, row0, node, lane);
 }
 
 // Joins the splits of every row that has several: out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  A thread owns four dimensions of a row; eight splits are on their way
