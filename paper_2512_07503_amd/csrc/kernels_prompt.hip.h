@@ -649,21 +649,27 @@ __global__ __launch_bounds__(kPromptWaves * 64, prompt_waves_per_simd(4, HD)) vo
     prompt_finish<float, HD>(a, s, w.st, kvh, range.several, prompt_slot(a, tile, kvh, split) * (ROWS / 32) + wave, row0, node, lane);
 }
 
-// Joins the splits of every row that has several: out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  A thread owns four dimensions of a row; eight splits are on their way
-// together.  Where a split saw nothing of a row l = 0.
-template <typename T, int HD>
+// Joins the splits of every row that has several: out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  A thread owns four dimensions of a row, of every WAYS-th eight splits, which are on their
+// way together; WAYS wavefronts share a row.  Where a split saw nothing of a row l = 0.
+struct PromptJoin { float m, denom; f32x4 t; };
+SJD_D void prompt_join_scale(PromptJoin &j, float m_use) {
+    const float alpha = __builtin_amdgcn_exp2f(j.m - m_use);
+    j.denom *= alpha;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) j.t[e] = finite_f(j.t[e]) ? j.t[e] * alpha : j.t[e];      // (alpha may be 0: not 0 * inf)
+}
+template <typename T, int HD, int WAYS>
 __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
-    constexpr int ROWS = kPromptWaves * 32, QUADS = ROWS * (HD / 4), WGS = QUADS / 256, N = 8;
+    constexpr int ROWS = kPromptWaves * 32, QUADS = ROWS * (HD / 4), EACH = 256 / WAYS, WGS = QUADS / EACH, N = 8;
     const int part = blockIdx.x % WGS, kvh = blockIdx.x / WGS % a.n_kv, tile = blockIdx.x / WGS / a.n_kv;
     const PromptTile s = prompt_find_tile(a, ROWS, tile);
     if (s.b < 0) return;
     const int splits = prompt_splits(prompt_keys(s.t, s.n, s.n_keys, a.G, ROWS), prompt_block(sizeof(T), HD), a.n_splits, a.per_split);
-    const int u = part * 256 + threadIdx.x, row = u & 31, j = (u >> 5) % (HD / 4) * 4, sub = (u >> 5) / (HD / 4);
+    const int u = part * EACH + threadIdx.x % EACH, way = threadIdx.x / EACH, row = u & 31, j = (u >> 5) % (HD / 4) * 4, sub = (u >> 5) / (HD / 4);
     const int rho = s.t * ROWS + sub * 32 + row, node = rho / a.G;
-    if (splits == 1 || node >= s.n) return;
-    float m = -INFINITY, denom = 0.0f;
-    f32x4 t = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int i0 = 0; i0 < splits; i0 += N) {
+    if (splits == 1) return;
+    PromptJoin x{-INFINITY, 0.0f, {0.0f, 0.0f, 0.0f, 0.0f}};
+    for (int i0 = way * N; i0 < splits && node < s.n; i0 += WAYS * N) {
         float pm[N], pl[N];
         f32x4 po[N];
 #pragma unroll
@@ -673,25 +679,49 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
             pl[i] = i0 + i < splits ? a.part_ml[slot * 64 + 32 + row] : 0.0f;
             po[i] = *reinterpret_cast<const f32x4 *>(a.part_o + slot * 32 * HD + prompt_part_index(row, j));
         }
-        float m_new = m;
+        float m = x.m;
 #pragma unroll
-        for (int i = 0; i < N; ++i) m_new = fmaxf(m_new, pm[i]);
-        const float m_use = m_new == -INFINITY ? 0.0f : m_new, alpha = __builtin_amdgcn_exp2f(m - m_use);
-        m = m_new;
-        denom *= alpha;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) t[e] = finite_f(t[e]) ? t[e] * alpha : t[e];      // (alpha may be 0: not 0 * inf)
+        for (int i = 0; i < N; ++i) m = fmaxf(m, pm[i]);
+        const float m_use = m == -INFINITY ? 0.0f : m;
+        prompt_join_scale(x, m_use);
+        x.m = m;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             if (pl[i] == 0.0f) continue;
             const float w = __builtin_amdgcn_exp2f(pm[i] - m_use);
-            denom += w * pl[i];
+            x.denom += w * pl[i];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) t[e] += finite_f(po[i][e]) ? w * po[i][e] : po[i][e];
+            for (int e = 0; e < 4; ++e) x.t[e] += finite_f(po[i][e]) ? w * po[i][e] : po[i][e];
         }
     }
-    const float inv = denom == 0.0f ? 0.0f : 1.0f / denom;
+    if constexpr (WAYS > 1) {
+        __shared__ float other[WAYS - 1][6][EACH];
+        if (way) {
+            other[way - 1][0][threadIdx.x % EACH] = x.m;
+            other[way - 1][1][threadIdx.x % EACH] = x.denom;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) t[e] = denom == 0.0f ? 0.0f : t[e] * inv;
-    prompt_store<T>(a, (size_t)s.r0 + node, kvh * a.G + rho - node * a.G, HD, j, t);
+            for (int e = 0; e < 4; ++e) other[way - 1][2 + e][threadIdx.x % EACH] = x.t[e];
+        }
+        __syncthreads();
+        if (way) return;
+        float m = x.m;
+#pragma unroll
+        for (int i = 0; i < WAYS - 1; ++i) m = fmaxf(m, other[i][0][threadIdx.x]);
+        const float m_use = m == -INFINITY ? 0.0f : m;
+        prompt_join_scale(x, m_use);
+#pragma unroll
+        for (int i = 0; i < WAYS - 1; ++i) {
+            PromptJoin y{other[i][0][threadIdx.x], other[i][1][threadIdx.x], {}};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y.t[e] = other[i][2 + e][threadIdx.x];
+            prompt_join_scale(y, m_use);
+            x.denom += y.denom;
+            x.t += y.t;
+        }
+    }
+    if (node >= s.n) return;
+    const float inv = x.denom == 0.0f ? 0.0f : 1.0f / x.denom;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x.t[e] = x.denom == 0.0f ? 0.0f : x.t[e] * inv;
+    prompt_store<T>(a, (size_t)s.r0 + node, kvh * a.G + rho - node * a.G, HD, j, x.t);
 }

@@ -32,16 +32,36 @@ template <typename T> void run_norm_rotary_type(hipStream_t st, dim3 grid, int t
 // ------------------------------------------------------------------------------------------------------------- attention
 struct PromptPlan { int tiles, n_splits, per_split; size_t part_o, part_ml; };
 
-// How many ways the keys of a tile are split: not at all where there is a workgroup for each of the 512 that the card holds, two a CU, without (what is split is written and read
-// once more); else into three times as many, of at least four blocks each, as sequences' lengths differ (1000 rows in 264 tiles behind 21 000 and 30 000 keys: 1, 2, 4, 6, 8, 12 ways: 550,
-// 461, 456, 432, 434, 438 us).
+// Workgroups that a CU holds at a time, by their registers and LDS
+int prompt_resident(int size, int hd) {
+    if (size == 2) return hd <= 32 ? 5 : hd <= 64 ? 4 : hd <= 128 ? 3 : 2;
+    return hd <= 32 ? 5 : hd <= 64 ? 4 : hd <= 96 ? 3 : hd <= 128 ? 2 : 1;
+}
+// How many ways the keys of a tile are split, from an estimate of what that takes, in us.  A block takes `alone`, and `each` of every workgroup of the CU where that is more.  If all workgroups have
+// their places at once, a split's blocks take that, one behind the other; if not, all blocks keep all CUs busy (causal prompts and those shorter than the longest with half of them), and the last
+// splits a part of them.  6 us are a workgroup's beginning and end, each time that all places are taken; several splits are written, read, and joined by a launch more.
+// (Its numbers are those that come nearest to what 1 to 96 ways took for 20 shapes, from one row behind 3 000 keys to 16 behind 100 000 and 4 000 over themselves, in both types: its choice is the best
+// for 14 of them and at most 8 % slower than that.  Three times as many workgroups as have places took twice as long at 4 x 300 rows behind 700, 17 % more at 16 behind 100 000.)
+int prompt_n_splits(int size, int hd, long rows, size_t work, size_t blocks) {
+    const double keys = prompt_block(size, hd) / 32 * (size == 4 ? hd / 64.0 : hd / 128.0), alone = (size == 4 ? 4.3 : 0.58) * keys, each = (size == 4 ? 0.35 : 0.53) * keys;
+    const size_t cus = 256, slots = cus * prompt_resident(size, hd);
+    double best = 0;
+    int n = 1;
+    for (size_t s = 1; s <= blocks && s <= 256; s += s < 4 ? 1 : s & (s - 1) ? s / 3 : s / 2) {       // 1, 2, 3, 4, 6, 8, 12 ..
+        const size_t per = ceil_div_sz(blocks, s), splits = ceil_div_sz(blocks, per), rounds = ceil_div_sz(work * splits, slots);
+        const double shared = each * ceil_div_sz(work * splits, cus);
+        const double us = (rounds <= 1 ? per * (shared > alone ? shared : alone) : 0.54 * each * work * blocks / cus + 0.2 * per * each * slots / cus) + 6 * rounds +
+                          (splits > 1 ? 9 + 0.05 * splits + 0.7e-6 * rows * hd * splits : 0);
+        if (s == 1 || us < best) { best = us; n = (int)splits; }
+    }
+    return n;
+}
 PromptPlan prompt_plan(int dtype, int n_rows, int n_seqs, int n_heads, int n_kv, int hd, int max_kv) {
     PromptPlan p;
     const int G = n_heads / n_kv, rows = kPromptWaves * 32, block = prompt_block(dtype == SJD_F32 ? 4 : 2, hd);
     p.tiles = (int)prompt_max_tiles(n_rows, n_seqs, G, rows);
     const size_t work = (size_t)p.tiles * n_kv, blocks = ceil_div_sz((size_t)max_kv, block);
-    const size_t want = work >= 512 ? 1 : ceil_div_sz(1536, work ? work : 1), most = blocks / 4 ? blocks / 4 : 1;
-    p.n_splits = (int)(want < most ? want : most);
+    p.n_splits = prompt_n_splits(dtype == SJD_F32 ? 4 : 2, hd, (long)n_rows * n_heads, work, blocks);
     p.per_split = (int)ceil_div_sz(blocks ? blocks : 1, p.n_splits);
     const size_t slots = p.n_splits > 1 ? work * p.n_splits * (rows / 32) : 0;
     p.part_o = slots * 32 * hd * sizeof(float);
@@ -49,7 +69,7 @@ PromptPlan prompt_plan(int dtype, int n_rows, int n_seqs, int n_heads, int n_kv,
     return p;
 }
 
-int check_prompt(int32_t dtype, int32_t n_rows, int32_t n_seqs, int32_t n_heads, int32_t n_kv, int32_t hd, int32_t max_rows, int32_t max_kv) {
+int check_prompt(int32_t dtype, int32_t n_rows, int32_t n_seqs, int32_t n_heads, int32_t n_kv, int32_t hd, int32_t max_rows, int32_t max_kv, PromptPlan &p) {
     if (dtype != SJD_F32 && dtype != SJD_BF16) TREE_FAIL(SJD_EINVAL, "rows are SJD_F32 or SJD_BF16");
     switch (hd) {
     case 32: case 64: case 96: case 128: case 192: case 256: break;
@@ -61,8 +81,8 @@ int check_prompt(int32_t dtype, int32_t n_rows, int32_t n_seqs, int32_t n_heads,
     // (and what follows stays within its integers)
     const long G = n_heads / n_kv;
     if (n_rows * G > 1l << 30 || prompt_max_tiles(n_rows, n_seqs, (int)G, 32 * kPromptWaves) * n_kv > (long)kMaxWorkgroups) TREE_FAIL(SJD_EINVAL, "too many rows for one launch");
-    const PromptPlan p = prompt_plan(dtype, n_rows, n_seqs, n_heads, n_kv, hd, max_kv);
-    if ((size_t)p.tiles * n_kv * p.n_splits > kMaxWorkgroups || (p.n_splits > 1 && (size_t)p.tiles * n_kv * (hd / 8) > kMaxWorkgroups))
+    p = prompt_plan(dtype, n_rows, n_seqs, n_heads, n_kv, hd, max_kv);
+    if ((size_t)p.tiles * n_kv * p.n_splits > kMaxWorkgroups || (p.n_splits > 1 && (size_t)p.tiles * n_kv * (hd / 2) > kMaxWorkgroups))
         TREE_FAIL(SJD_EINVAL, "too many rows for one launch");
     return SJD_OK;
 }
@@ -76,7 +96,11 @@ template <typename T, int HD> void run_prompt(hipStream_t st, const PromptArgs &
         if (wide_kv) prompt_attention32_kernel<HD, true><<<grid, kPromptWaves * 64, 0, st>>>(a);
         else prompt_attention32_kernel<HD, false><<<grid, kPromptWaves * 64, 0, st>>>(a);
     }
-    if (a.n_splits > 1) prompt_join_kernel<T, HD><<<(unsigned)((size_t)a.tiles * a.n_kv * (kPromptWaves * 32 * HD / 1024)), 256, 0, st>>>(a);
+    if (a.n_splits > 1) {
+        const unsigned quads = (unsigned)((size_t)a.tiles * a.n_kv * (kPromptWaves * 32 * HD / 1024));
+        if (a.n_splits > 8) prompt_join_kernel<T, HD, 4><<<4 * quads, 256, 0, st>>>(a);
+        else prompt_join_kernel<T, HD, 1><<<quads, 256, 0, st>>>(a);
+    }
 }
 template <typename T> void run_prompt_type(hipStream_t st, int hd, const PromptArgs &a, bool wide_kv) {
     switch (hd) {
@@ -159,9 +183,9 @@ int sjd_op_norm_rotary(void *hip_stream, int32_t dtype, int32_t norm, float eps,
 int sjd_op_prompt_attention_workspace(int32_t dtype, int32_t n_rows, int32_t n_seqs, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_rows,
                                       int32_t max_kv, uint64_t *bytes) {
     if (!bytes) TREE_FAIL(SJD_EINVAL, "null argument");
-    const int rc = check_prompt(dtype, n_rows, n_seqs, n_heads, n_kv_heads, head_dim, max_rows, max_kv);
+    PromptPlan p;
+    const int rc = check_prompt(dtype, n_rows, n_seqs, n_heads, n_kv_heads, head_dim, max_rows, max_kv, p);
     if (rc) return rc;
-    const PromptPlan p = prompt_plan(dtype, n_rows, n_seqs, n_heads, n_kv_heads, head_dim, max_kv);
     *bytes = p.part_o + p.part_ml;
     return SJD_OK;
 }
@@ -170,7 +194,8 @@ int sjd_op_prompt_attention(void *hip_stream, int32_t dtype, const void *q, int6
                             void *out, int64_t out_stride, const int32_t *row_start, const int32_t *kv_start, int32_t n_rows, int32_t n_kv_rows, int32_t n_seqs,
                             int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, float scale, int32_t max_rows, int32_t max_kv, void *workspace,
                             uint64_t workspace_bytes) {
-    const int rc = check_prompt(dtype, n_rows, n_seqs, n_heads, n_kv_heads, head_dim, max_rows, max_kv);
+    PromptPlan p;
+    const int rc = check_prompt(dtype, n_rows, n_seqs, n_heads, n_kv_heads, head_dim, max_rows, max_kv, p);
     if (rc) return rc;
     if (!kv_start) n_kv_rows = n_rows;
     if (n_kv_rows < 0 || n_kv_rows > 1 << 30) TREE_FAIL(SJD_EINVAL, "n_kv_rows must be 0 .. 2^30");
@@ -188,7 +213,6 @@ int sjd_op_prompt_attention(void *hip_stream, int32_t dtype, const void *q, int6
     if (n_kv_rows && (!rows_apart(k, k_stride, kv_row, n_kv_rows, out, out_stride, row, n_rows, size) ||
                       !rows_apart(v, v_stride, kv_row, n_kv_rows, out, out_stride, row, n_rows, size)))
         TREE_FAIL(SJD_EINVAL, "the output overlaps keys or values");
-    const PromptPlan p = prompt_plan(dtype, n_rows, n_seqs, n_heads, n_kv_heads, head_dim, max_kv);
     if (p.part_o + p.part_ml > workspace_bytes)
         TREE_FAIL(SJD_ECAPACITY, "the workspace holds %llu bytes, %zu are needed", (unsigned long long)workspace_bytes, p.part_o + p.part_ml);
     if (p.part_o && (!workspace || (uintptr_t)workspace % 16)) TREE_FAIL(SJD_EINVAL, "the workspace must be 16-byte aligned");
