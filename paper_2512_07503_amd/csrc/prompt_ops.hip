@@ -37,21 +37,23 @@ int prompt_resident(int size, int hd) {
     if (size == 2) return hd <= 32 ? 5 : hd <= 64 ? 4 : hd <= 128 ? 3 : 2;
     return hd <= 32 ? 5 : hd <= 64 ? 4 : hd <= 96 ? 3 : hd <= 128 ? 2 : 1;
 }
-// How many ways the keys of a tile are split, from an estimate of what that takes, in us.  A block takes `alone`, and `each` of every workgroup of the CU where that is more.  If all workgroups have
-// their places at once, a split's blocks take that, one behind the other; if not, all blocks keep all CUs busy (causal prompts and those shorter than the longest with half of them), and the last
-// splits a part of them.  6 us are a workgroup's beginning and end, each time that all places are taken; several splits are written, read, and joined by a launch more.
-// (Its numbers are those that come nearest to what 1 to 96 ways took for 20 shapes, from one row behind 3 000 keys to 16 behind 100 000 and 4 000 over themselves, in both types: its choice is the best
-// for 14 of them and at most 8 % slower than that.  Three times as many workgroups as have places took twice as long at 4 x 300 rows behind 700, 17 % more at 16 behind 100 000.)
+// How many ways the keys of a tile are split: in bf16 not at all where there is a workgroup for every place without (what is split is written and read once more); else from an estimate of what that
+// takes, in us.  A block takes `alone`, and `each` of every workgroup of the CU where that is more.  If all workgroups have their places at once, a split's blocks take that, one behind the other; if
+// not, all blocks keep all CUs busy (71 % of them, as sequences differ, and causal prompts see half of their own rows), and the last splits a part of them.  5.5 us are a workgroup's beginning and end,
+// each time that all places are taken; several splits are written, read, and joined by a launch more.
+// (Its numbers are those that come nearest to what 1 to 96 ways took for 37 shapes of both types, from one row behind 3 000 keys and 16 behind 100 000 to 16 001 over themselves: its choice is the best
+// for 24 of them, and at most 13 % slower than that.  Three times as many workgroups as there are places took 82 % more at 4 x 300 rows behind 700, no splits 27 times as long at 16 behind 100 000.)
 int prompt_n_splits(int size, int hd, long rows, size_t work, size_t blocks) {
-    const double keys = prompt_block(size, hd) / 32 * (size == 4 ? hd / 64.0 : hd / 128.0), alone = (size == 4 ? 4.3 : 0.58) * keys, each = (size == 4 ? 0.35 : 0.53) * keys;
+    const double keys = prompt_block(size, hd) / 32 * (size == 4 ? hd / 64.0 : hd / 128.0), alone = (size == 4 ? 4.7 : 0.84) * keys, each = (size == 4 ? 1.6 : 0.54) * keys;
     const size_t cus = 256, slots = cus * prompt_resident(size, hd);
+    if (size == 2 && work >= slots) return 1;
     double best = 0;
     int n = 1;
     for (size_t s = 1; s <= blocks && s <= 256; s += s < 4 ? 1 : s & (s - 1) ? s / 3 : s / 2) {       // 1, 2, 3, 4, 6, 8, 12 ..
         const size_t per = ceil_div_sz(blocks, s), splits = ceil_div_sz(blocks, per), rounds = ceil_div_sz(work * splits, slots);
         const double shared = each * ceil_div_sz(work * splits, cus);
-        const double us = (rounds <= 1 ? per * (shared > alone ? shared : alone) : 0.54 * each * work * blocks / cus + 0.2 * per * each * slots / cus) + 6 * rounds +
-                          (splits > 1 ? 9 + 0.05 * splits + 0.7e-6 * rows * hd * splits : 0);
+        const double us = (rounds <= 1 ? per * (shared > alone ? shared : alone) : 0.71 * each * work * blocks / cus + 0.67 * per * each * slots / cus) + 5.5 * rounds +
+                          (splits > 1 ? 7 + 0.06 * splits + 1.4e-6 * rows * hd * splits : 0);
         if (s == 1 || us < best) { best = us; n = (int)splits; }
     }
     return n;
