@@ -649,18 +649,25 @@ __global__ __launch_bounds__(kPromptWaves * 64, prompt_waves_per_simd(4, HD)) vo
     prompt_finish<float, HD>(a, s, w.st, kvh, range.several, prompt_slot(a, tile, kvh, split) * (ROWS / 32) + wave, row0, node, lane);
 }
 
-// Joins the splits of every row that has several: out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  A thread owns four dimensions of a row, of every WAYS-th eight splits, which are on their
+// Joins the splits of every row that has several: out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  A thread owns four dimensions of a row, of every WAYS-th few splits, which are on their
 // way together; WAYS wavefronts share a row.  Where a split saw nothing of a row l = 0.
+// CAREFUL: infinities stay what they are when their weight is 0 (a result that is NaN without is computed once more so).
 struct PromptJoin { float m, denom; f32x4 t; };
-SJD_D void prompt_join_scale(PromptJoin &j, float m_use) {
-    const float alpha = __builtin_amdgcn_exp2f(j.m - m_use);
-    j.denom *= alpha;
+template <bool CAREFUL> SJD_D f32x4 prompt_weighted(f32x4 t, float w) {
+    if constexpr (!CAREFUL) return t * w;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) j.t[e] = finite_f(j.t[e]) ? j.t[e] * alpha : j.t[e];      // (alpha may be 0: not 0 * inf)
+    for (int e = 0; e < 4; ++e) t[e] = finite_f(t[e]) ? t[e] * w : t[e];
+    return t;
+}
+// a and b, about the larger reference
+template <bool CAREFUL> SJD_D PromptJoin prompt_join(PromptJoin a, PromptJoin b) {
+    const float m = fmaxf(a.m, b.m), m_use = m == -INFINITY ? 0.0f : m, x = __builtin_amdgcn_exp2f(a.m - m_use), y = __builtin_amdgcn_exp2f(b.m - m_use);
+    return {m, a.denom * x + b.denom * y, prompt_weighted<CAREFUL>(a.t, x) + prompt_weighted<CAREFUL>(b.t, y)};
 }
 template <typename T, int HD, int WAYS>
 __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
-    constexpr int ROWS = kPromptWaves * 32, QUADS = ROWS * (HD / 4), EACH = 256 / WAYS, WGS = QUADS / EACH, N = 8;
+    constexpr int ROWS = kPromptWaves * 32, QUADS = ROWS * (HD / 4), EACH = 256 / WAYS, WGS = QUADS / EACH, N = WAYS == 1 ? 8 : 4;
+    __shared__ PromptJoin other[WAYS][EACH];
     const int part = blockIdx.x % WGS, kvh = blockIdx.x / WGS % a.n_kv, tile = blockIdx.x / WGS / a.n_kv;
     const PromptTile s = prompt_find_tile(a, ROWS, tile);
     if (s.b < 0) return;
@@ -668,56 +675,41 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
     const int u = part * EACH + threadIdx.x % EACH, way = threadIdx.x / EACH, row = u & 31, j = (u >> 5) % (HD / 4) * 4, sub = (u >> 5) / (HD / 4);
     const int rho = s.t * ROWS + sub * 32 + row, node = rho / a.G;
     if (splits == 1) return;
-    PromptJoin x{-INFINITY, 0.0f, {0.0f, 0.0f, 0.0f, 0.0f}};
-    for (int i0 = way * N; i0 < splits && node < s.n; i0 += WAYS * N) {
-        float pm[N], pl[N];
-        f32x4 po[N];
+    auto sum = [&](auto careful) {
+        PromptJoin x{-INFINITY, 0.0f, {0.0f, 0.0f, 0.0f, 0.0f}};
+        for (int i0 = way * N; i0 < splits && node < s.n; i0 += WAYS * N) {
+            PromptJoin y[N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const size_t slot = prompt_slot(a, tile, kvh, min(i0 + i, splits - 1)) * (ROWS / 32) + sub;
-            pm[i] = a.part_ml[slot * 64 + row];
-            pl[i] = i0 + i < splits ? a.part_ml[slot * 64 + 32 + row] : 0.0f;
-            po[i] = *reinterpret_cast<const f32x4 *>(a.part_o + slot * 32 * HD + prompt_part_index(row, j));
+            for (int i = 0; i < N; ++i) {
+                const size_t slot = prompt_slot(a, tile, kvh, min(i0 + i, splits - 1)) * (ROWS / 32) + sub;
+                y[i].m = a.part_ml[slot * 64 + row];
+                y[i].denom = i0 + i < splits ? a.part_ml[slot * 64 + 32 + row] : 0.0f;
+                y[i].t = *reinterpret_cast<const f32x4 *>(a.part_o + slot * 32 * HD + prompt_part_index(row, j));
+            }
+            float m = x.m;
+#pragma unroll
+            for (int i = 0; i < N; ++i) m = fmaxf(m, y[i].m);
+            const float m_use = m == -INFINITY ? 0.0f : m, alpha = __builtin_amdgcn_exp2f(x.m - m_use);
+            x.m = m;
+            x.denom *= alpha;
+            x.t = prompt_weighted<decltype(careful)::value>(x.t, alpha);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float w = y[i].denom == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(y[i].m - m_use);
+                x.denom += w * y[i].denom;
+                x.t += prompt_weighted<decltype(careful)::value>(y[i].t, w);
+            }
         }
-        float m = x.m;
-#pragma unroll
-        for (int i = 0; i < N; ++i) m = fmaxf(m, pm[i]);
-        const float m_use = m == -INFINITY ? 0.0f : m;
-        prompt_join_scale(x, m_use);
-        x.m = m;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            if (pl[i] == 0.0f) continue;
-            const float w = __builtin_amdgcn_exp2f(pm[i] - m_use);
-            x.denom += w * pl[i];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x.t[e] += finite_f(po[i][e]) ? w * po[i][e] : po[i][e];
-        }
-    }
+        return x;
+    };
+    PromptJoin x = sum(std::false_type());
+    if (__ballot(!(x.t[0] + x.t[1] + x.t[2] + x.t[3] == x.t[0] + x.t[1] + x.t[2] + x.t[3]))) x = sum(std::true_type());
     if constexpr (WAYS > 1) {
-        __shared__ float other[WAYS - 1][6][EACH];
-        if (way) {
-            other[way - 1][0][threadIdx.x % EACH] = x.m;
-            other[way - 1][1][threadIdx.x % EACH] = x.denom;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) other[way - 1][2 + e][threadIdx.x % EACH] = x.t[e];
-        }
+        if (way) other[way][threadIdx.x % EACH] = x;
         __syncthreads();
         if (way) return;
-        float m = x.m;
 #pragma unroll
-        for (int i = 0; i < WAYS - 1; ++i) m = fmaxf(m, other[i][0][threadIdx.x]);
-        const float m_use = m == -INFINITY ? 0.0f : m;
-        prompt_join_scale(x, m_use);
-#pragma unroll
-        for (int i = 0; i < WAYS - 1; ++i) {
-            PromptJoin y{other[i][0][threadIdx.x], other[i][1][threadIdx.x], {}};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y.t[e] = other[i][2 + e][threadIdx.x];
-            prompt_join_scale(y, m_use);
-            x.denom += y.denom;
-            x.t += y.t;
-        }
+        for (int i = 1; i < WAYS; ++i) x = prompt_join<true>(x, other[i][threadIdx.x]);
     }
     if (node >= s.n) return;
     const float inv = x.denom == 0.0f ? 0.0f : 1.0f / x.denom;
