@@ -1,6 +1,11 @@
 // Norms of queries and keys for each head, and the rotary positions (kernels_rotary.hip.h) in the same pass:
 //   y = (x - c) / sqrt(mean((x - c)^2) + eps) * gain + bias,   c = 0 or the mean,   then pairs of y turned.
 // A head is held in the registers of a team of lanes, 16 elements each, from the load to the store: read once, written once, rounded once.
+//
+// What bounds it: memory, and as soon as that is near, the vector units (bf16, 12 000 rows of 40 heads of 128, root mean squares: 40 us, 6.1 TB/s where a copy does 5.0 - 5.5, as half of it
+// stays in the card's cache; vector units busy for 75 % of the cycles; 9 408 rows of 64 heads with means, gains and biases 62 us, 5.0 TB/s, 73 %).  A team is as small as a head allows, so that a sum over it is a few
+// moves within a wavefront; a team's next head is loaded while this one is worked on (89 -> 49 us); and a row's sines are computed once, by the workgroup, for all of its heads.  Few rows are one head a
+// team, and latency (8 rows of 40 heads: 3.6 us).
 #pragma once
 #include "kernels_rotary.hip.h"
 #include "lanes.hip.h"

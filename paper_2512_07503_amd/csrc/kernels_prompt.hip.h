@@ -1,10 +1,19 @@
 // Attention of packed prompts: causal, grouped heads, ragged sequences, keys and values as they come from a projection or from a cache that was read back.
 //
 // Rows (i, h) of one kv head of a sequence are cut into tiles (prompt_layout.h), so that the query heads of a group share keys and values.  Per block
-// of keys a wavefront computes, for each of its tiles of 32 rows,
+// of keys a wavefront computes, for 32 of its tile's rows,
 //   S^T (keys x rows) = K Q^T,   online softmax per row = per accumulator column,   O^T (dimensions x rows) += V^T P^T,
 // and P^T needs no data movement: the accumulator registers of S^T are the B operand of the second product, if the keys of V^T are taken in their order.
-// Keys and values go through LDS, straight from memory, for all wavefronts of a workgroup.
+// Keys and values go through LDS, straight from memory, for all four wavefronts of a workgroup; a block's products come from there while the next one arrives.
+//
+// What bounds it: matrix and vector units, and, before either is full, the card's power (bf16, 16 001 rows of 32 heads of 128 in 8 groups: 1 880 - 1 980 us, 1.06 - 1.12 PFLOP/s, where a large library
+// product reaches 1.22 - 1.4; matrix units busy for 58 % of the cycles, vector units for 47, at 1.5 - 1.7 GHz).  A block's 16 products of 32 rows are 512 cycles of a SIMD, its exponentials and what
+// belongs to them some 75 instructions, which other wavefronts' products hide; there are two to five of them a SIMD.  Short prompts pay for a tile's beginning and end, some 9 us with waiting, of
+// which the CU's other workgroups hide a part (12 prompts of 61 to 2 352 rows, 32 heads of 128: 248 - 259 us, 0.75 - 0.78 PFLOP/s; 38 % and 39 %).  fp32: the matrix units' own rate, 154
+// TFLOP/s (2 048 rows of 16 heads: 78 - 88 from heads of 64 on).
+// Tried, and not here: workgroups of 8 wavefronts with four blocks in LDS (16 001 rows: the same; 12 prompts 3 % slower), parts of a block's products between another's exponentials in one wavefront (10 %
+// slower), 64 rows a wavefront (registers), workgroups that stay and take one tile after the other with the next one's keys on their way (12 prompts 12 % slower: shares fixed beforehand come out uneven,
+// and each block has more to keep track of), values on their way to registers before the exponentials (the same with heads of 128, 10 to 26 % slower with 64, 192 and 256).
 #pragma once
 #include <type_traits>
 
