@@ -466,9 +466,11 @@ template <int HD> struct PromptWave16 {
     u32x4 q[NQ], k[HELD], v[HELD], p[HALVES][2];      // operands: queries, keys, values, probabilities
     f32x16 s[HALVES];
     float m, sum, e0, e1;
+    float unset;                                      // NaN as long as m is nothing yet, of a row that sees something; else 0
     bool wild = false;                                // values of blocks that were masked were infinite or NaN
     PromptPlaces<HD> at;
     SJD_D explicit PromptWave16(int lane) : at(lane) { st.clear(); m = 0.0f; }
+    SJD_D void begin(bool sees) { unset = sees ? NAN : 0.0f; }
     SJD_D void load_k(const unsigned char *block, int n) { k[n % HELD] = at.keys(block, n / NQ, n % NQ); }
     SJD_D void load_v(const unsigned char *block, int n) { v[n % HELD] = at.values(block, n / DB, n % DB); }
     SJD_D void score(int n) {
@@ -485,7 +487,7 @@ template <int HD> struct PromptWave16 {
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[i][e] = 32 * i + 8 * (e >> 2) + (e & 3) <= mine ? s[i][e] : -INFINITY;
     }
-    // Probabilities are 2^(score - m).  As long as a lane's of a block add up to at most 1 none is above 1, and m stays; else, and at first, it is put ahead of the largest score.
+    // Probabilities are 2^(score - m).  As long as a lane's of a block add up to at most 1 none is above 1, and m stays; else, and until there is a score above -inf, it is put ahead of the largest score.
     SJD_D void settle(float scale_log2e) {
         float mx = s[0][0];
 #pragma unroll
@@ -494,6 +496,7 @@ template <int HD> struct PromptWave16 {
             for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[i][e]);
         prompt_rescale<HD>(st, prompt_both_halves(mx) * scale_log2e);
         m = st.m == -INFINITY ? 0.0f : st.m;           // a row that has seen nothing: not (-inf) - (-inf)
+        unset = st.m == -INFINITY ? unset : 0.0f;
     }
     // probabilities 2 n and 2 n + 1; those of n - 1 as operands.  What the products take is what the sum adds, so that a row's weights add up to 1 whatever their rounding to bf16 (a row
     // that sees one key gives its value, exactly).
@@ -508,8 +511,8 @@ template <int HD> struct PromptWave16 {
             e1 = __builtin_amdgcn_exp2f(fmaf(s[I][2 * n + 1], scale_log2e, -m));
         }
     }
-    SJD_D void weigh_all(float scale_log2e) {
-        sum = 0.0f;
+    SJD_D void weigh_all(float scale_log2e, float from) {
+        sum = from;
 #pragma unroll
         for (int n = 0; n < 9; ++n) weigh<0>(n, scale_log2e);
         if constexpr (HALVES == 2)
@@ -539,8 +542,8 @@ template <int HD> struct PromptWave16 {
         }
         return found;
     }
-    // A block.  last: of its keys, the last one that the lane's row sees; masked: some row may not see all of it; first: nothing came before it.
-    SJD_D void block(const unsigned char *keys, const unsigned char *values, int last, bool masked, bool first, float scale_log2e) {
+    // A block.  last: of its keys, the last one that the lane's row sees; masked: some row may not see all of it.
+    SJD_D void block(const unsigned char *keys, const unsigned char *values, int last, bool masked, float scale_log2e) {
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int n = 0; n < AHEAD; ++n) load_k(keys, n);
@@ -549,10 +552,10 @@ template <int HD> struct PromptWave16 {
         prompt_spread<AHEAD, 0>([&](int n) { score(NK - AHEAD + n); }, [&](int) {});
         __builtin_amdgcn_s_setprio(0);
         if (masked) mask(last);
-        weigh_all(scale_log2e);
-        if (__ballot(first || !(sum <= 1.0f))) {
+        weigh_all(scale_log2e, unset);
+        if (__ballot(!(sum <= 1.0f))) {
             settle(scale_log2e);
-            weigh_all(scale_log2e);
+            weigh_all(scale_log2e, 0.0f);
         }
         st.l += sum;
 #pragma unroll
@@ -605,9 +608,10 @@ __global__ __launch_bounds__(kPromptWaves * 64, prompt_waves_per_simd(2, HD)) vo
     // (queries: waited for here; at their first use, in the loop, it would be a wait for everything, every time)
 #pragma unroll
     for (int n = 0; n < HD / 16; ++n) asm volatile("" : "+v"(w.q[n]));
+    w.begin(sees >= blk * BLOCK);
     for (; blk < mine; ++blk) {
         turn();
-        w.block(lds, lds + BYTES, sees - blk * BLOCK, blk * BLOCK + BLOCK - 1 > low, blk == range.first, a.scale_log2e);
+        w.block(lds, lds + BYTES, sees - blk * BLOCK, blk * BLOCK + BLOCK - 1 > low, a.scale_log2e);
         w.at.move(buf ? 2 * BYTES : -2 * BYTES);
     }
     // what is left the other wavefronts see: this one helps to fetch (in a loop of its own: with a branch around the block above the output would be copied every time)

@@ -63,7 +63,9 @@ PromptPlan prompt_plan(int dtype, int n_rows, int n_seqs, int n_heads, int n_kv,
     const int G = n_heads / n_kv, rows = kPromptWaves * 32, block = prompt_block(dtype == SJD_F32 ? 4 : 2, hd);
     p.tiles = (int)prompt_max_tiles(n_rows, n_seqs, G, rows);
     const size_t work = (size_t)p.tiles * n_kv, blocks = ceil_div_sz((size_t)max_kv, block);
-    p.n_splits = prompt_n_splits(dtype == SJD_F32 ? 4 : 2, hd, (long)n_rows * n_heads, work, blocks);
+    // (places of sequences that have no rows are not counted)
+    const size_t busy = ((size_t)n_rows * G / rows + (n_seqs < n_rows ? n_seqs : n_rows)) * n_kv;
+    p.n_splits = prompt_n_splits(dtype == SJD_F32 ? 4 : 2, hd, (long)n_rows * n_heads, busy, blocks);
     p.per_split = (int)ceil_div_sz(blocks ? blocks : 1, p.n_splits);
     const size_t slots = p.n_splits > 1 ? work * p.n_splits * (rows / 32) : 0;
     p.part_o = slots * 32 * hd * sizeof(float);
@@ -78,7 +80,7 @@ int check_prompt(int32_t dtype, int32_t n_rows, int32_t n_seqs, int32_t n_heads,
     default: TREE_FAIL(SJD_EINVAL, "head_dim must be 32, 64, 96, 128, 192 or 256");
     }
     if (n_kv < 1 || n_kv > 65535 || n_heads < 1 || n_heads % n_kv || n_heads > 1 << 20) TREE_FAIL(SJD_EINVAL, "n_kv_heads must be 1 .. 65535, n_heads a multiple of it");
-    if (n_seqs < 1 || n_rows < 0 || n_rows > 1 << 29) TREE_FAIL(SJD_EINVAL, "n_seqs must be positive, n_rows 0 .. 2^29");
+    if (n_seqs < 1 || n_seqs > 1 << 30 || n_rows < 0 || n_rows > 1 << 29) TREE_FAIL(SJD_EINVAL, "n_seqs must be 1 .. 2^30, n_rows 0 .. 2^29");
     if (max_rows < 0 || max_rows > 1 << 29 || max_kv < 0 || max_kv > 1 << 30) TREE_FAIL(SJD_EINVAL, "max_rows must be 0 .. 2^29, max_kv 0 .. 2^30");
     // (and what follows stays within its integers)
     const long G = n_heads / n_kv;

@@ -324,3 +324,30 @@ def test_many_sequences(dtype, n_seqs, most):
     c = Case(dtype, 3, 3, 32, n, t, seed=23, lead=3, trail=200)
     c.check(c.run())
     c.check(c.run(max_kv=1000))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hd", [64, 128, 256])
+@pytest.mark.parametrize("max_kv", [100, 100000])
+def test_scores_that_are_minus_infinity(dtype, hd, max_kv):
+    """The first 70 of 100 keys have no weight, and the others' scores are far below 0: the result is that of the others alone."""
+    def edit(c):
+        c.q[..., 0], c.q[..., 1] = 1.0, 1.0
+        c.k[:70, :, 0] = float("-inf")
+        c.k[70:, :, 1] = -300.0 * hd ** 0.5
+    c = Case(dtype, 4, 2, hd, [30], [100], seed=24, edit=edit)
+    few = Case(dtype, 4, 2, hd, [30], [30], seed=24)
+    few.q, few.k, few.v = c.q, c.k[70:], c.v[70:]
+    few.check(c.run(max_kv=max_kv))
+
+
+@pytest.mark.parametrize("n_seqs", [64, 500])
+def test_slots_without_rows_do_not_change_the_division(n_seqs):
+    """A batch of slots of which few have a row, behind many keys: the same result, and a workspace as for those alone."""
+    import paper_2512_07503_amd as sjd
+    n, t = [0] * n_seqs, [0] * n_seqs
+    n[1], n[40], n[63] = 1, 3, 1
+    t[1], t[40], t[63] = 3000, 2000, 50
+    c = Case("bf16", 8, 2, 128, n, t, seed=25)
+    c.check(c.run())
+    assert sjd.binding._prompt_bytes(sjd.BF16, 5, n_seqs, 8, 2, 128, 3, 3000) > 0
