@@ -10,7 +10,7 @@
 // as equal ones have larger ids.  At most one step's elements come at a time, so that a buffer of them and 64 more always holds them, after a selection of the n best.
 //
 // What bounds it: without ids memory, and the vector units behind it, an exponential and four to five other instructions an element (bf16, 4 099 rows of 65 536: 99 us, 5.4 TB/s; vector units busy for
-// 75 % of the cycles).  With ids, what is collected: short rows are few steps, the first of which collects the most (fp32, 256 rows of 65 536, 20 ids: 26.5 + 4.3 us for the joining
+// 75 % of the cycles).  With ids, what is collected: short rows are few steps, the first of which collects the most (fp32, 256 rows of 65 536, 20 ids: 25.8 + 4.2 us for the joining
 // launch, 2.3 TB/s; vector units 43 %, the rest waits; of a row four workgroups have a part each).  Few rows: latency (8 of 16 384, 5 ids: 7.8 + 4.0 us; bf16, 33 rows of 184 621 of which 32 770 ids may be
 // taken, 20 ids: 15.8 + 4.8 us).
 // Tried, and not here: four steps' loads at a time (registers: 37 against 30 us for the 256 rows), thresholds from every lane's largest element so far in every step (the same there, 33 masked rows 23
@@ -260,7 +260,9 @@ SJD_D void logprob_step(LogprobState &st, const float (&z)[16], Id id, uint32_t 
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const uint64_t takes = __ballot(z[e] >= st.least);
-            if (z[e] >= st.least) keys[st.count + __popcll(takes & ((1ull << lane) - 1))] = logprob_key(z[e], id(e));
+            if (!takes) continue;
+            const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(takes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)takes, 0u));
+            if (z[e] >= st.least) keys[st.count + before] = logprob_key(z[e], id(e));
             st.count += __popcll(takes);
         }
         if (n >= n_top) st.least = logprob_above(st.least);
