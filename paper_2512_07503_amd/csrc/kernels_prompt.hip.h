@@ -542,7 +542,8 @@ template <int HD> struct PromptWave16 {
         }
         return found;
     }
-    // A block.  last: of its keys, the last one that the lane's row sees; masked: some row may not see all of it.
+    // A block.  last: of its keys, the last one that the lane's row sees; masked: some row may not see all of it.  (Who has products goes first: 8 192 rows of 16 heads of 192 and 256 1 089 and
+    // 1 158 TFLOP/s, 1 022 and 1 048 without; with narrower ones the same.)
     SJD_D void block(const unsigned char *keys, const unsigned char *values, int last, bool masked, float scale_log2e) {
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll

@@ -119,6 +119,7 @@ template <typename T> void run_prompt_type(hipStream_t st, int hd, const PromptA
 
 // ------------------------------------------------------------------------------------------------------ log probabilities
 // How many workgroups a row is split over: as many as the card holds at once, four a CU, but none with less than one step a wavefront, and no more than one joining workgroup holds.
+// (512, 768, 1024, 2048 workgroups: 256 rows of 65 536 with 20 ids 30.7, 30.7, 28.7, 37.8 us, 33 masked rows of 184 621 25.3, 21.9, 20.3, 22.0.)
 int logprob_splits(int n_rows, int vocab, int n_top) {
     const int want = 1024 / (n_rows > 0 ? n_rows : 1), most = vocab / (kLogprobWaves * kLogprobStep), held = n_top ? kLogprobJoin / n_top : 64;
     int n = want < most ? want : most;
