@@ -542,16 +542,19 @@ template <int HD> struct PromptWave16 {
         }
         return found;
     }
-    // A block.  last: of its keys, the last one that the lane's row sees; masked: some row may not see all of it.  (Who has products goes first: 8 192 rows of 16 heads of 192 and 256 1 089 and
-    // 1 158 TFLOP/s, 1 022 and 1 048 without; with narrower ones the same.)
+    // Who has products goes first (8 192 rows of 16 heads of 192 and 256 1 089 and 1 158 TFLOP/s, 1 022 and 1 048 without; of 128 the same; of 64 and 96 785 and 964, 808 and 978 without).
+    template <int P> static SJD_D void priority() {
+        if constexpr (HALVES == 1) __builtin_amdgcn_s_setprio(P);
+    }
+    // A block.  last: of its keys, the last one that the lane's row sees; masked: some row may not see all of it.
     SJD_D void block(const unsigned char *keys, const unsigned char *values, int last, bool masked, float scale_log2e) {
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int n = 0; n < AHEAD; ++n) load_k(keys, n);
-        __builtin_amdgcn_s_setprio(1);
+        priority<1>();
         prompt_spread<NK - AHEAD, NK - AHEAD>([&](int n) { score(n); }, [&](int n) { load_k(keys, n + AHEAD); });
         prompt_spread<AHEAD, 0>([&](int n) { score(NK - AHEAD + n); }, [&](int) {});
-        __builtin_amdgcn_s_setprio(0);
+        priority<0>();
         if (masked) mask(last);
         weigh_all(scale_log2e, unset);
         if (__ballot(!(sum <= 1.0f))) {
@@ -564,11 +567,11 @@ template <int HD> struct PromptWave16 {
 #pragma unroll
         for (int n = 0; n < NV; n += AHEAD) {           // (those of a masked block are looked at while the next ones are not yet there)
             if (masked) wild |= tame<AHEAD>(v + n % HELD);
-            __builtin_amdgcn_s_setprio(1);
+            priority<1>();
             if (n + AHEAD < NV) prompt_spread<AHEAD, AHEAD>([&](int i) { product(n + i); }, [&](int i) { load_v(values, n + i + AHEAD); });
             else prompt_spread<AHEAD, 0>([&](int i) { product(n + i); }, [&](int) {});
         }
-        __builtin_amdgcn_s_setprio(0);
+        priority<0>();
     }
 };
 
