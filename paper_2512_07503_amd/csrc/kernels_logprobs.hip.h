@@ -11,7 +11,7 @@
 //
 // What bounds it: without ids memory, and the vector units behind it, an exponential and four to five other instructions an element (bf16, 4 099 rows of 65 536: 99 us, 5.4 TB/s; vector units busy for
 // 75 % of the cycles).  With ids, what is collected: short rows are few steps, the first of which collects the most (fp32, 256 rows of 65 536, 20 ids: 25.8 + 4.2 us for the joining
-// launch, 2.3 TB/s; vector units 43 %, the rest waits; of a row four workgroups have a part each).  Few rows: latency (8 of 16 384, 5 ids: 7.8 + 4.0 us; bf16, 33 rows of 184 621 of which 32 770 ids may be
+// launch, 2.3 TB/s; vector units 43 %, the rest waits; of a row four workgroups have a part each).  Few rows: latency (8 of 16 384, 5 ids: 13.8 us; bf16, 33 rows of 184 621 of which 32 770 ids may be
 // taken, 20 ids: 15.8 + 4.8 us).
 // Tried, and not here: four steps' loads at a time (registers: 37 against 30 us for the 256 rows), thresholds from every lane's largest element so far in every step (the same there, 33 masked rows 23
 // against 20 us), a second round of workgroups that only ranks.

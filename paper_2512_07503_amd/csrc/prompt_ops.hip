@@ -120,7 +120,10 @@ template <typename T> void run_prompt_type(hipStream_t st, int hd, const PromptA
 // ------------------------------------------------------------------------------------------------------ log probabilities
 // How many workgroups a row is split over: as many as the card holds at once, four a CU, but none with less than one step a wavefront, and no more than one joining workgroup holds.
 // (512, 768, 1024, 2048 workgroups: 256 rows of 65 536 with 20 ids 30.7, 30.7, 28.7, 37.8 us, 33 masked rows of 184 621 25.3, 21.9, 20.3, 22.0.)
+// Up to four steps a wavefront a row is not split: the launch that joins takes longer, or, where it does not, costs the host more than it saves (8 rows, in a graph and call by call: 8 192 with 5 ids
+// 9.5 and 12.8 us, split 10.5 and 16.7; 16 384 without ids 7.0 and 12.5, 7.1 and 16.6, with 5 13.2 and 13.3, 10.4 and 17.1; 65 536 with 5 33.4 and 33.6, 11.1 and 16.8).
 int logprob_splits(int n_rows, int vocab, int n_top) {
+    if (vocab <= 4 * kLogprobWaves * kLogprobStep) return 1;
     const int want = 1024 / (n_rows > 0 ? n_rows : 1), most = vocab / (kLogprobWaves * kLogprobStep), held = n_top ? kLogprobJoin / n_top : 64;
     int n = want < most ? want : most;
     if (n > held) n = held;

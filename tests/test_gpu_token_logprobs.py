@@ -34,7 +34,7 @@ def tensors(z, tokens, dtype):
     return t if dtype == "f32" else t.bfloat16(), torch.tensor(np.asarray(tokens, dtype=np.int32), device="cuda")
 
 
-SHAPES = [(1, 1), (3, 2), (5, 7), (2, 63), (4, 64), (3, 100), (7, 1000), (2, 1023), (2, 4096), (3, 4099), (1, 16384), (40, 5003), (5, 70001), (1100, 300), (2, 200003)]
+SHAPES = [(1, 1), (3, 2), (5, 7), (2, 63), (4, 64), (3, 100), (7, 1000), (2, 1023), (2, 4096), (3, 4099), (1, 16384), (3, 16385), (2, 20001), (40, 5003), (5, 70001), (1100, 300), (2, 200003)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
