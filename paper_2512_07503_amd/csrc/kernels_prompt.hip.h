@@ -77,7 +77,7 @@ SJD_D PromptTile prompt_find_tile(const PromptArgs &a, int rows, int index) {
             const int step = (n + 63) / 64;
             const bool in = lane * step < n;
             b = lo + lane * step;
-            const int start = in ? prompt_first_tile(rows_first(a.row_start, b, a.n_rows), b, a.G, rows) : 0;
+            const int start = in ? prompt_place(rows_first(a.row_start, b, a.n_rows), b, a.G, rows) : 0;
             const unsigned long long upto = __ballot(in && start <= index);
             if (!upto) return PromptTile{-1, 0, 0, 0, 0, 0};
             l = 63 - __clzll((long long)upto);

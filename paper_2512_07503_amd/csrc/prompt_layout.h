@@ -13,10 +13,10 @@ constexpr int prompt_offset(int n, int n_keys) { return n_keys - n; }
 constexpr int prompt_tiles(int n, int G, int tile) { return (int)(((long)n * G + tile - 1) / tile); }
 // Where the tiles of sequence b begin whose rows begin at `first`, if every sequence has its place whatever those before it have: places ascend, and those behind a sequence's tiles are empty.
 constexpr int prompt_first_tile(int first, int b, int G, int tile) { return (int)((long)first * G / tile) + b; }
-// An upper bound of the tiles, and of these places, over n_rows rows of n_seqs sequences
-constexpr long prompt_max_tiles(long n_rows, long n_seqs, int G, int tile) {
-    return n_rows * G / tile + (n_seqs < n_rows || n_seqs > 64 ? n_seqs : n_rows);
-}
+// Where they begin if only sequences with rows have places (those without lie where the next one begins, or behind the last): of the sequences before b at most `first` have rows.
+constexpr int prompt_place(int first, int b, int G, int tile) { return prompt_first_tile(first, b < first ? b : first, G, tile); }
+// An upper bound of the tiles, and of these places, over n_rows rows of n_seqs sequences, however many of them have rows
+constexpr long prompt_max_tiles(long n_rows, long n_seqs, int G, int tile) { return n_rows * G / tile + (n_seqs < n_rows ? n_seqs : n_rows); }
 // keys that some row of tile t of a sequence sees: 0 .. prompt_keys - 1
 constexpr int prompt_keys(int t, int n, int n_keys, int G, int tile) {
     const long last = ((long)(t + 1) * tile - 1) / G;

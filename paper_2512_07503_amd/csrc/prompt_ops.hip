@@ -63,9 +63,7 @@ PromptPlan prompt_plan(int dtype, int n_rows, int n_seqs, int n_heads, int n_kv,
     const int G = n_heads / n_kv, rows = kPromptWaves * 32, block = prompt_block(dtype == SJD_F32 ? 4 : 2, hd);
     p.tiles = (int)prompt_max_tiles(n_rows, n_seqs, G, rows);
     const size_t work = (size_t)p.tiles * n_kv, blocks = ceil_div_sz((size_t)max_kv, block);
-    // (places of sequences that have no rows are not counted)
-    const size_t busy = ((size_t)n_rows * G / rows + (n_seqs < n_rows ? n_seqs : n_rows)) * n_kv;
-    p.n_splits = prompt_n_splits(dtype == SJD_F32 ? 4 : 2, hd, (long)n_rows * n_heads, busy, blocks);
+    p.n_splits = prompt_n_splits(dtype == SJD_F32 ? 4 : 2, hd, (long)n_rows * n_heads, work, blocks);
     p.per_split = (int)ceil_div_sz(blocks ? blocks : 1, p.n_splits);
     const size_t slots = p.n_splits > 1 ? work * p.n_splits * (rows / 32) : 0;
     p.part_o = slots * 32 * hd * sizeof(float);

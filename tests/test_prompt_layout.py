@@ -89,3 +89,57 @@ def test_tiles_splits_and_places(tmp_path):
                     str(tmp_path / "main")], check=True)
     r = subprocess.run([str(tmp_path / "main")], capture_output=True, text=True)
     assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout + r.stderr
+
+
+_PLACES = r"""
+#include <cstdio>
+#include <cstdlib>
+#include <vector>
+#include "prompt_layout.h"
+#define CHECK(c) do { if (!(c)) { printf("line %d: %s\n", __LINE__, #c); exit(1); } } while (0)
+
+int main() {
+    srand(2);
+    for (int it = 0; it < 3000; ++it) {
+        const int seqs = 1 + rand() % (it % 2 ? 9 : 400), G = 1 + rand() % 8, tile = 32 << rand() % 4, live = 1 + rand() % 100;
+        std::vector<int> start(seqs + 1), owner, of;
+        start[0] = rand() % 3 ? 0 : rand() % 300;
+        for (int b = 0; b < seqs; ++b) start[b + 1] = start[b] + (rand() % 100 < live ? rand() % (rand() % 4 ? 3 : 300) : 0);
+        const int rows = start[seqs] + (rand() % 2 ? rand() % 50 : 0);
+        const long places = prompt_max_tiles(rows, seqs, G, tile);
+        CHECK(places <= (long)rows * G / tile + seqs && places <= (long)rows * G / tile + rows);
+        // every tile has a place below the bound, and no two have the same
+        std::vector<int> b_of(places, -1), t_of(places, -1);
+        for (int b = 0, before = 0; b < seqs; ++b) {
+            const int at = prompt_place(start[b], b, G, tile);
+            CHECK(at >= before);
+            before = at;
+            for (int t = 0; t < prompt_tiles(start[b + 1] - start[b], G, tile); ++t) {
+                CHECK(at + t < places && b_of[at + t] < 0);
+                b_of[at + t] = b;
+                t_of[at + t] = t;
+            }
+        }
+        // and is found as the last sequence that begins at or before it
+        for (long i = 0; i < places; ++i) {
+            int b = -1;
+            for (int c = 0; c < seqs; ++c)
+                if (prompt_place(start[c], c, G, tile) <= i) b = c;
+            const int t = b < 0 ? -1 : (int)i - prompt_place(start[b], b, G, tile);
+            const bool there = b >= 0 && t < prompt_tiles(start[b + 1] - start[b], G, tile);
+            CHECK(there == (b_of[i] >= 0) && (!there || (b == b_of[i] && t == t_of[i])));
+        }
+    }
+    CHECK(prompt_max_tiles(8, 100000, 4, 128) == 8 && prompt_max_tiles(0, 100000, 4, 128) == 0);
+    puts("ok");
+}
+"""
+
+
+def test_places_of_sequences_with_rows(tmp_path):
+    """Sequences without rows take no places: the bound is that of the rows, and the search still finds every tile."""
+    (tmp_path / "main.cpp").write_text(_PLACES)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-fsanitize=undefined,address", "-fno-sanitize-recover=all", "-I", CSRC, str(tmp_path / "main.cpp"), "-o",
+                    str(tmp_path / "main")], check=True)
+    r = subprocess.run([str(tmp_path / "main")], capture_output=True, text=True)
+    assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout + r.stderr

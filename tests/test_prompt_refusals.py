@@ -115,3 +115,15 @@ def test_parts_of_a_row_fit_the_join(n_top):
             assert sjd.lib().sjd_op_token_logprobs_workspace(rows, vocab, n_top, C.byref(b)) == sjd.OK
             parts = b.value // rows // (16 + 8 * n_top)
             assert b.value == rows * parts * (16 + 8 * n_top) and parts * n_top <= 1024
+
+
+@pytest.mark.parametrize("dtype", [sjd.BF16, sjd.F32])
+@pytest.mark.parametrize("rows", [1, 8, 40])
+@pytest.mark.parametrize("max_kv", [3000, 30000, 100000])
+def test_slots_without_rows_need_no_workspace(dtype, rows, max_kv):
+    """A batch of any number of slots has at most `rows` sequences with rows: its workspace is what so many sequences need, and the call is not refused for its slots."""
+    sizes = dict(dtype=dtype, n=rows, H=32, Hk=8, hd=128, max_rows=rows, max_kv=max_kv)
+    rc, alone = need(**sizes, seqs=rows)
+    assert rc == sjd.OK and alone > 0
+    for seqs in (64, 65, 500, 4096, 1 << 20, 1 << 30):
+        assert need(**sizes, seqs=seqs) == (sjd.OK, alone), seqs
