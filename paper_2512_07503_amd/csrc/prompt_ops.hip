@@ -43,13 +43,16 @@ int prompt_resident(int size, int hd) {
 // each time that all places are taken; several splits are written, read, and joined by a launch more.
 // (Its numbers are those that come nearest to what 1 to 96 ways took for 37 shapes of both types, from one row behind 3 000 keys and 16 behind 100 000 to 16 001 over themselves: its choice is the best
 // for 24 of them, and at most 13 % slower than that.  Three times as many workgroups as there are places took 82 % more at 4 x 300 rows behind 700, no splits 27 times as long at 16 behind 100 000.)
+// No more of them than workgroups for kPromptRounds times the places: then the last ones' part, which is all that splits take off, is at most 1 / kPromptRounds, and the workspace does not grow without
+// bound with what max_kv expects (fp32, 2^20 rows of 16 heads behind as many keys: 49 GiB of partial results for 0.4 % of the time), nor the launch beyond what one holds.
+constexpr size_t kPromptRounds = 32;
 int prompt_n_splits(int size, int hd, long rows, size_t work, size_t blocks) {
     const double keys = prompt_block(size, hd) / 32 * (size == 4 ? hd / 64.0 : hd / 128.0), alone = (size == 4 ? 4.7 : 0.84) * keys, each = (size == 4 ? 1.6 : 0.54) * keys;
     const size_t cus = 256, slots = cus * prompt_resident(size, hd);
     if (size == 2 && work >= slots) return 1;
     double best = 0;
     int n = 1;
-    for (size_t s = 1; s <= blocks && s <= 256; s += s < 4 ? 1 : s & (s - 1) ? s / 3 : s / 2) {       // 1, 2, 3, 4, 6, 8, 12 ..
+    for (size_t s = 1; s <= blocks && s <= 256 && (s == 1 || work * s <= kPromptRounds * slots); s += s < 4 ? 1 : s & (s - 1) ? s / 3 : s / 2) {       // 1, 2, 3, 4, 6, 8, 12 ..
         const size_t per = ceil_div_sz(blocks, s), splits = ceil_div_sz(blocks, per), rounds = ceil_div_sz(work * splits, slots);
         const double shared = each * ceil_div_sz(work * splits, cus);
         const double us = (rounds <= 1 ? per * (shared > alone ? shared : alone) : 0.71 * each * work * blocks / cus + 0.67 * per * each * slots / cus) + 5.5 * rounds +
@@ -84,8 +87,6 @@ int check_prompt(int32_t dtype, int32_t n_rows, int32_t n_seqs, int32_t n_heads,
     const long G = n_heads / n_kv;
     if (n_rows * G > 1l << 30 || prompt_max_tiles(n_rows, n_seqs, (int)G, 32 * kPromptWaves) * n_kv > (long)kMaxWorkgroups) TREE_FAIL(SJD_EINVAL, "too many rows for one launch");
     p = prompt_plan(dtype, n_rows, n_seqs, n_heads, n_kv, hd, max_kv);
-    if ((size_t)p.tiles * n_kv * p.n_splits > kMaxWorkgroups || (p.n_splits > 1 && (size_t)p.tiles * n_kv * (hd / 2) > kMaxWorkgroups))
-        TREE_FAIL(SJD_EINVAL, "too many rows for one launch");
     return SJD_OK;
 }
 

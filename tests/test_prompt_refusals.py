@@ -127,3 +127,15 @@ def test_slots_without_rows_need_no_workspace(dtype, rows, max_kv):
     assert rc == sjd.OK and alone > 0
     for seqs in (64, 65, 500, 4096, 1 << 20, 1 << 30):
         assert need(**sizes, seqs=seqs) == (sjd.OK, alone), seqs
+
+
+def test_expected_keys_refuse_no_call():
+    """max_kv only chooses how the work is divided: a call that is accepted without splits is accepted whatever it says, with a workspace of at most 32 times the places' partial
+    results (1 280 workgroups of 128 rows), and of a few rows with more keys than are split one by one."""
+    for dtype, n, H, Hk, hd in [(sjd.F32, 1 << 20, 16, 4, 128), (sjd.F32, 1 << 22, 16, 4, 128), (sjd.F32, 1 << 22, 16, 16, 64), (sjd.F32, 1 << 20, 64, 1, 256), (sjd.F32, 100000, 8, 8, 32),
+                                (sjd.BF16, 1 << 22, 16, 4, 128), (sjd.F32, 1, 8, 1, 128)]:
+        for seqs in (1, 300):
+            assert need(dtype=dtype, n=n, seqs=seqs, H=H, Hk=Hk, hd=hd, max_rows=0, max_kv=0) == (sjd.OK, 0)
+            for max_kv in (1 << 16, 1 << 20, 1 << 30):
+                rc, bytes_ = need(dtype=dtype, n=n, seqs=seqs, H=H, Hk=Hk, hd=hd, max_rows=n, max_kv=max_kv)
+                assert rc == sjd.OK and bytes_ <= 32 * 1280 * 128 * (hd + 2) * 4, (n, max_kv)
