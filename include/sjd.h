@@ -480,7 +480,7 @@ int sjd_op_prompt_attention(void *hip_stream, int32_t dtype, const void *q, int6
  *   top_ids, top_logprobs [n_rows][n_top]: the likeliest ids, the lower one first where they are as likely, and their ln p; -1 and -inf behind the last id whose logit
  *   is above -inf.
  * Logits may be -inf (masked ids); of a row that is -inf altogether every ln p is -inf and the entropy is 0.  A row that holds a NaN or +inf has NaN for its numbers, -1 for
- * its top_ids, and no meaning in its rank.  Sums are fp32.  n_top 0 .. 64 (0: top_ids and top_logprobs may be NULL); vocab <= 2^24.  Outputs may not overlap each
+ * its top_ids, and no meaning in its rank.  Sums are fp32; no ln p is above 0.  n_top 0 .. 64 (0: top_ids and top_logprobs may be NULL); vocab <= 2^24.  Outputs may not overlap each
  * other or an input.  Workspace as in sjd_op_prompt_attention. */
 int sjd_op_token_logprobs_workspace(int32_t n_rows, int32_t vocab, int32_t n_top, uint64_t *bytes);
 int sjd_op_token_logprobs(void *hip_stream, int32_t dtype, const void *logits, int64_t stride, const int32_t *tokens, float *logprob, int32_t *rank, float *entropy,

@@ -159,7 +159,8 @@ template <typename Key> SJD_D void logprob_finish(const LogprobArgs &a, size_t r
     // NaN and +inf among the logits make s NaN
     const bool bad = r.s != r.s;
     const float log2_s = __builtin_amdgcn_logf(r.s), ln_s = kLn2 * log2_s;
-    auto of = [&](float z) { return bad ? __builtin_nanf("") : z == -INFINITY ? -INFINITY : (z - r.m) - ln_s; };
+    // (s may have been rounded below the term of the row's only likely id: no logarithm of a probability is above 0)
+    auto of = [&](float z) { return bad ? __builtin_nanf("") : z == -INFINITY ? -INFINITY : fminf((z - r.m) - ln_s, 0.0f); };
     if (first == 0) {
         a.logprob[row] = of(z_token);
         a.rank[row] = r.rank;
@@ -202,7 +203,8 @@ SJD_D void logprob_step(LogprobState &st, const float (&z)[16], Id id, uint32_t 
     float top = logprob_max(z[0], z[1]);
 #pragma unroll
     for (int e = 2; e < 16; e += 2) top = logprob_max3(top, z[e], z[e + 1]);
-    // The reference is the largest logit of a lane, but for 8: it moves where it is exceeded by more (exponentials of up to 2^11.6 cost the sums nothing).
+    // The reference is the largest logit of a lane, but for 8: it moves where it is exceeded by more (exponentials of up to 2^11.6 cost the sums
+    // nothing; the logarithm of one id that has nearly all the weight, a difference of two numbers of up to 8 then, is up to 1e-6 off).
     if (__ballot(top > st.m + kLogprobSlack)) {
         const float m = top > st.m + kLogprobSlack ? top : st.m;
         const bool far = fabsf(m) >= kLogprobFar && m > -INFINITY;

@@ -177,3 +177,23 @@ def test_workspace():
     with pytest.raises(sjd.SjdError) as e:
         sjd.op_token_logprobs(z, tokens, n_top=9, workspace=guard[:need - 16])
     assert e.value.code == sjd.ECAPACITY
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [40, 5003, 70001])
+def test_nothing_is_above_zero(dtype, vocab):
+    """Rows of which one id has all the weight, alone or beside ids that are far below or follow at once: ln p is at most 0, as p is at most 1."""
+    rng = np.random.default_rng(vocab)
+    z = np.full((120, vocab), -np.inf)
+    tokens = rng.integers(0, vocab, 120)
+    z[40:80] = 2.5 * rng.standard_normal((40, vocab)) - 60.0
+    z[np.arange(120), tokens] = 30.0 * rng.standard_normal(120)
+    z[80:, 0] = np.where(tokens[80:] == 0, z[80:, 0], z[np.arange(80, 120), tokens[80:]] - rng.uniform(1.0, 8.0, 40))
+    z, tokens = tensors(z, tokens, dtype)
+    for n_top in (0, 3):
+        got = check(z, tokens, n_top)
+        assert got[0].max() <= 0 and (not n_top or got[4].max() <= 0) and got[2].min() >= 0
+    # (many rows, of which none is split)
+    import paper_2512_07503_amd as sjd
+    got = sjd.op_token_logprobs(z.repeat(20, 1), tokens.repeat(20), n_top=2)
+    assert got[0].max().item() <= 0 and got[4].max().item() <= 0
