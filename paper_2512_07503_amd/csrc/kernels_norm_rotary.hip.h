@@ -18,9 +18,11 @@ struct NormRotaryArgs {
 };
 
 // The normalised x in its place: z = (x - c) / sqrt(mean((x - c)^2) + eps), of a lane's elements (0 where it has none: bit e of `has`; FULL: it has all).
-// With means: c rounded is 2^-24 of it off, which may be many times the deviation, so what it leaves, the mean of the differences from it, is taken off as well.
+// With means: c rounded is 2^-24 of it off, which may be many times the deviation, so what it leaves, the mean of the differences from it, is taken off as well: in the same multiplication as the
+// scale, unless that mean is most of the differences (heads of nearly one value), of which their spread would be what roundings leave.  Then it is taken off them first, divided without an
+// error where it can be: a head of one value is 0 about its mean.
 // Squares of elements beyond 2^60 do not fit: then they are taken 2^-72 times as large (the norm does not change, but for eps, which is far below).
-template <int N, int TEAM, bool LAYER, bool FULL> SJD_D float norm_moments(float (&x)[N], uint32_t has, float inv, float &off) {
+template <int N, int TEAM, bool LAYER, bool FULL> SJD_D float norm_moments(float (&x)[N], uint32_t has, float n, float inv, float &off) {
     off = 0.0f;
     float first[2] = {0.0f, 0.0f}, second[2] = {0.0f, 0.0f};      // (two chains of additions each)
     if constexpr (LAYER) {
@@ -39,21 +41,34 @@ template <int N, int TEAM, bool LAYER, bool FULL> SJD_D float norm_moments(float
     for (int e = 0; e < N; ++e) second[e & 1] = fmaf(x[e], x[e], second[e & 1]);
     const float var = lanes_sum<TEAM>(second[0] + second[1]) * inv;
     if constexpr (!LAYER) return var;
-    off = lanes_sum<TEAM>(first[0] + first[1]) * inv;
-    const float less = var - off * off;
+    const float sum = lanes_sum<TEAM>(first[0] + first[1]);
+    off = sum * inv;
+    float less = var - off * off;
+    if (less < 0.25f * var) {            // (the same in all of the team)
+        off = fmaf(fmaf(-off, n, sum), inv, off);
+        first[0] = first[1] = second[0] = second[1] = 0.0f;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            x[e] = FULL || (has >> e & 1u) ? x[e] - off : 0.0f;
+            first[e & 1] += x[e];
+            second[e & 1] = fmaf(x[e], x[e], second[e & 1]);
+        }
+        off = lanes_sum<TEAM>(first[0] + first[1]) * inv;
+        less = lanes_sum<TEAM>(second[0] + second[1]) * inv - off * off;
+    }
     return less < 0.0f ? 0.0f : less;
 }
 template <int N, int TEAM, bool LAYER, bool FULL> SJD_D void normalise(float (&x)[N], uint32_t has, int hd, float eps) {
-    const float inv = 1.0f / (float)hd;
+    const float n = (float)hd, inv = 1.0f / n;
     float y[N], off;
     if constexpr (LAYER)
 #pragma unroll
         for (int e = 0; e < N; ++e) y[e] = x[e];
-    float var = norm_moments<N, TEAM, LAYER, FULL>(x, has, inv, off);
+    float var = norm_moments<N, TEAM, LAYER, FULL>(x, has, n, inv, off);
     if (!(var < INFINITY)) {
 #pragma unroll
         for (int e = 0; e < N; ++e) x[e] = (LAYER ? y[e] : x[e]) * 0x1p-72f;
-        var = norm_moments<N, TEAM, LAYER, FULL>(x, has, inv, off);
+        var = norm_moments<N, TEAM, LAYER, FULL>(x, has, n, inv, off);
         eps = 0x1p-126f;
     }
     const float scale = __builtin_amdgcn_rsqf(var + eps), less = -off * scale;     // (within 2^-23; the argument is at least 1e-30)

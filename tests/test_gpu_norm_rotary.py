@@ -152,3 +152,19 @@ def test_is_the_norm_and_op_rotary():
     a, _ = sjd.op_rotary(q, None, pos, table)
     b, _ = sjd.op_norm_rotary(q, None, pos, table, torch.ones(128, device="cuda"), eps=1e-30)
     assert (a - b).abs().max().item() <= 8 * 2.0 ** -24      # a root and a quotient of 1, a step each, before the turn; sums of two
+
+
+@pytest.mark.parametrize("hd", [50, 64, 80, 96, 160, 240, 504])
+@pytest.mark.parametrize("eps", [1e-5, 1e-30])
+def test_heads_of_one_value(hd, eps):
+    """Whatever rounding their mean leaves, heads of one value are 0 about it, also where eps is far below it; and heads of which one element is a step larger are what they are in 64 bits."""
+    import paper_2512_07503_amd as sjd
+    import torch
+    rng = np.random.default_rng(hd)
+    x = (rng.uniform(1.0, 2.0, (1000, 4, 1)) * 10.0 ** rng.integers(-3, 38, (1000, 4, 1)) * np.ones(hd)).astype(np.float32)
+    x[700:, :, hd // 3] = np.nextafter(x[700:, :, hd // 3], np.float32(np.inf))
+    t, gain, r = tensor(x, "f32"), tensor(np.ones(hd), "f32"), 2 * (hd // 4)
+    zero = torch.zeros(1000, dtype=torch.int32, device="cuda")
+    got, _ = sjd.op_norm_rotary(t, None, zero, sjd.rope_table(r), gain, norm="layer", eps=eps)
+    assert (got[:700] == 0).all()
+    check(got, t, gain, None, True, eps, np.zeros(1000, dtype=np.int64), tree_oracle.frequencies(r), False, 1.0, "f32")
