@@ -287,9 +287,14 @@ template <int HD> struct PromptState {
 // Probabilities are 2^(score - m).  A rescaling puts m 8 above the row's maximum, a whole number (it is exact), and the next one comes when the maximum has grown
 // beyond m: until then the largest probability is between 2^-9 and 1, so rescalings are rare, and no sum of products with finite values overflows that does not in
 // the formula.
-constexpr float kPromptAhead = 8.0f;
-template <int HD> SJD_D void prompt_rescale(PromptState<HD> &st, float mx) {
-    const float m = mx > st.m ? __builtin_ceilf(mx) + kPromptAhead : st.m;
+// From magnitudes of 2^24 on m, a float, may be far off the maximum, whose exponent is exact (score * scale_log2e, in one instruction with the difference).  There m is the next float at or below it, and exponents
+// above 0, which are smaller than a rounding of the scores, are 0: the largest score has the weight 1, those of its rounding too, and whatever is below it less.
+constexpr float kPromptAhead = 8.0f, kPromptFar = 0x1p24f;
+template <int HD> SJD_D void prompt_rescale(PromptState<HD> &st, float score, float scale_log2e) {
+    const float mx = score * scale_log2e;
+    float ahead = __builtin_ceilf(mx) + kPromptAhead;
+    if (fabsf(mx) >= kPromptFar) ahead = fmaf(score, scale_log2e, -mx) < 0.0f ? __builtin_bit_cast(float, __builtin_bit_cast(int, mx) + (mx < 0.0f ? 1 : -1)) : mx;
+    const float m = mx > st.m ? ahead : st.m;
     const float alpha = __builtin_amdgcn_exp2f(st.m - (m == -INFINITY ? 0.0f : m));     // (not (-inf) - (-inf))
     st.m = m;
     st.l *= alpha;
@@ -300,6 +305,9 @@ template <int HD> SJD_D void prompt_rescale(PromptState<HD> &st, float mx) {
         __builtin_amdgcn_sched_barrier(0);
     }
 }
+
+// An exponent after a rescaling: at most 0 (NaN stays)
+SJD_D float prompt_exponent(float score, float scale_log2e, float m) { return __builtin_elementwise_minimum(fmaf(score, scale_log2e, -m), 0.0f); }
 
 // the larger of a lane's and its partner's in the other half
 SJD_D float prompt_both_halves(float x) {
@@ -383,12 +391,12 @@ template <int HD> struct PromptWave32 {
         float mx = s[0];
 #pragma unroll
         for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
-        mx = prompt_both_halves(mx) * scale_log2e;
-        if (__ballot(mx > st.m)) prompt_rescale<HD>(st, mx);
+        mx = prompt_both_halves(mx);
+        if (__ballot(mx * scale_log2e > st.m)) prompt_rescale<HD>(st, mx, scale_log2e);
         const float m = st.m == -INFINITY ? 0.0f : st.m;        // a row that has seen nothing so far: not (-inf) - (-inf)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], scale_log2e, -m));
+            s[e] = __builtin_amdgcn_exp2f(prompt_exponent(s[e], scale_log2e, m));
             st.l += s[e];
         }
 #pragma unroll
@@ -494,30 +502,31 @@ template <int HD> struct PromptWave16 {
         for (int i = 0; i < HALVES; ++i)
 #pragma unroll
             for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[i][e]);
-        prompt_rescale<HD>(st, prompt_both_halves(mx) * scale_log2e);
+        prompt_rescale<HD>(st, prompt_both_halves(mx), scale_log2e);
         m = st.m == -INFINITY ? 0.0f : st.m;           // a row that has seen nothing: not (-inf) - (-inf)
         unset = st.m == -INFINITY ? unset : 0.0f;
     }
     // probabilities 2 n and 2 n + 1; those of n - 1 as operands.  What the products take is what the sum adds, so that a row's weights add up to 1 whatever their rounding to bf16 (a row
-    // that sees one key gives its value, exactly).
-    template <int I> SJD_D void weigh(int n, float scale_log2e) {
+    // that sees one key gives its value, exactly).  SETTLED: after a rescaling.
+    template <bool SETTLED, int I> SJD_D void weigh(int n, float scale_log2e) {
         if (n > 0) {
             const uint32_t both = pack_bf16(e0, e1);
             p[I][(n - 1) / 4][(n - 1) % 4] = both;
             sum = prompt_add_pair(sum, both);
         }
         if (n < 8) {
-            e0 = __builtin_amdgcn_exp2f(fmaf(s[I][2 * n], scale_log2e, -m));
-            e1 = __builtin_amdgcn_exp2f(fmaf(s[I][2 * n + 1], scale_log2e, -m));
+            auto exponent = [&](float x) { return SETTLED ? prompt_exponent(x, scale_log2e, m) : fmaf(x, scale_log2e, -m); };
+            e0 = __builtin_amdgcn_exp2f(exponent(s[I][2 * n]));
+            e1 = __builtin_amdgcn_exp2f(exponent(s[I][2 * n + 1]));
         }
     }
-    SJD_D void weigh_all(float scale_log2e, float from) {
+    template <bool SETTLED> SJD_D void weigh_all(float scale_log2e, float from) {
         sum = from;
 #pragma unroll
-        for (int n = 0; n < 9; ++n) weigh<0>(n, scale_log2e);
+        for (int n = 0; n < 9; ++n) weigh<SETTLED, 0>(n, scale_log2e);
         if constexpr (HALVES == 2)
 #pragma unroll
-            for (int n = 0; n < 9; ++n) weigh<1>(n, scale_log2e);
+            for (int n = 0; n < 9; ++n) weigh<SETTLED, 1>(n, scale_log2e);
     }
     SJD_D void product(int n) {
         st.o[n % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[n % HELD]), __builtin_bit_cast(bf16x8, p[n / (2 * DB)][n / DB % 2]), st.o[n % DB], 0, 0, 0);
@@ -556,10 +565,10 @@ template <int HD> struct PromptWave16 {
         prompt_spread<AHEAD, 0>([&](int n) { score(NK - AHEAD + n); }, [&](int) {});
         priority<0>();
         if (masked) mask(last);
-        weigh_all(scale_log2e, unset);
+        weigh_all<false>(scale_log2e, unset);
         if (__ballot(!(sum <= 1.0f))) {
             settle(scale_log2e);
-            weigh_all(scale_log2e, 0.0f);
+            weigh_all<true>(scale_log2e, 0.0f);
         }
         st.l += sum;
 #pragma unroll

@@ -351,3 +351,27 @@ def test_slots_without_rows_do_not_change_the_division(n_seqs):
     c = Case("bf16", 8, 2, 128, n, t, seed=25)
     c.check(c.run())
     assert sjd.binding._prompt_bytes(sjd.BF16, 5, n_seqs, 8, 2, 128, 3, 3000) > 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hd", [64, 128, 256])
+def test_scores_that_are_far_from_zero(dtype, hd):
+    """Scores q_0 k_0 of up to 2^127 in magnitude, exact in fp32 and at least 2^20 apart where they are not equal: a row is the mean of the values whose keys have its largest one.  Their
+    weights are the same number, so a sum of T is (T + 16) 2^-24 of sum p |v| off, the quotient 2^-22, and the result is rounded."""
+    import torch
+    rng = np.random.default_rng(26)
+    for top, scale in ((20, np.log(2.0)), (24, None), (28, 0.7), (33, None), (60, None), (119, np.log(2.0))):
+        for sign in (1.0, -1.0):
+            def edit(c):
+                c.q.zero_()
+                c.q[:, :, 0] = sign * 2.0 ** top
+                c.k[:, :, 0] = torch.from_numpy(rng.integers(1, 200, (len(c.k), c.Hkv)).astype(np.float32)).cuda().to(c.k.dtype)
+            for n, t, max_kv in (([150, 1, 40], None, 150), ([5, 40], [2300, 90], 2300), ([5, 40], [2300, 90], 64)):
+                c = Case(dtype, 4, 2, hd, n, t, seed=27, edit=edit)
+                got = host(c.run(max_kv=max_kv, scale=float(scale or 0.0)))
+                assert np.isfinite(got).all(), (top, sign, n)
+                for b in range(len(n)):
+                    rows, keys = slice(c.at[b], c.at[b + 1]), slice(c.kat[b], c.kat[b + 1])
+                    want, size, _ = prompt_oracle.attention(host(c.q[rows]), host(c.k[keys]), host(c.v[keys]), scale or hd ** -0.5)
+                    tol = ((c.t[b] + 16) * 2.0 ** -24 + 2.0 ** -22) * size + (2.0 ** -24 if dtype == "f32" else 2.0 ** -8) * np.abs(want) * (1 + 2.0 ** -7)
+                    assert (np.abs(got[rows] - want) <= tol).all(), (top, sign, n, np.abs(got[rows] - want).max())
