@@ -149,11 +149,15 @@ typedef const __attribute__((address_space(1))) void prompt_glb_t;
 typedef short prompt_s16x4 __attribute__((ext_vector_type(4)));
 
 // 16 bytes of each lane, `off` from base, to LDS, the lanes' one behind the other.  In the compiler's own form every read of what it cannot tell from the target would wait for the load, the reads
-// of another buffer of the same array among them; here prompt_barrier is what waits.  (M0 is nobody's: the compiler sets it wherever it needs it.)
+// of another buffer of the same array among them; here prompt_barrier is what waits.  M0 is named as written, so that the compiler sets it again where it needs it behind this (it warns that it
+// does not keep a reserved register, which is what is meant).
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 SJD_D void prompt_to_lds(const char *base, uint32_t off, unsigned char *lds) {
     const uint32_t to = (uint32_t)(uintptr_t)(prompt_lds_t *)lds;
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off), "s"(base) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 
 // Keys or values of a block on their way to LDS.  WIDE: rows are 16-byte aligned and go there without passing through registers.  Tokens behind the last are
 // copies of the last one: nobody sees them.
