@@ -24,6 +24,8 @@ constexpr int prompt_keys(int t, int n, int n_keys, int G, int tile) {
     const int seen = i + 1 + prompt_offset(n, n_keys);
     return seen < 0 ? 0 : seen;
 }
+// Workgroups that a CU holds at a time, by the registers and the LDS of the kernel for aligned rows (size: bytes of an element)
+constexpr int prompt_resident(int size, int hd) { return size == 2 ? hd <= 64 ? 4 : hd <= 128 ? 3 : 2 : hd <= 32 ? 5 : hd <= 64 ? 4 : hd <= 96 ? 3 : hd <= 128 ? 2 : 1; }
 // How many splits there are of a tile whose rows see n_keys_seen keys, of at most n_splits, of `per` blocks each (the last of all takes what is left)
 constexpr int prompt_splits(int n_keys_seen, int block, int n_splits, int per) {
     const int blocks = (n_keys_seen + block - 1) / block, want = (blocks + per - 1) / per;

@@ -32,11 +32,6 @@ template <typename T> void run_norm_rotary_type(hipStream_t st, dim3 grid, int t
 // ------------------------------------------------------------------------------------------------------------- attention
 struct PromptPlan { int tiles, n_splits, per_split; size_t part_o, part_ml; };
 
-// Workgroups that a CU holds at a time, by their registers and LDS
-int prompt_resident(int size, int hd) {
-    if (size == 2) return hd <= 32 ? 5 : hd <= 64 ? 4 : hd <= 128 ? 3 : 2;
-    return hd <= 32 ? 5 : hd <= 64 ? 4 : hd <= 96 ? 3 : hd <= 128 ? 2 : 1;
-}
 // How many ways the keys of a tile are split: in bf16 not at all where there is a workgroup for every place without (what is split is written and read once more); else from an estimate of what that
 // takes, in us.  A block takes `alone`, and `each` of every workgroup of the CU where that is more.  If all workgroups have their places at once, a split's blocks take that, one behind the other; if
 // not, all blocks keep all CUs busy (71 % of them, as sequences differ, and causal prompts see half of their own rows), and the last splits a part of them.  5.5 us are a workgroup's beginning and end,
