@@ -464,8 +464,8 @@ int sjd_op_norm_rotary(void *hip_stream, int32_t dtype, int32_t norm, float eps,
  * q and out [n_rows][n_heads][head_dim], k and v [n_kv_rows][n_kv_heads][head_dim] of `dtype` (SJD_F32 or SJD_BF16; a row's heads are contiguous, rows a stride
  * apart: parts of a fused projection); head_dim 32, 64, 96, 128, 192 or 256.  Sums are fp32; for SJD_BF16 probabilities are rounded to bf16 for the products
  * with values and for the sum that divides.  out may be q with the same stride, and may not overlap it otherwise, nor k and v.  scale > 0, or 0 for 1 / sqrt(head_dim).
- * max_rows, max_kv: what a sequence's queries and keys are expected to reach; they only choose how the work is divided, and with it the order of
- * sums.  Workspace (16-byte aligned): the bytes that sjd_op_prompt_attention_workspace writes to *bytes (HOST; may be 0) for the same
+ * max_kv: what a sequence's keys are expected to reach; it only chooses how the work is divided, and with it the order of sums and the workspace.  max_rows, the same of its
+ * queries, is checked, and changes nothing.  Workspace (16-byte aligned): the bytes that sjd_op_prompt_attention_workspace writes to *bytes (HOST; may be 0) for the same
  * arguments.  SJD_ECAPACITY: it is smaller. */
 int sjd_op_prompt_attention_workspace(int32_t dtype, int32_t n_rows, int32_t n_seqs, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_rows,
                                       int32_t max_kv, uint64_t *bytes);

@@ -692,8 +692,8 @@ def _prompt_bytes(*sizes):
 def op_prompt_attention(q, k, v, row_start, kv_start=None, max_rows=None, max_kv=None, scale=0.0, out=None, workspace=None):
     """Causal attention of packed prompts: q [rows, heads, head_dim], k and v [kv_rows, kv_heads, head_dim] (rows may be strided).  Sequence b's queries are rows
     row_start[b] .. row_start[b + 1] - 1, its keys rows kv_start[b] .. (the same rows without a kv_start), the last of which are its queries' own: query i of n sees the
-    first i + 1 + t - n of t keys.  row_start, kv_start int32 [n_seqs + 1].  max_rows, max_kv: what a sequence's queries and keys are expected to reach (default: all rows); they
-    only choose how the work is divided.  -> out like q; rows of no sequence are not written."""
+    first i + 1 + t - n of t keys.  row_start, kv_start int32 [n_seqs + 1].  max_kv: what a sequence's keys are expected to reach (default: all rows; say it where
+    sequences are much shorter than all of them together); it only chooses how the work is divided.  max_rows, the same of its queries, changes nothing.  -> out like q; rows of no sequence are not written."""
     import torch
     device = _device_of(q, k, v, row_start, kv_start, out, workspace)
     code, shape = _row_code(q, "q"), q.shape
@@ -715,7 +715,7 @@ def op_prompt_attention(q, k, v, row_start, kv_start=None, max_rows=None, max_kv
         max_rows = rows
     if max_kv is None:
         max_kv = kv_rows
-    at, size, keep = _workspace(workspace, _prompt_bytes(code, rows, seqs, heads, kv_heads, hd, max_rows, max_kv), q)
+    at, size, keep = _workspace(workspace, _prompt_bytes(code, rows, seqs, heads, kv_heads, hd, 0, max_kv), q)      # (max_rows does not change it)
     _enqueue(device, lib().sjd_op_prompt_attention, code, q.data_ptr(), strides[0], k.data_ptr(), strides[1], v.data_ptr(), strides[2], out.data_ptr(), out_stride,
              _vector(row_start, seqs + 1, torch.int32, "row_start"), None if kv_start is None else _vector(kv_start, seqs + 1, torch.int32, "kv_start"), rows, kv_rows, seqs,
              heads, kv_heads, hd, scale, max_rows, max_kv, at, size)

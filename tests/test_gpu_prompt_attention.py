@@ -375,3 +375,17 @@ def test_scores_that_are_far_from_zero(dtype, hd):
                     want, size, _ = prompt_oracle.attention(host(c.q[rows]), host(c.k[keys]), host(c.v[keys]), scale or hd ** -0.5)
                     tol = ((c.t[b] + 16) * 2.0 ** -24 + 2.0 ** -22) * size + (2.0 ** -24 if dtype == "f32" else 2.0 ** -8) * np.abs(want) * (1 + 2.0 ** -7)
                     assert (np.abs(got[rows] - want) <= tol).all(), (top, sign, n, np.abs(got[rows] - want).max())
+
+
+def test_max_rows_changes_nothing():
+    """Neither the bits nor the workspace, whose size is asked for once."""
+    import paper_2512_07503_amd as sjd
+    c = Case("bf16", 8, 2, 64, [5, 3], [3000, 1000], seed=28)
+    first = c.run().clone()
+    misses = sjd.binding._prompt_bytes.cache_info().misses
+    for max_rows in (0, 1, 7, 100000):
+        assert (c.run(max_rows=max_rows) == first).all()
+    assert sjd.binding._prompt_bytes.cache_info().misses == misses
+    for max_rows in (-1, (1 << 29) + 1):
+        with pytest.raises(sjd.SjdError):
+            c.run(max_rows=max_rows)

@@ -139,3 +139,8 @@ def test_expected_keys_refuse_no_call():
             for max_kv in (1 << 16, 1 << 20, 1 << 30):
                 rc, bytes_ = need(dtype=dtype, n=n, seqs=seqs, H=H, Hk=Hk, hd=hd, max_rows=n, max_kv=max_kv)
                 assert rc == sjd.OK and bytes_ <= 32 * 1280 * 128 * (hd + 2) * 4, (n, max_kv)
+
+
+def test_max_rows_needs_no_workspace():
+    for max_kv in (20, 3000, 1 << 20):
+        assert len({need(H=32, Hk=8, hd=128, max_rows=m, max_kv=max_kv) for m in (0, 1, 10, 1 << 29)}) == 1
