@@ -389,3 +389,27 @@ def test_max_rows_changes_nothing():
     for max_rows in (-1, (1 << 29) + 1):
         with pytest.raises(sjd.SjdError):
             c.run(max_rows=max_rows)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_short_sequences_and_a_long_one(dtype):
+    rng = np.random.default_rng(15)
+    n = rng.integers(0, 4, 300).tolist()
+    n[170] = 90
+    c = Case(dtype, 2, 1, 32, n, seed=15)
+    c.check(c.run())
+    c = Case(dtype, 2, 1, 32, n, [m + int(x) for m, x in zip(n, rng.integers(0, 9, 300))], seed=16)
+    c.check(c.run())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n_seqs", [65, 1000, 70000])
+def test_few_rows_in_many_slots(dtype, n_seqs):
+    """A row here and there, ahead of everything, and in the last slot, behind keys that are split."""
+    n, t = [0] * n_seqs, [0] * n_seqs
+    for b, rows, keys in ((0, 1, 900), (1, 2, 0), (n_seqs // 2, 130, 2500), (n_seqs - 2, 3, 3000), (n_seqs - 1, 1, 1)):
+        n[b], t[b] = rows, keys
+    t[7] = 50                       # (keys that nobody asks about)
+    c = Case(dtype, 8, 2, 64, n, t, seed=29, lead=3, trail=2)
+    c.check(c.run())
+    c.check(c.run(max_kv=100))
