@@ -413,3 +413,22 @@ def test_few_rows_in_many_slots(dtype, n_seqs):
     c = Case(dtype, 8, 2, 64, n, t, seed=29, lead=3, trail=2)
     c.check(c.run())
     c.check(c.run(max_kv=100))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hd", [64, 128, 256])
+def test_many_scores_near_the_reference(dtype, hd):
+    """Scores (base 2) that rise by up to 8 behind the first block, for all keys from there on, for some rows of a tile more than for others, and fall again: the reference is moved by
+    whole numbers, and the weights before and behind it add up."""
+    import torch
+    rng = np.random.default_rng(30)
+
+    def edit(c):
+        c.q[..., 0] = torch.from_numpy(rng.integers(0, 3, c.q.shape[:2]).astype(np.float32)).cuda().to(c.q.dtype)
+        c.q[..., 1:] = 0
+        c.k[..., 0] = 0
+        for at, score in ((64, 2.5), (128, 3.5), (200, 4.0), (300, 1.0), (400, 7.0)):
+            c.k[at:, :, 0] = score
+    for n, t, max_kv in (([500, 90], None, 500), ([30], [500], 500), ([30], [500], 64)):
+        c = Case(dtype, 4, 2, hd, n, t, seed=31, edit=edit)
+        c.check(c.run(scale=float(np.log(2.0)), max_kv=max_kv), scale=float(np.log(2.0)))
