@@ -158,7 +158,8 @@ __global__ __launch_bounds__(256) void norm_rotary_kernel(NormRotaryArgs p) {
     }
 }
 
-// Any alignment and sizes: a wavefront a head, a lane has pairs lane + 64 n and elements behind the turned part 2 half + lane + 64 n.
+// Any alignment and sizes: a wavefront a head, a lane has pairs lane + 64 n and elements behind the turned part 2 half + lane + 64 n, each loaded by itself.  (bf16, rows of one element more than above: 12 002 of
+// 40 heads of 128 39 -> 133 us, 9 408 of 64 with means, gains and biases 56 -> 348; 12 002 of 40 heads of 80 with 32 dimensions turned 32 us, with 30 154.  fp32: 93 -> 164 and 115 -> 305.)
 template <typename T, bool LAYER>
 __global__ __launch_bounds__(256) void norm_rotary_any_kernel(NormRotaryArgs p) {
     const RotaryArgs &a = p.r;

@@ -9,8 +9,9 @@
 // What bounds it: matrix and vector units, and, before either is full, the card's power (bf16, 16 001 rows of 32 heads of 128 in 8 groups: 1 880 - 1 980 us, 1.06 - 1.12 PFLOP/s, where a large library
 // product reaches 1.22 - 1.4; matrix units busy for 58 % of the cycles, vector units for 47, at 1.5 - 1.7 GHz).  A block's 16 products of 32 rows are 512 cycles of a SIMD, its exponentials and what
 // belongs to them some 75 instructions, which other wavefronts' products hide; there are two to five of them a SIMD.  Short prompts pay for a tile's beginning and end, some 9 us with waiting, of
-// which the CU's other workgroups hide a part (12 prompts of 61 to 2 352 rows, 32 heads of 128: 248 - 259 us, 0.75 - 0.78 PFLOP/s; 38 % and 39 %).  fp32: the matrix units' own rate, 154
-// TFLOP/s (2 048 rows of 16 heads: 78 - 88 from heads of 64 on).
+// which the CU's other workgroups hide a part (12 prompts of 61 to 2 352 rows, 32 heads of 128: 248 - 259 us, 0.75 - 0.78 PFLOP/s; 38 % and 39 %).  With heads of 32 and 64 the products of
+// a block are fewer and its 75 instructions are not: 8 192 rows of 16 heads 520 - 540 and 780 - 818 TFLOP/s.  fp32: a block's chain from products to exponentials to products, which the CU's other
+// workgroups hide where there are some: of the matrix units' 154 TFLOP/s 118 - 127 over 8 192 rows of 16 heads of 64, 128 and 256, 78 - 88 over 2 048, which are one workgroup a CU.
 // Tried, and not here: workgroups of 8 wavefronts with four blocks in LDS (16 001 rows: the same; 12 prompts 3 % slower), parts of a block's products between another's exponentials in one wavefront (10 %
 // slower), 64 rows a wavefront (registers), workgroups that stay and take one tile after the other with the next one's keys on their way (12 prompts 12 % slower: shares fixed beforehand come out uneven,
 // and each block has more to keep track of), values on their way to registers before the exponentials (the same with heads of 128, 10 to 26 % slower with 64, 192 and 256).
@@ -36,8 +37,12 @@ struct PromptArgs {
 };
 
 constexpr int kPromptWaves = 4;
+// bf16: the products' operands have 16 bits, so probabilities are rounded to them, by 2^-8 of each at most; results are 1.9 - 2.3e-3 off (root mean square, relative; 120 to 16 001 rows of normal values),
+// where their own rounding alone is 1.6e-3.  op_tree_attention does the same.
+
 // Waves that the compiler leaves registers for, of a SIMD: two overlap one's products with the other's exponentials (fp32, 8 192 rows of 16 heads of 128 in 4 groups over themselves: 67 against 52 TFLOP/s);
-// with heads of 192 and 256 in fp32 the queries and the output alone fill what one may have.
+// with heads of 192 and 256 in fp32 the queries and the output alone fill what one may have.  (bf16 with heads of 256 takes all 256 registers and keeps 3 more in memory; with heads of 96 and 128, and
+// fp32 with 96, 43 to 47 scalars lie in lanes of a vector register.)
 constexpr int prompt_waves_per_simd(int size, int hd) { return size == 2 || hd <= 128 ? 2 : 1; }
 // Tokens of a block.  Of wide heads 32, which halves the scores, and with operands that are loaded as others are used up leaves room for a second wave or a third (bf16, as above, heads of 256: 1 120
 // against 435 TFLOP/s, 192: 1 104 against 811, 128: 999 against 979; heads of 64: 772 against 784).
@@ -159,7 +164,8 @@ SJD_D void prompt_to_lds(const char *base, uint32_t off, unsigned char *lds) {
 }
 #pragma clang diagnostic pop
 
-// Keys or values of a block on their way to LDS.  WIDE: rows are 16-byte aligned and go there without passing through registers.  Tokens behind the last are
+// Keys or values of a block on their way to LDS.  WIDE: rows are 16-byte aligned and go there without passing through registers.  (Element by element, rows of one element more: 8 192 rows of 16 heads of 64,
+// 128 and 256 in bf16 168 -> 225, 282 -> 418, 477 -> 661 us, 2 048 in fp32 108 -> 113, 198 -> 213, 441 -> 622.)  Tokens behind the last are
 // copies of the last one: nobody sees them.
 template <typename T, int HD, bool WIDE> struct PromptFetch {
     static constexpr int BLOCK = prompt_block(sizeof(T), HD), ROW = HD * sizeof(T), PIECES = BLOCK * ROW / 16, THREADS = kPromptWaves * 64, PER = PIECES / THREADS;

@@ -96,6 +96,7 @@ template <typename T, int HD> void run_prompt(hipStream_t st, const PromptArgs &
     }
     if (a.n_splits > 1) {
         const unsigned quads = (unsigned)((size_t)a.tiles * a.n_kv * (kPromptWaves * 32 * HD / 1024));
+        // (One wavefront a row, four: 4 splits 25.9 and 29.5 us the call, 5 in fp32 14.9 and 15.4, 8 101 and 104, 12 427 and 435, 16 in fp32 123 and 125, 32 15.5 and 13.3, 63 31.4 and 27.4.)
         if (a.n_splits > 8) prompt_join_kernel<T, HD, 4><<<4 * quads, 256, 0, st>>>(a);
         else prompt_join_kernel<T, HD, 1><<<quads, 256, 0, st>>>(a);
     }
@@ -114,8 +115,16 @@ template <typename T> void run_prompt_type(hipStream_t st, int hd, const PromptA
 // ------------------------------------------------------------------------------------------------------ log probabilities
 // How many workgroups a row is split over: as many as the card holds at once, four a CU, but none with less than one step a wavefront, and no more than one joining workgroup holds.
 // (512, 768, 1024, 2048 workgroups: 256 rows of 65 536 with 20 ids 30.7, 30.7, 28.7, 37.8 us, 33 masked rows of 184 621 25.3, 21.9, 20.3, 22.0.)
-// Up to four steps a wavefront a row is not split: the launch that joins takes longer, or, where it does not, costs the host more than it saves (8 rows, in a graph and call by call: 8 192 with 5 ids
-// 9.5 and 12.8 us, split 10.5 and 16.7; 16 384 without ids 7.0 and 12.5, 7.1 and 16.6, with 5 13.2 and 13.3, 10.4 and 17.1; 65 536 with 5 33.4 and 33.6, 11.1 and 16.8).
+// Up to four steps a wavefront a row is not split: up to three (12 000) the launch that joins takes longer, in a graph and call by call; from five (20 000) on a split row with ids is faster in a graph and as
+// fast call by call, where the second launch costs the host 4 us.  At four it is 3 us slower call by call and 2 to 3 faster in a graph.  (8 rows, fp32, us in a graph, unsplit and split, and call by call:
+//            no ids                        5 ids                          20 ids
+//    8 192   5.3   7.1    12.2 16.0    9.8 10.5    12.7 16.7    13.3 12.7    13.5 16.7
+//   12 000   7.2   8.6    12.2 16.1   12.4 12.8    12.7 16.8    16.1 15.9    16.2 17.0
+//   16 384   7.0   7.0    12.3 16.1   12.9 10.7    13.2 16.9    16.1 13.3    16.3 16.7
+//   20 000   9.0   8.4    12.1 16.1   16.0 12.5    16.3 16.7    18.6 15.8    18.8 17.2
+//   32 768  10.4   7.1    12.3 16.4   21.9 10.8    21.9 16.9    23.1 14.5    23.3 16.8
+//   48 000  14.8   8.3    15.1 16.3   28.1 12.6    28.3 16.7    30.8 16.9    31.0 17.2
+// one row, 64 rows and bf16 the same but for 1 or 2 us; 256 rows gain less.)
 int logprob_splits(int n_rows, int vocab, int n_top) {
     if (vocab <= 4 * kLogprobWaves * kLogprobStep) return 1;
     const int want = 1024 / (n_rows > 0 ? n_rows : 1), most = vocab / (kLogprobWaves * kLogprobStep), held = n_top ? kLogprobJoin / n_top : 64;
